@@ -119,6 +119,18 @@ typedef struct {
     int32_t num_pages, max_pages_per_seq;
 } fmtp_kv;
 
+/* The same cache held in 8 bits. k_pages / v_pages: dev [num_pages, Hkv, page_size, dh] e4m3 codes (OCP 8-bit floating
+ * point: 4 exponent and 3 mantissa bits, largest number 448, no infinity); k_scales / v_scales: dev [num_pages, Hkv], one
+ * fp32 scale for each block of tokens (a page) and KV head; a value is code * scale. Half the bytes of fmtp_kv plus 4 bytes in
+ * page_size * dh. num_pages * Hkv * page_size < 2^32. Pages are 16-byte aligned. */
+typedef struct {
+    uint8_t *k_pages, *v_pages;
+    float *k_scales, *v_scales;
+    const int32_t *block_table;
+    const int32_t *seq_lens;
+    int32_t num_pages, max_pages_per_seq;
+} fmtp_kv8;
+
 /* ---- context ------------------------------------------------------------------------ */
 
 /* Validates `shape` for the current device and creates a context (host memory only).
@@ -307,6 +319,80 @@ int fastmtp_target_step(fmtp_ctx *ctx, const fmtp_target_w *w, const int32_t *to
                         const fmtp_kv *layer_kvs, int B, int M,
                         fmtp_bf16 *out_h, fmtp_bf16 *out_logits, int32_t *out_argmax,
                         uint32_t *dev_status, void *stream);
+
+/* ---- an 8-bit K/V cache ------------------------------------------------------------------ */
+
+/* The paper keeps its caches in 16 bits; these calls have no counterpart in it. They hold the K/V of a target model in 8
+ * bits (see fmtp_kv8), which halves what a sequence costs in memory and what attention over it has to read.
+ * seq_lens[b] = L_b positions are committed; no call changes seq_lens. In all of them n_new is dev [B] or NULL: rows
+ * m < n_new[b] of sequence b count (values outside [0, M] are clamped, 0: the sequence sits this call out), NULL: all M. Rows that
+ * do not count are never read, and what belongs to them in an output is left as it was. */
+
+/* Quantises K/V rows into the cache as positions L_b + m.
+ *
+ *   k, v   dev bf16, row r = b*M + m at k + r*ld: [Hkv, dh] (keys after the rotary embedding). ld >= Hkv*dh, a multiple of
+ *          8 (so that k and v may be views of one fused projection's output); k, v 16-byte aligned
+ *
+ * For each block and KV head that gets new tokens, K and V apart: with a = the largest finite magnitude of the new tokens, the
+ * new scale is the smallest power of two s >= 2^-120 with a <= 448 s, or the present scale where that is larger and the block
+ * holds committed tokens (positions below L_b). New values become e4m3(x / s), nearest, halves to even; infinities become +-448,
+ * NaN stays NaN. Committed codes are multiplied by old scale / s and rounded again where s grew: exact for a cache that only
+ * these calls wrote, but for codes that become subnormal (below 2^-6 s). What lies at and behind L_b + n_new[b] (rejected drafts,
+ * nothing yet) neither counts nor changes. A block written by the call must belong to one sequence only; committed whole
+ * blocks may be shared.
+ * Positions without a slot (beyond max_pages_per_seq * page_size or max_ctx) and blocks whose page is out of range are skipped
+ * and flagged. Any B, M >= 1; uses no workspace; calls on the same inputs give the same cache (also when repeated). */
+int fastmtp_kv8_append(fmtp_ctx *ctx, const fmtp_bf16 *k, const fmtp_bf16 *v, long long ld, const fmtp_kv8 *kv, int B, int M,
+                       const int32_t *n_new, uint32_t *dev_status, void *stream);
+
+/* Reads the cache back: out[b, i] = bf16(code * scale) of position start[b] + i for i < count[b].
+ *
+ *   start, count  dev [B] or NULL: from position 0 on; everything that is committed from there on
+ *   out_k, out_v  dev [B, max_n, Hkv, dh] bf16, 16-byte aligned; rows i >= count[b] are left as they were
+ *
+ * At most max_n positions of a sequence are read; positions without a slot are left out and flagged. Uses no workspace. */
+int fastmtp_kv8_read(fmtp_ctx *ctx, const fmtp_kv8 *kv, int B, int max_n, const int32_t *start, const int32_t *count,
+                     fmtp_bf16 *out_k, fmtp_bf16 *out_v, uint32_t *dev_status, void *stream);
+
+/* Causal grouped-query attention over the cache. Row m of sequence b is a query at position L_b + m and sees positions
+ * 0 .. L_b + m, its own among them: call it after fastmtp_kv8_append of the same rows (seq_lens as for that call).
+ * out = softmax(q K^T / sqrt(dh)) V with K, V = code * scale.
+ *
+ *   q    dev bf16, row r = b*M + m at q + r*ldq: [Hq, dh] (after the rotary embedding); ldq >= Hq*dh, a multiple of 8;
+ *        q 16-byte aligned
+ *   out  dev [B, M, Hq, dh] bf16
+ *
+ * M = 1 is a decoding step, M = K+1 scores drafts, up to M = 64 a chunk of a prompt. A query that is not finite gives NaN. Queries
+ * beyond the last slot see all slots and are flagged. Requires B*M <= max_rows, M <= 64. Results do not depend on the batch
+ * a sequence is in; rows scored with another M agree within rounding (the context is cut at other places). */
+int fastmtp_kv8_attention(fmtp_ctx *ctx, const fmtp_bf16 *q, long long ldq, const fmtp_kv8 *kv, int B, int M, const int32_t *n_new,
+                          fmtp_bf16 *out, uint32_t *dev_status, void *stream);
+
+/* fastmtp_target_step over caches in 8 bits: the same arguments and outputs; every layer's rows go through
+ * fastmtp_kv8_append and fastmtp_kv8_attention (rotated queries, keys and values rounded to bf16 first). Runs on the batched
+ * path whatever B is (groups of up to 64 rows); M <= 64. Because a block's scale may have grown for a draft that was
+ * rejected since, speculative and plain greedy decoding agree within rounding, not bit for bit. */
+int fastmtp_target_step_kv8(fmtp_ctx *ctx, const fmtp_target_w *w, const int32_t *tokens, const fmtp_kv8 *layer_kvs, int B, int M,
+                            fmtp_bf16 *out_h, fmtp_bf16 *out_logits, int32_t *out_argmax, uint32_t *dev_status, void *stream);
+
+/* ---- log probabilities -------------------------------------------------------------------- */
+
+/* What a server answers with beside the tokens (no counterpart in the paper): for every row of logits the log probability
+ * of a given token, the entropy of the distribution (in nats) and the top_n most probable ids with their log probabilities. One
+ * pass over the logits; e.g. the [B, K+1, V] logits of a verification with the tokens it emitted, or a draft's fp32 logits.
+ *
+ *   logits           dev, row r at logits + r*ld (elements): [V] bf16, or fp32 if f32 != 0; ld >= V; aligned to an element
+ *   tokens           dev [rows] int32 (may be NULL if out_logprob is). An id outside [0, V) is flagged and taken as 0
+ *   out_logprob      dev [rows] fp32 or NULL        out_entropy   dev [rows] fp32 or NULL
+ *   out_top_ids      dev [rows, top_n] int32, best first, ties to the lowest id (NULL if top_n == 0)
+ *   out_top_logprobs dev [rows, top_n] fp32 or NULL
+ *
+ * A NaN logit counts as minus infinity. Equal infinite maxima share the probability. A row that holds nothing else than minus
+ * infinity gives log probabilities of minus infinity, entropy 0 and the lowest ids, and is flagged (FMTP_DEV_ALL_NAN).
+ * Requires rows <= 4096, 0 <= top_n <= 32, top_n <= V <= 2^30. Uses the context workspace; the same call gives the same bits. */
+int fastmtp_logprobs(fmtp_ctx *ctx, const void *logits, int f32, long long ld, const int32_t *tokens, int rows, int V,
+                     float *out_logprob, float *out_entropy, int top_n, int32_t *out_top_ids, float *out_top_logprobs,
+                     uint32_t *dev_status, void *stream);
 
 #ifdef __cplusplus
 }

@@ -27,7 +27,8 @@ EXPORTS = ["fmtp_create", "fmtp_destroy", "fmtp_workspace_bytes", "fmtp_set_work
            "fmtp_last_cuda_error", "fmtp_launch_count", "fmtp_tmem_launch_count", "fmtp_selftest_wait_timeout", "fmtp_selftest_inject_wait_timeout", "fmtp_selftest_ahead",
            "fastmtp_draft", "fastmtp_draft_host",
            "fastmtp_verify_accept", "fastmtp_verify_accept_host", "fastmtp_verify_accept_static", "fastmtp_accept_ids",
-           "fastmtp_target_step"]
+           "fastmtp_target_step", "fastmtp_kv8_append", "fastmtp_kv8_read", "fastmtp_kv8_attention", "fastmtp_target_step_kv8",
+           "fastmtp_logprobs"]
 
 _p = C.c_void_p
 
@@ -54,6 +55,11 @@ class fmtp_target_w(C.Structure):
 
 class fmtp_kv(C.Structure):
     _fields_ = [("k_pages", _p), ("v_pages", _p), ("block_table", _p), ("seq_lens", _p),
+                ("num_pages", C.c_int32), ("max_pages_per_seq", C.c_int32)]
+
+
+class fmtp_kv8(C.Structure):
+    _fields_ = [("k_pages", _p), ("v_pages", _p), ("k_scales", _p), ("v_scales", _p), ("block_table", _p), ("seq_lens", _p),
                 ("num_pages", C.c_int32), ("max_pages_per_seq", C.c_int32)]
 
 
@@ -97,6 +103,17 @@ lib.fastmtp_verify_accept_static.restype = C.c_int
 lib.fastmtp_target_step.argtypes = [_p, C.POINTER(fmtp_target_w), _p, C.POINTER(fmtp_kv), C.c_int, C.c_int,
                                     _p, _p, _p, _p, _p]
 lib.fastmtp_target_step.restype = C.c_int
+lib.fastmtp_kv8_append.argtypes = [_p, _p, _p, C.c_longlong, C.POINTER(fmtp_kv8), C.c_int, C.c_int, _p, _p, _p]
+lib.fastmtp_kv8_append.restype = C.c_int
+lib.fastmtp_kv8_read.argtypes = [_p, C.POINTER(fmtp_kv8), C.c_int, C.c_int, _p, _p, _p, _p, _p, _p]
+lib.fastmtp_kv8_read.restype = C.c_int
+lib.fastmtp_kv8_attention.argtypes = [_p, _p, C.c_longlong, C.POINTER(fmtp_kv8), C.c_int, C.c_int, _p, _p, _p, _p]
+lib.fastmtp_kv8_attention.restype = C.c_int
+lib.fastmtp_target_step_kv8.argtypes = [_p, C.POINTER(fmtp_target_w), _p, C.POINTER(fmtp_kv8), C.c_int, C.c_int,
+                                        _p, _p, _p, _p, _p]
+lib.fastmtp_target_step_kv8.restype = C.c_int
+lib.fastmtp_logprobs.argtypes = [_p, _p, C.c_int, C.c_longlong, _p, C.c_int, C.c_int, _p, _p, C.c_int, _p, _p, _p, _p]
+lib.fastmtp_logprobs.restype = C.c_int
 
 
 class FastMTPError(RuntimeError):
@@ -148,6 +165,12 @@ def target_w(t: dict):
 def kv(t: dict) -> fmtp_kv:
     return fmtp_kv(t["k_pages"].data_ptr(), t["v_pages"].data_ptr(), t["block_table"].data_ptr(),
                    t["seq_lens"].data_ptr(), int(t["k_pages"].shape[0]), int(t["block_table"].shape[1]))
+
+
+def kv8(t: dict) -> fmtp_kv8:
+    """The same over an 8-bit cache: e4m3 (or uint8) pools and fp32 scales."""
+    return fmtp_kv8(t["k_pages"].data_ptr(), t["v_pages"].data_ptr(), t["k_scales"].data_ptr(), t["v_scales"].data_ptr(),
+                    t["block_table"].data_ptr(), t["seq_lens"].data_ptr(), int(t["k_pages"].shape[0]), int(t["block_table"].shape[1]))
 
 
 def fmtp_selftest_wait_timeout(dev_status, limit_ms, dev_waited_ns=None, stream=None):
@@ -266,6 +289,39 @@ class Context:
         self._check(lib.fastmtp_target_step(self.handle, C.byref(w), _ptr(tokens), arr, B, M, _ptr(out_h),
                                             _ptr(out_logits), _ptr(out_argmax), _ptr(dev_status), _stream(stream)),
                     "fastmtp_target_step")
+
+    def fastmtp_kv8_append(self, k, v, kv: fmtp_kv8, B, M, n_new=None, dev_status=None, stream=None, ld=None):
+        """ld: elements between rows of k and of v (default: dense [B, M, Hkv, dh]); they may be views of a wider tensor."""
+        ld = self.shape.n_kv_heads * self.shape.head_dim if ld is None else int(ld)
+        self._check(lib.fastmtp_kv8_append(self.handle, _ptr(k), _ptr(v), ld, C.byref(kv), B, M, _ptr(n_new), _ptr(dev_status),
+                                           _stream(stream)), "fastmtp_kv8_append")
+
+    def fastmtp_kv8_read(self, kv: fmtp_kv8, B, max_n, out_k, out_v, start=None, count=None, dev_status=None, stream=None):
+        self._check(lib.fastmtp_kv8_read(self.handle, C.byref(kv), B, max_n, _ptr(start), _ptr(count), _ptr(out_k), _ptr(out_v),
+                                         _ptr(dev_status), _stream(stream)), "fastmtp_kv8_read")
+
+    def fastmtp_kv8_attention(self, q, kv: fmtp_kv8, B, M, out, n_new=None, dev_status=None, stream=None, ldq=None):
+        """ldq: elements between rows of q (default: dense [B, M, Hq, dh])."""
+        ldq = self.shape.n_q_heads * self.shape.head_dim if ldq is None else int(ldq)
+        self._check(lib.fastmtp_kv8_attention(self.handle, _ptr(q), ldq, C.byref(kv), B, M, _ptr(n_new), _ptr(out),
+                                              _ptr(dev_status), _stream(stream)), "fastmtp_kv8_attention")
+
+    def fastmtp_target_step_kv8(self, w: fmtp_target_w, tokens, layer_kvs, B, M, out_h=None, out_logits=None,
+                                out_argmax=None, dev_status=None, stream=None):
+        n = len(layer_kvs)
+        arr = (fmtp_kv8 * n)(*layer_kvs)
+        self._check(lib.fastmtp_target_step_kv8(self.handle, C.byref(w), _ptr(tokens), arr, B, M, _ptr(out_h), _ptr(out_logits),
+                                                _ptr(out_argmax), _ptr(dev_status), _stream(stream)), "fastmtp_target_step_kv8")
+
+    def fastmtp_logprobs(self, logits, tokens, rows, V, out_logprob=None, out_entropy=None, top_n=0, out_top_ids=None,
+                         out_top_logprobs=None, dev_status=None, stream=None, ld=None):
+        """logits: bf16 or fp32 (told by its dtype); ld: elements between its rows (default V)."""
+        if logits is not None and logits.dtype not in (torch.bfloat16, torch.float32):
+            raise FastMTPError(-3, "fastmtp_logprobs")
+        f32 = int(logits is not None and logits.dtype == torch.float32)
+        self._check(lib.fastmtp_logprobs(self.handle, _ptr(logits), f32, V if ld is None else int(ld), _ptr(tokens), rows, V,
+                                         _ptr(out_logprob), _ptr(out_entropy), top_n, _ptr(out_top_ids), _ptr(out_top_logprobs),
+                                         _ptr(dev_status), _stream(stream)), "fastmtp_logprobs")
 
 
 # ---- conversions between the generators' numpy arrays and torch tensors (no arithmetic) ------

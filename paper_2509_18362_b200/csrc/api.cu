@@ -1,10 +1,12 @@
 // C ABI of the library: context, workspace layout, argument validation and the entry points
 // declared in include/fastmtp.h. Host code only marshals; every step of the path runs in the
-// kernels of megakernel.cu and verify.cu.
+// kernels of megakernel.cu, batched.cu, verify.cu, kv8.cu and logprobs.cu.
 #include "../../include/fastmtp.h"
 #include "mega.cuh"
 #include "batched.cuh"
 #include "ahead.cuh"
+#include "kv8.cuh"
+#include "logprobs.cuh"
 
 #include <cmath>
 #include <cstdlib>
@@ -29,6 +31,8 @@ struct fmtp_ctx {
     size_t ctrl_off, ctrl_bytes;
     unsigned long long *vkeys;
     uint32_t *vcounter;
+    LpPart *lp_parts;          // fastmtp_logprobs
+    uint32_t *lp_counters;
     // staging for the *_host entry points (device side inside the workspace, host side pinned)
     bf16_t *st_h;
     int32_t *st_tok, *st_next, *st_out;
@@ -115,6 +119,8 @@ size_t layout(fmtp_ctx *c, unsigned char *base) {
     s.rope_sin = sinb;
     c->vkeys = cv.take<unsigned long long>(kVerifyMaxRows);
     c->vcounter = cv.take<uint32_t>(1);
+    c->lp_parts = cv.take<LpPart>((size_t)logprobs_slots(c->n_sm));
+    c->lp_counters = cv.take<uint32_t>(kLpMaxRows);
     c->st_h = cv.take<bf16_t>((size_t)RB * d);
     c->st_tok = cv.take<int32_t>((size_t)RB);
     c->st_next = cv.take<int32_t>((size_t)RB);
@@ -228,6 +234,28 @@ bool kv_ok(const fmtp_kv &kv) {
 void set_kv(KvPtrs &dst, const fmtp_kv &kv) {
     dst.k_pages = kv.k_pages; dst.v_pages = kv.v_pages; dst.block_table = kv.block_table;
     dst.seq_lens = kv.seq_lens; dst.num_pages = kv.num_pages; dst.max_pages = kv.max_pages_per_seq;
+}
+
+bool kv8_ok(const fmtp_kv8 &kv) {
+    return kv.k_pages && kv.v_pages && kv.k_scales && kv.v_scales && kv.block_table && kv.seq_lens && kv.num_pages > 0 && kv.max_pages_per_seq > 0 &&
+           aligned16(kv.k_pages) && aligned16(kv.v_pages) && (reinterpret_cast<uintptr_t>(kv.k_scales) & 3u) == 0 &&
+           (reinterpret_cast<uintptr_t>(kv.v_scales) & 3u) == 0;
+}
+// Rows of a pool are counted in 32 bits by the kernels.
+bool kv8_fits(const fmtp_ctx *c, const fmtp_kv8 &kv) {
+    return (unsigned long long)kv.num_pages * c->shape.n_kv_heads <= 0xffffffffull / (unsigned long long)c->shape.page_size;
+}
+// The cache of the sequences from b0 on.
+Kv8Ptrs kv8_ptrs(const fmtp_kv8 &kv, int b0) {
+    Kv8Ptrs p;
+    p.k_pages = kv.k_pages; p.v_pages = kv.v_pages; p.k_scales = kv.k_scales; p.v_scales = kv.v_scales;
+    p.block_table = kv.block_table + (size_t)b0 * kv.max_pages_per_seq;
+    p.seq_lens = kv.seq_lens + b0;
+    p.num_pages = kv.num_pages; p.max_pages = kv.max_pages_per_seq;
+    return p;
+}
+Kv8Shape kv8_shape(const fmtp_ctx *c) {
+    return Kv8Shape{c->shape.n_q_heads, c->shape.n_kv_heads, c->shape.head_dim, c->shape.page_size, c->shape.max_ctx};
 }
 
 int launch_mega(fmtp_ctx *c, MegaParams &p, cudaStream_t st) {
@@ -438,6 +466,61 @@ int check_draft_args(const fmtp_ctx *c, const fmtp_mtp_w *w, const void *h_last,
     return FMTP_OK;
 }
 
+// Everything the target calls can check on the host but their caches.
+int check_target_args(const fmtp_ctx *c, const fmtp_target_w *w, const void *tokens, const void *kvs, int B, int M) {
+    if (!c || !w || !tokens || !kvs) return FMTP_EINVAL;
+    if (!c->ws) return FMTP_ENOMEM;
+    if (B <= 0 || M <= 0) return FMTP_EINVAL;
+    const int nl = c->shape.n_layers;
+    if (nl <= 0 || (long long)B * M > c->shape.max_rows) return FMTP_ESHAPE;
+    if (!w->embed || !w->lm_head || !w->g_final || !w->layers) return FMTP_EINVAL;
+    if (!aligned16(w->embed) || !aligned16(w->lm_head) || !aligned16(w->g_final)) return FMTP_EINVAL;
+    for (int l = 0; l < nl; ++l) if (!layer_ok(w->layers[l])) return FMTP_EINVAL;
+    return FMTP_OK;
+}
+
+// A target call on the batched path (kvs or kv8s): groups of whole sequences, up to 64 rows each, every layer's weights streamed once
+// per group by the tensor-core GEMM path.
+int target_batched(fmtp_ctx *c, const fmtp_target_w *w, const int32_t *tokens, const fmtp_kv *kvs, const fmtp_kv8 *kv8s, int B, int M,
+                   fmtp_bf16 *out_h, fmtp_bf16 *out_logits, int32_t *out_argmax, uint32_t *dev_status, void *stream) {
+    if (out_h && !aligned16(out_h)) return FMTP_EINVAL;
+    const int nl = c->shape.n_layers, V = c->shape.vocab, d = c->shape.d, Gs = kBatchRows / M;
+    LayerPtrs layers[kMaxLayers];
+    KvPtrs lkv[kMaxLayers];
+    Kv8Ptrs lkv8[kMaxLayers];
+    for (int b0 = 0; b0 < B; b0 += Gs) {
+        const int Bg = (B - b0 < Gs) ? B - b0 : Gs;
+        BatchedTargetCall tc;
+        std::memset(&tc, 0, sizeof(tc));
+        tc.sh = c->bsh; tc.ws = c->bws;
+        tc.rope_cos = c->s.rope_cos; tc.rope_sin = c->s.rope_sin;
+        tc.n_sm = c->n_sm; tc.smem_optin = c->smem_optin; tc.ahead_budget = c->ahead_budget; tc.cache = &c->tmaps; tc.wait_limit_ns = kDefaultWaitNs;
+        tc.B = Bg; tc.M = M; tc.n_layers = nl;
+        tc.tokens = tokens + (size_t)b0 * M;
+        tc.out_h = out_h ? out_h + (size_t)b0 * M * d : nullptr;
+        tc.out_logits = out_logits ? out_logits + (size_t)b0 * M * V : nullptr;
+        tc.out_argmax = out_argmax ? out_argmax + (size_t)b0 * M : nullptr;
+        tc.user_status = dev_status;
+        tc.embed = w->embed; tc.lm_head = w->lm_head; tc.g_final = w->g_final;
+        for (int l = 0; l < nl; ++l) {
+            set_layer(layers[l], w->layers[l]);
+            if (kvs) {
+                set_kv(lkv[l], kvs[l]);
+                lkv[l].block_table += (size_t)b0 * kvs[l].max_pages_per_seq;
+                lkv[l].seq_lens += b0;
+            } else {
+                lkv8[l] = kv8_ptrs(kv8s[l], b0);
+            }
+        }
+        tc.layers = layers;
+        tc.kvs = kvs ? lkv : nullptr;
+        tc.kv8s = kv8s ? lkv8 : nullptr;
+        int err = batched_target(tc, static_cast<cudaStream_t>(stream), &c->launches);
+        if (err) return cuda_fail(c, (cudaError_t)err);
+    }
+    return FMTP_OK;
+}
+
 }  // namespace
 
 extern "C" {
@@ -611,56 +694,20 @@ int fastmtp_verify_accept_host(fmtp_ctx *c, const fmtp_bf16 *logits_host, const 
 int fastmtp_target_step(fmtp_ctx *c, const fmtp_target_w *w, const int32_t *tokens, const fmtp_kv *kvs, int B, int M,
                         fmtp_bf16 *out_h, fmtp_bf16 *out_logits, int32_t *out_argmax, uint32_t *dev_status,
                         void *stream) {
-    if (!c || !w || !tokens || !kvs) return FMTP_EINVAL;
-    if (!c->ws) return FMTP_ENOMEM;
-    if (B <= 0 || M <= 0) return FMTP_EINVAL;
+    int rc = check_target_args(c, w, tokens, kvs, B, M);
+    if (rc) return rc;
     const int nl = c->shape.n_layers;
-    if (nl <= 0 || (long long)B * M > c->shape.max_rows) return FMTP_ESHAPE;
-    if (!w->embed || !w->lm_head || !w->g_final || !w->layers) return FMTP_EINVAL;
-    if (!aligned16(w->embed) || !aligned16(w->lm_head) || !aligned16(w->g_final)) return FMTP_EINVAL;
-    for (int l = 0; l < nl; ++l) if (!layer_ok(w->layers[l]) || !kv_ok(kvs[l])) return FMTP_EINVAL;
+    for (int l = 0; l < nl; ++l) if (!kv_ok(kvs[l])) return FMTP_EINVAL;
     const int V = c->shape.vocab, d = c->shape.d;
-    if (B >= c->batched_min && M <= kBatchRows) {
-        // more rows than one launch of the persistent kernel takes: groups of whole sequences, up to 64 rows each,
-        // every layer's weights streamed once per group by the tensor-core GEMM path
-        if ((out_h && !aligned16(out_h))) return FMTP_EINVAL;
-        const int Gs = kBatchRows / M;
-        std::vector<LayerPtrs> layers(nl);
-        std::vector<KvPtrs> lkv(nl);
-        for (int b0 = 0; b0 < B; b0 += Gs) {
-            const int Bg = (B - b0 < Gs) ? B - b0 : Gs;
-            BatchedTargetCall tc;
-            std::memset(&tc, 0, sizeof(tc));
-            tc.sh = c->bsh; tc.ws = c->bws;
-            tc.rope_cos = c->s.rope_cos; tc.rope_sin = c->s.rope_sin;
-            tc.n_sm = c->n_sm; tc.smem_optin = c->smem_optin; tc.ahead_budget = c->ahead_budget; tc.cache = &c->tmaps; tc.wait_limit_ns = kDefaultWaitNs;
-            tc.B = Bg; tc.M = M; tc.n_layers = nl;
-            tc.tokens = tokens + (size_t)b0 * M;
-            tc.out_h = out_h ? out_h + (size_t)b0 * M * d : nullptr;
-            tc.out_logits = out_logits ? out_logits + (size_t)b0 * M * V : nullptr;
-            tc.out_argmax = out_argmax ? out_argmax + (size_t)b0 * M : nullptr;
-            tc.user_status = dev_status;
-            tc.embed = w->embed; tc.lm_head = w->lm_head; tc.g_final = w->g_final;
-            for (int l = 0; l < nl; ++l) {
-                set_layer(layers[l], w->layers[l]);
-                set_kv(lkv[l], kvs[l]);
-                lkv[l].block_table += (size_t)b0 * kvs[l].max_pages_per_seq;
-                lkv[l].seq_lens += b0;
-            }
-            tc.layers = layers.data();
-            tc.kvs = lkv.data();
-            int err = batched_target(tc, static_cast<cudaStream_t>(stream), &c->launches);
-            if (err) return cuda_fail(c, (cudaError_t)err);
-        }
-        return FMTP_OK;
-    }
+    if (B >= c->batched_min && M <= kBatchRows)
+        return target_batched(c, w, tokens, kvs, nullptr, B, M, out_h, out_logits, out_argmax, dev_status, stream);
     if (M > kMaxRows) return FMTP_ESHAPE;                // the rows of one sequence share a launch
     const int G = group_size(c, 1, B, M);
     if (G < 1) return FMTP_ESHAPE;
     for (int b0 = 0; b0 < B; b0 += G) {
         const int Bg = (B - b0 < G) ? B - b0 : G;
         MegaParams p;
-        int rc = configure(c, p, 1, Bg, M);
+        rc = configure(c, p, 1, Bg, M);
         if (rc) return rc;
         p.K = 1;
         p.n_layers = nl;
@@ -681,6 +728,86 @@ int fastmtp_target_step(fmtp_ctx *c, const fmtp_target_w *w, const int32_t *toke
         rc = launch_mega(c, p, static_cast<cudaStream_t>(stream));
         if (rc) return rc;
     }
+    return FMTP_OK;
+}
+
+int fastmtp_target_step_kv8(fmtp_ctx *c, const fmtp_target_w *w, const int32_t *tokens, const fmtp_kv8 *kvs, int B, int M,
+                            fmtp_bf16 *out_h, fmtp_bf16 *out_logits, int32_t *out_argmax, uint32_t *dev_status, void *stream) {
+    int rc = check_target_args(c, w, tokens, kvs, B, M);
+    if (rc) return rc;
+    for (int l = 0; l < c->shape.n_layers; ++l) {
+        if (!kv8_ok(kvs[l])) return FMTP_EINVAL;
+        if (!kv8_fits(c, kvs[l])) return FMTP_ESHAPE;
+    }
+    if (M > kBatchRows) return FMTP_ESHAPE;
+    return target_batched(c, w, tokens, nullptr, kvs, B, M, out_h, out_logits, out_argmax, dev_status, stream);
+}
+
+int fastmtp_kv8_append(fmtp_ctx *c, const fmtp_bf16 *k, const fmtp_bf16 *v, long long ld, const fmtp_kv8 *kv, int B, int M,
+                       const int32_t *n_new, uint32_t *dev_status, void *stream) {
+    if (!c || !k || !v || !kv) return FMTP_EINVAL;
+    if (!c->ws) return FMTP_ENOMEM;
+    if (B <= 0 || M <= 0 || !aligned16(k) || !aligned16(v) || !kv8_ok(*kv)) return FMTP_EINVAL;
+    if (ld < (long long)c->shape.n_kv_heads * c->shape.head_dim || ld % 8) return FMTP_EINVAL;
+    if (!kv8_fits(c, *kv) || M > c->shape.max_ctx) return FMTP_ESHAPE;
+    int err = kv8_append(kv8_shape(c), k, v, ld, kv8_ptrs(*kv, 0), B, M, n_new, dev_status ? dev_status : c->s.status,
+                         static_cast<cudaStream_t>(stream), &c->launches);
+    return err ? cuda_fail(c, (cudaError_t)err) : FMTP_OK;
+}
+
+int fastmtp_kv8_read(fmtp_ctx *c, const fmtp_kv8 *kv, int B, int max_n, const int32_t *start, const int32_t *count,
+                     fmtp_bf16 *out_k, fmtp_bf16 *out_v, uint32_t *dev_status, void *stream) {
+    if (!c || !kv || !out_k || !out_v) return FMTP_EINVAL;
+    if (!c->ws) return FMTP_ENOMEM;
+    if (B <= 0 || max_n <= 0 || !aligned16(out_k) || !aligned16(out_v) || !kv8_ok(*kv)) return FMTP_EINVAL;
+    if (!kv8_fits(c, *kv)) return FMTP_ESHAPE;
+    int err = kv8_read(kv8_shape(c), kv8_ptrs(*kv, 0), B, max_n, start, count, out_k, out_v, dev_status ? dev_status : c->s.status,
+                       static_cast<cudaStream_t>(stream), &c->launches);
+    return err ? cuda_fail(c, (cudaError_t)err) : FMTP_OK;
+}
+
+int fastmtp_kv8_attention(fmtp_ctx *c, const fmtp_bf16 *q, long long ldq, const fmtp_kv8 *kv, int B, int M, const int32_t *n_new,
+                          fmtp_bf16 *out, uint32_t *dev_status, void *stream) {
+    if (!c || !q || !kv || !out) return FMTP_EINVAL;
+    if (!c->ws) return FMTP_ENOMEM;
+    if (B <= 0 || M <= 0 || !aligned16(q) || (reinterpret_cast<uintptr_t>(out) & 1u) || !kv8_ok(*kv)) return FMTP_EINVAL;
+    const int row = c->shape.n_q_heads * c->shape.head_dim;
+    if (ldq < row || ldq % 8) return FMTP_EINVAL;
+    if (!kv8_fits(c, *kv) || M > kBatchRows || (long long)B * M > c->shape.max_rows) return FMTP_ESHAPE;
+    const int Gs = kBatchRows / M;
+    for (int b0 = 0; b0 < B; b0 += Gs) {
+        Kv8AttnCall a;
+        std::memset(&a, 0, sizeof(a));
+        a.sh = kv8_shape(c);
+        a.kv = kv8_ptrs(*kv, b0);
+        a.q = q + (long long)b0 * M * ldq; a.ldq = ldq;
+        a.B = B - b0 < Gs ? B - b0 : Gs; a.M = M;
+        a.n_new = n_new ? n_new + b0 : nullptr;
+        a.part = c->bws.att_part; a.max_chunks = c->bws.max_chunks;
+        a.out = out + (size_t)b0 * M * row;
+        a.status = dev_status ? dev_status : c->s.status;
+        a.n_sm = c->n_sm;
+        int err = kv8_attention(a, static_cast<cudaStream_t>(stream), &c->launches);
+        if (err) return cuda_fail(c, (cudaError_t)err);
+    }
+    return FMTP_OK;
+}
+
+int fastmtp_logprobs(fmtp_ctx *c, const void *logits, int f32, long long ld, const int32_t *tokens, int rows, int V, float *out_logprob,
+                     float *out_entropy, int top_n, int32_t *out_top_ids, float *out_top_logprobs, uint32_t *dev_status, void *stream) {
+    if (!c || !logits || (out_logprob && !tokens) || (top_n > 0 && !out_top_ids)) return FMTP_EINVAL;
+    if (!c->ws) return FMTP_ENOMEM;
+    if (rows <= 0 || V <= 0 || top_n < 0 || top_n > V || ld < V) return FMTP_EINVAL;
+    if ((reinterpret_cast<uintptr_t>(logits) & (f32 ? 3u : 1u)) != 0) return FMTP_EINVAL;
+    if (rows > kLpMaxRows || top_n > kLpMaxTop || V > (1 << 30)) return FMTP_ESHAPE;
+    LpCall a;
+    std::memset(&a, 0, sizeof(a));
+    a.logits = logits; a.f32 = f32 != 0; a.ld = ld; a.tokens = tokens; a.rows = rows; a.V = V; a.top = top_n;
+    a.out_logprob = out_logprob; a.out_entropy = out_entropy; a.out_ids = out_top_ids; a.out_tops = out_top_logprobs;
+    a.parts = c->lp_parts; a.counters = c->lp_counters; a.status = dev_status ? dev_status : c->s.status; a.n_sm = c->n_sm;
+    int err = logprobs_launch(a, static_cast<cudaStream_t>(stream));
+    if (err) return cuda_fail(c, (cudaError_t)err);
+    c->launches++;
     return FMTP_OK;
 }
 

@@ -338,6 +338,34 @@ __global__ void qkv_finish_kernel(const QkvArgs a) {
     dst[e + half] = f32_bf16bits(hi);
 }
 
+// ---- the same for a cache in 8 bits: the rows' rotated queries and keys and their values, rounded to bf16, side by side, as
+// kv8_append and kv8_attention take them. Block = (head, row), dh/2 threads.
+__global__ void qkv_rows_kernel(const QkvArgs a) {
+    chain_release();
+    const int head = blockIdx.x, r = blockIdx.y, e = threadIdx.x, half = a.dh >> 1;
+    const int max_tokens = min(a.kv.max_pages * a.page, a.max_ctx);
+    bool valid;
+    const int pos = min(geo_pos(a.geo, a.kv, r, &valid), max_tokens - 1);
+    const bool rotate = head < a.Hq + a.Hkv;
+    const float cs = rotate ? a.rope_cos[(size_t)pos * half + e] : 1.f, sn = rotate ? a.rope_sin[(size_t)pos * half + e] : 0.f;
+    chain_wait();
+    float lo = 0.f, hi = 0.f;
+    float x[kBatchMaxSplits], y[kBatchMaxSplits];
+#pragma unroll
+    for (int s = 0; s < kBatchMaxSplits; ++s)
+        if (s < a.splits) {
+            const float *pp = a.partial + ((size_t)s * a.rows + r) * a.ldp + head * a.dh;
+            x[s] = pp[e];
+            y[s] = pp[e + half];
+        }
+#pragma unroll
+    for (int s = 0; s < kBatchMaxSplits; ++s)
+        if (s < a.splits) { lo += x[s]; hi += y[s]; }
+    bf16_t *dst = a.q + (size_t)r * (a.qdim + 2 * a.kvdim) + head * a.dh;
+    dst[e] = f32_bf16bits(lo * cs - hi * sn);
+    dst[e + half] = f32_bf16bits(hi * cs + lo * sn);
+}
+
 // ---- attention. A work item is one 256-token chunk of one (sequence, KV head) for up to ROWS rows of the sequence: the
 // M rows of a target step or of a draft's extend step share the K/V stream (ROWS = 4), later draft steps have one row
 // (ROWS = 1). The Hq/Hkv query heads of the group share it as well. One persistent CTA per SM; its eight compute warps
@@ -1175,6 +1203,7 @@ size_t batched_layout(BatchedWs &ws, unsigned char *base, const BatchedShape &sh
     ws.hout = reinterpret_cast<float *>(take((size_t)rows * sh.d * 4));
     ws.q = reinterpret_cast<bf16_t *>(take((size_t)rows * 2 * qdim * 2));
     ws.att_part = reinterpret_cast<float *>(take((size_t)rows * sh.Hq * ws.max_chunks * (sh.dh + 2) * 4));
+    ws.qkv = reinterpret_cast<bf16_t *>(take((size_t)rows * (qdim + 2 * kvdim) * 2));
     ws.keys_bytes = (size_t)(sh.max_K > 1 ? sh.max_K : 1) * kBatchRows * 8 + 256;
     ws.keys = reinterpret_cast<unsigned long long *>(take(ws.keys_bytes));
     ws.id_bitmap = reinterpret_cast<uint32_t *>(take((size_t)((sh.V + 31) / 32) * 4));
@@ -1357,7 +1386,11 @@ int batched_target(const BatchedTargetCall &c, cudaStream_t st, long long *launc
     if ((rc = post(0, 0, c.layers[0].g_in))) return rc;
     for (int l = 0; l < c.n_layers; ++l) {
         const LayerPtrs &L = c.layers[l];
-        const KvPtrs &kv = c.kvs[l];
+        KvPtrs kv{};
+        if (c.kv8s) {                             // (positions and capacity only)
+            kv.block_table = c.kv8s[l].block_table; kv.seq_lens = c.kv8s[l].seq_lens;
+            kv.num_pages = c.kv8s[l].num_pages; kv.max_pages = c.kv8s[l].max_pages;
+        } else kv = c.kvs[l];
         GemmArgs g{};
         g.a[0] = L.wq; g.a[1] = L.wk; g.a[2] = L.wv;
         g.a_rows[0] = qdim; g.a_rows[1] = kvdim; g.a_rows[2] = kvdim; g.n_seg = 3; g.epi = EPI_PARTIAL;
@@ -1365,12 +1398,21 @@ int batched_target(const BatchedTargetCall &c, cudaStream_t st, long long *launc
         {
             QkvArgs a{};
             a.qdim = qdim; a.kvdim = kvdim; a.dh = sh.dh; a.Hq = sh.Hq; a.Hkv = sh.Hkv; a.splits = g.splits; a.rows = R;
-            a.ldp = ws.ldp; a.page = sh.page; a.max_ctx = sh.max_ctx; a.geo = geo; a.partial = ws.partial; a.q = ws.q;
+            a.ldp = ws.ldp; a.page = sh.page; a.max_ctx = sh.max_ctx; a.geo = geo; a.partial = ws.partial; a.q = c.kv8s ? ws.qkv : ws.q;
             a.kv = kv; a.rope_cos = c.rope_cos; a.rope_sin = c.rope_sin; a.status = ws.status;
             ++*launches;
-            if ((rc = (int)launch_chained(qkv_finish_kernel, dim3(sh.Hq + 2 * sh.Hkv, R), dim3(sh.dh / 2), 0, st, a))) return rc;
+            auto kern = c.kv8s ? qkv_rows_kernel : qkv_finish_kernel;
+            if ((rc = (int)launch_chained(kern, dim3(sh.Hq + 2 * sh.Hkv, R), dim3(sh.dh / 2), 0, st, a))) return rc;
         }
-        if ((rc = attention(sh, ws, kv, geo, R, c.n_sm, c.wait_limit_ns, 0, c.cache, st, launches))) return rc;
+        if (c.kv8s) {
+            const Kv8Shape s8{sh.Hq, sh.Hkv, sh.dh, sh.page, sh.max_ctx};
+            const int ld = qdim + 2 * kvdim;
+            if ((rc = kv8_append(s8, ws.qkv + qdim, ws.qkv + qdim + kvdim, ld, c.kv8s[l], c.B, c.M, nullptr, ws.status, st, launches))) return rc;
+            Kv8AttnCall a{};
+            a.sh = s8; a.kv = c.kv8s[l]; a.q = ws.qkv; a.ldq = ld; a.B = c.B; a.M = c.M;
+            a.part = ws.att_part; a.max_chunks = ws.max_chunks; a.xop = ws.xop0; a.ld_xop = ws.ld0; a.status = ws.status; a.n_sm = c.n_sm;
+            if ((rc = kv8_attention(a, st, launches))) return rc;
+        } else if ((rc = attention(sh, ws, kv, geo, R, c.n_sm, c.wait_limit_ns, 0, c.cache, st, launches))) return rc;
         g = GemmArgs{};
         g.a[0] = L.wo; g.a_rows[0] = d; g.n_seg = 1; g.epi = EPI_PARTIAL;
         g.ahead[0] = L.w_gate; g.ahead[1] = L.w_up; g.ahead_rows = sh.F; g.ahead_ld = d; g.ahead_limit = gemm_ahead_limit(c.ahead_budget, sh.F);

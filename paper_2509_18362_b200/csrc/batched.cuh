@@ -4,6 +4,7 @@
 // and fewer than 3 sequences at 7B-class widths -- run there instead.)
 #pragma once
 #include "mega.cuh"
+#include "kv8.cuh"
 
 namespace fmtp {
 
@@ -37,6 +38,7 @@ struct BatchedWs {
     float *hout;                  // [rows][d]   final-normed hidden state (recursed in fp32)
     bf16_t *q;                    // rotated, scaled queries as high and low bf16 parts
     float *att_part;              // [rows][Hq][max_chunks][dh + 2]  (o, m, l) per context chunk
+    bf16_t *qkv;                  // [rows][qdim + 2 kvdim] rotated queries and keys, values (target steps over 8-bit caches)
     unsigned long long *keys;     // [max_K][kBatchRows] argmax keys
     uint32_t *id_bitmap;          // [ceil(V/32)] membership bits of the subset
     int32_t *sorted_ids;          // [V] the subset in ascending id order
@@ -93,7 +95,8 @@ struct BatchedTargetCall {
     uint32_t *user_status;
     const bf16_t *embed, *lm_head, *g_final;
     const LayerPtrs *layers;              // host array [n_layers]
-    const KvPtrs *kvs;                    // host array [n_layers]
+    const KvPtrs *kvs;                    // host array [n_layers], or
+    const Kv8Ptrs *kv8s;                  // the same in 8 bits
 };
 
 // Enqueues one target-decoder step (all layers, final norm, full output head) for B sequences of M rows.

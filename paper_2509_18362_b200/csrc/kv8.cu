@@ -1,0 +1,811 @@
+// Operators over a paged K/V cache held in 8 bits: see kv8.cuh.
+#include "kv8.cuh"
+#include "batched.cuh"
+#include "ptx.cuh"
+#include "umma.cuh"
+
+namespace fmtp {
+
+namespace {
+
+constexpr uint32_t kDevBadPage = 0x2u, kDevBadPos = 0x4u;
+constexpr int kMaxLen = 1 << 30;      // a longer committed length is the caller's error: flagged like any position without a slot
+
+__device__ __forceinline__ int kv8_len(const Kv8Ptrs &kv, int b) { return min(max(kv.seq_lens[b], 0), kMaxLen); }
+__device__ __forceinline__ int kv8_rows(const int32_t *n_new, int b, int M) { return n_new ? min(max(n_new[b], 0), M) : M; }
+// Quotient by the page size: a shift for powers of two (shift >= 0).
+__device__ __forceinline__ int page_of(int pos, int page, int shift) { return shift >= 0 ? pos >> shift : pos / page; }
+int shift_of(int page) {
+    for (int s = 0; s < 31; ++s) if (page == (1 << s)) return s;
+    return -1;
+}
+
+// ---- e4m3 (4 significant bits, largest number 448, smallest 2^-9, NaN but no infinity)
+__device__ __forceinline__ uint32_t to_e4m3x2(float lo, float hi) {          // nearest, halves to even; beyond +-448: +-448
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f32 %0, %1, %2;" : "=h"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t e4m3x2_f16x2(uint16_t v) {               // exact
+    uint32_t r;
+    asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(v));
+    return r;
+}
+__device__ __forceinline__ void f16x2_f32(uint32_t h, float &a, float &b) {
+    asm("{.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(a), "=f"(b) : "r"(h));
+}
+__device__ __forceinline__ void e4m3x4_f32(uint32_t w, float (&x)[4]) {
+    f16x2_f32(e4m3x2_f16x2((uint16_t)(w & 0xffffu)), x[0], x[1]);
+    f16x2_f32(e4m3x2_f16x2((uint16_t)(w >> 16)), x[2], x[3]);
+}
+__device__ __forceinline__ uint32_t to_e4m3x4(const float (&x)[4], float f) {
+    return to_e4m3x2(x[0] * f, x[1] * f) | (to_e4m3x2(x[2] * f, x[3] * f) << 16);
+}
+// Largest finite magnitude of eight bf16 values as bf16 bits (infinities and NaN do not count), joined to `m` (two lanes).
+__device__ __forceinline__ uint32_t finite_max(uint32_t m, uint32_t w) {
+    const uint32_t a = w & 0x7fff7fffu;
+    return __vmaxu2(m, a & ~__vcmpgeu2(a, 0x7f807f80u));
+}
+// Smallest power of two s >= 2^-120 with amax <= 448 s, from amax's bf16 bits: amax = 1.f * 2^E, 448 = 1.75 * 2^8.
+constexpr int kMinScaleExp = -120;
+__device__ __forceinline__ float scale_for(uint32_t amax_bits) {
+    int e = (int)(amax_bits >> 7) - 127 - 8 + ((amax_bits & 0x7fu) > 0x60u ? 1 : 0);
+    e = max(e, kMinScaleExp);
+    return __uint_as_float((uint32_t)(e + 127) << 23);
+}
+
+// ---- append: a warp quantises the new tokens of one block of one sequence and KV head (K and V are separate warps). Positions
+// [first, end) of the block are new, those before `first` committed. The new scale covers the new tokens and is never below the
+// committed tokens' one; where it grows, these are rounded once more (a shift of the exponent, exact but for subnormal codes).
+// What lies behind `end` (rejected drafts, nothing) is left and does not count.
+struct Append8Args {
+    int Hkv, page, shift, max_ctx, B, M, nb;         // nb: blocks that M rows can touch
+    const bf16_t *k, *v;
+    long long ld;
+    const int32_t *n_new;
+    Kv8Ptrs kv;
+    uint32_t *status;
+};
+constexpr int kAppendWarps = 4;
+
+template <int DH>
+__global__ void __launch_bounds__(kAppendWarps * 32) kv8_append_kernel(const Append8Args a) {
+    chain_release();
+    chain_wait();
+    constexpr int LPR = DH / 8;                      // lanes per row: eight values each
+    constexpr int RPI = 32 / LPR;                    // rows per step of the warp
+    constexpr int NT = 16 / RPI;                     // steps of a 16-token tile
+    const int lane = threadIdx.x & 31, piece = lane % LPR, sub = lane / LPR;
+    const long long w = (long long)blockIdx.x * kAppendWarps + (threadIdx.x >> 5);
+    const int head2 = (int)(w % (2 * a.Hkv));        // key heads, then value heads
+    const long long t = w / (2 * a.Hkv);
+    const int i = (int)(t % a.nb), b = (int)(t / a.nb);
+    if (b >= a.B) return;
+    const int L = kv8_len(a.kv, b), n = kv8_rows(a.n_new, b, a.M);
+    const int max_tokens = min((int)min((long long)a.kv.max_pages * a.page, (long long)kMaxLen), a.max_ctx);
+    const int blk = page_of(L, a.page, a.shift) + i;
+    const int at = blk * a.page;                     // position of the block's first token
+    if (at >= L + n) return;
+    const int first = max(L, at);
+    int end = min(L + n, at + a.page);
+    if (end > max_tokens) {                          // positions without a slot: flagged, not written
+        if (lane == 0) atomicOr(a.status, kDevBadPos);
+        end = max_tokens;
+        if (first >= end) return;
+    }
+    const bool is_v = head2 >= a.Hkv;
+    const int kvh = is_v ? head2 - a.Hkv : head2;
+    const int page = a.kv.block_table[(size_t)b * a.kv.max_pages + blk];
+    if ((unsigned)page >= (unsigned)a.kv.num_pages) {          // not written either
+        if (lane == 0) atomicOr(a.status, kDevBadPage);
+        return;
+    }
+    const size_t slot = (size_t)page * a.Hkv + kvh;
+    uint8_t *dst = (is_v ? a.kv.v_pages : a.kv.k_pages) + slot * a.page * DH + piece * 8;
+    float *scale = (is_v ? a.kv.v_scales : a.kv.k_scales) + slot;
+    const bf16_t *src = (is_v ? a.v : a.k) + ((long long)b * a.M - L) * a.ld + (long long)kvh * DH + piece * 8;      // + position * ld
+    const float s_old = first > at ? *scale : 0.f;
+    uint4 x[NT];
+    auto load = [&](int p0) {
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            const int p = p0 + u * RPI + sub;
+            x[u] = p < end ? *reinterpret_cast<const uint4 *>(src + p * a.ld) : make_uint4(0, 0, 0, 0);
+        }
+    };
+    uint32_t m = 0;
+    for (int p0 = first; p0 < end; p0 += 16) {       // (more than one turn where a block is longer than 16 tokens)
+        load(p0);
+#pragma unroll
+        for (int u = 0; u < NT; ++u) m = finite_max(finite_max(finite_max(finite_max(m, x[u].x), x[u].y), x[u].z), x[u].w);
+    }
+    m = max(m & 0xffffu, m >> 16);
+    m = __reduce_max_sync(0xffffffffu, m);
+    float s = scale_for(m);
+    if (first > at) {
+        if (s_old >= s) s = s_old;
+        else {
+            const float f = s_old / s;               // (a scale that is not a positive number makes the committed codes zeros or NaN)
+            for (int p = at + sub; p < first; p += RPI) {
+                uint2 *c = reinterpret_cast<uint2 *>(dst + (size_t)(p - at) * DH);
+                uint2 v = *c;
+                float y[4];
+                e4m3x4_f32(v.x, y);
+                v.x = to_e4m3x4(y, f);
+                e4m3x4_f32(v.y, y);
+                v.y = to_e4m3x4(y, f);
+                *c = v;
+            }
+        }
+    }
+    if (lane == 0) *scale = s;
+    const float inv = 1.0f / s;                      // exact for a power of two
+    for (int p0 = first; p0 < end; p0 += 16) {
+        if (end - first > 16) load(p0);
+#pragma unroll
+        for (int u = 0; u < NT; ++u) {
+            const int p = p0 + u * RPI + sub;
+            if (p >= end) continue;
+            const float y[4] = {bf16lo_f32(x[u].x), bf16hi_f32(x[u].x), bf16lo_f32(x[u].y), bf16hi_f32(x[u].y)};
+            const float z[4] = {bf16lo_f32(x[u].z), bf16hi_f32(x[u].z), bf16lo_f32(x[u].w), bf16hi_f32(x[u].w)};
+            *reinterpret_cast<uint2 *>(dst + (size_t)(p - at) * DH) = make_uint2(to_e4m3x4(y, inv), to_e4m3x4(z, inv));
+        }
+    }
+}
+
+// ---- reading back: a warp takes 16 tokens of one sequence and KV head, 16 codes per lane and step.
+struct Read8Args {
+    int Hkv, page, shift, max_ctx, B, max_n, tiles;
+    const int32_t *start, *count;
+    Kv8Ptrs kv;
+    bf16_t *out_k, *out_v;
+    uint32_t *status;
+};
+constexpr int kReadWarps = 4;
+
+__device__ __forceinline__ uint4 dequant8(uint32_t a, uint32_t b, float s) {
+    float x[4], y[4];
+    e4m3x4_f32(a, x);
+    e4m3x4_f32(b, y);
+    uint4 r;
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.x) : "f"(x[1] * s), "f"(x[0] * s));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.y) : "f"(x[3] * s), "f"(x[2] * s));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.z) : "f"(y[1] * s), "f"(y[0] * s));
+    asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r.w) : "f"(y[3] * s), "f"(y[2] * s));
+    return r;
+}
+
+template <int DH>
+__global__ void __launch_bounds__(kReadWarps * 32) kv8_read_kernel(const Read8Args a) {
+    chain_release();
+    chain_wait();
+    constexpr int LPR = DH / 16, RPI = 32 / LPR, NT = 16 / RPI;
+    const int lane = threadIdx.x & 31, piece = lane % LPR, sub = lane / LPR;
+    const long long w = (long long)blockIdx.x * kReadWarps + (threadIdx.x >> 5);
+    const int kvh = (int)(w % a.Hkv);
+    const long long t = w / a.Hkv;
+    const int tile = (int)(t % a.tiles), b = (int)(t / a.tiles);
+    if (b >= a.B) return;
+    const int max_tokens = min((int)min((long long)a.kv.max_pages * a.page, (long long)kMaxLen), a.max_ctx);
+    const int s0 = a.start ? min(max(a.start[b], 0), kMaxLen) : 0;
+    int n = a.count ? max(a.count[b], 0) : max(kv8_len(a.kv, b) - s0, 0);
+    n = min(n, a.max_n);
+    if (n > max_tokens - s0) {
+        if (lane == 0 && tile == 0) atomicOr(a.status, kDevBadPos);
+        n = max(max_tokens - s0, 0);
+    }
+    const int i0 = tile * 16;
+    if (i0 >= n) return;
+    size_t row[NT];
+    float sk[NT], sv[NT];
+    uint4 ck[NT], cv[NT];
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        const int pos = s0 + min(i0 + u * RPI + sub, n - 1), blk = page_of(pos, a.page, a.shift);
+        int page = a.kv.block_table[(size_t)b * a.kv.max_pages + blk];
+        if ((unsigned)page >= (unsigned)a.kv.num_pages) { atomicOr(a.status, kDevBadPage); page = 0; }
+        const size_t slot = (size_t)page * a.Hkv + kvh;
+        sk[u] = a.kv.k_scales[slot];
+        sv[u] = a.kv.v_scales[slot];
+        row[u] = slot * a.page + (pos - blk * a.page);
+    }
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        ck[u] = ldnc128(a.kv.k_pages + row[u] * DH + piece * 16);
+        cv[u] = ldnc128(a.kv.v_pages + row[u] * DH + piece * 16);
+    }
+#pragma unroll
+    for (int u = 0; u < NT; ++u) {
+        const int i = i0 + u * RPI + sub;
+        if (i >= n) continue;
+        const size_t o = (((size_t)b * a.max_n + i) * a.Hkv + kvh) * DH + piece * 16;
+        *reinterpret_cast<uint4 *>(a.out_k + o) = dequant8(ck[u].x, ck[u].y, sk[u]);
+        *reinterpret_cast<uint4 *>(a.out_k + o + 8) = dequant8(ck[u].z, ck[u].w, sk[u]);
+        *reinterpret_cast<uint4 *>(a.out_v + o) = dequant8(cv[u].x, cv[u].y, sv[u]);
+        *reinterpret_cast<uint4 *>(a.out_v + o + 8) = dequant8(cv[u].z, cv[u].w, sv[u]);
+    }
+}
+
+// ---- attention. The (row, query head) pairs that share a KV head of a sequence are dealt to tiles of eight; a work item is one chunk of
+// a sequence's context for one KV head and a set of RW * WR tiles. A CTA of four warps walks a contiguous range of items: WR
+// warps take RW tiles each, and the context's 32-token blocks go round the WT = 4 / WR groups of such warps.
+//
+// Both products run on mma.sync.m16n8k32 with e4m3 operands (twice the rate of the 16-bit forms at twice the depth): K and V enter
+// as they lie in the cache, nothing is converted. The exact counterpart of an e4m3 code needs more than e4m3's four bits, so
+// the A operand carries a tile's eight pairs twice: rows 0-7 the high parts, rows 8-15 what is left, scaled up. Two parts hold a
+// bf16 query exactly (eight bits; the second one reaches 2^-23 of the head's largest element) and a probability to 2^-9 of
+// itself or 2^-23 of the chunk's largest. The accumulator's lanes are the A operand's in both products, so probabilities
+// never leave their registers: a lane holds pair lane/4 and tokens 2q, 2q+1 (q = lane % 4) of each eight, and the contraction over
+// tokens takes them in that order: V's transposed 16-bit ldmatrix gives dims 2u, 2u+1 of two tokens in a word, and two byte
+// permutations per two words sort them by dimension.
+//
+// Scores are scaled by the token's K scale, probabilities by its V scale over the largest seen so far (O carries both factors).
+// A stage of the ring is 32 tokens of K and V with their scales, copied by the warps that read them (16-byte cp.async, any page
+// size: a lane looks up where one token lies, one stage ahead).
+struct Attn8Args {
+    int Hq, Hkv, gq, page, shift, max_ctx, max_chunks, B, M;
+    const bf16_t *q;
+    long long ldq;
+    const int32_t *n_new;
+    Kv8Ptrs kv;
+    float *part;
+    bf16_t *out, *xop;
+    int ld_xop;
+    uint32_t *status;
+};
+
+constexpr int kA8Warps = 4, kA8Threads = kA8Warps * 32;
+constexpr int kA8Blk = 32;                           // tokens of a stage
+constexpr float kP8 = 256.f, kPlo8 = 32.f, kQlo8 = 16.f;      // scales of a probability, of its second part, of a query's second part
+
+// Tokens of a chunk: a function of the sequence's committed length and of the call's rows per sequence, never of the batch.
+__host__ __device__ __forceinline__ int chunk8(int n_ctx, int pairs) {
+    int c = pairs > 32 ? 1024 : pairs > 8 ? 512 : 256;
+    while ((n_ctx + c - 1) / c > 64) c *= 2;
+    return c;
+}
+
+template <int DH, int WR>
+struct Attn8Smem {
+    static constexpr int WT = kA8Warps / WR;
+    static constexpr int S = WT == 4 ? 3 : WT == 2 ? 5 : 8;                  // stages
+    static constexpr int KV = kA8Blk * DH;                                   // bytes of a stage's K (or V) codes
+    static constexpr int STAGE = 2 * KV + 2 * kA8Blk * 4;
+    static constexpr int O_ML = WT * S * STAGE;                              // [4 warps][8 pairs] (max, sum)
+    static constexpr int O_LAST = O_ML + kA8Warps * 8 * 8;                   // [4 warps] the stage that a warp read last
+    static constexpr int O_TAB = O_LAST + kA8Warps * 4;
+    static constexpr int TOTAL = O_TAB + (4 * kBatchRows + 1) * 4;
+};
+
+__device__ __forceinline__ void mma_e4m3(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+        : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
+        : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+__device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ void ldsm4_trans(uint32_t addr, uint32_t (&r)[4]) {
+    asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
+                 : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
+}
+__device__ __forceinline__ float2 lds64f(uint32_t addr) {
+    float2 v;
+    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+    return v;
+}
+__device__ __forceinline__ float exp2_approx(float x) {      // 2^x; results below the normal range are zero, as is 2^-inf
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void *src, uint32_t bytes) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+// Two values as the two e4m3 parts: high parts in the low half of the result, what is left of them (times `up`) in the upper half.
+__device__ __forceinline__ uint32_t split_e4m3(float a, float b, float up) {
+    const uint32_t hi = to_e4m3x2(a, b);
+    float ha, hb;
+    f16x2_f32(e4m3x2_f16x2((uint16_t)hi), ha, hb);
+    return hi | (to_e4m3x2((a - ha) * up, (b - hb) * up) << 16);
+}
+// Byte position of 16-byte piece c of token row t: the eight rows an ldmatrix phase reads lie in different banks.
+template <int DH>
+__device__ __forceinline__ uint32_t piece_at(int t, int c) {
+    return (uint32_t)(t * DH + ((DH == 128 ? (c ^ (t & 7)) : (c ^ ((t >> 1) & 3))) << 4));
+}
+
+struct Item8 {                                       // one (sequence, KV head, tile set, chunk)
+    int seq, kvh, set, chunk, t0, t1;                // tokens [t0, t1) of the context
+};
+
+template <int DH, int RW, int WR>
+__global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
+    chain_release();
+    chain_wait();
+    using Lay = Attn8Smem<DH, WR>;
+    constexpr int WT = Lay::WT, S = Lay::S, KS = DH / 32, ND = DH / 16, TILES = RW * WR;
+    extern __shared__ __align__(128) unsigned char smem[];
+    int *prefix = reinterpret_cast<int *>(smem + Lay::O_TAB);              // [B + 1] items before a sequence
+    int *tpos = prefix + kBatchRows + 1;                                   // position of a sequence's row 0
+    int *tval = tpos + kBatchRows;                                         // its rows that count
+    int *tchk = tval + kBatchRows;                                         // tokens of its chunks
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wr = warp % WR, wt = warp / WR;
+    const int max_tokens = min((int)min((long long)a.kv.max_pages * a.page, (long long)kMaxLen), a.max_ctx);
+    const int gq = a.gq;
+    auto row_ctx = [&](int pos0, int m) -> int { return min(pos0 + m, max_tokens - 1) + 1; };     // positions that row m sees
+    if (warp == 0) {                                 // two sequences per lane
+        int cnt[2];
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int s = 2 * lane + u;
+            cnt[u] = 0;
+            if (s < a.B) {
+                const int len = kv8_len(a.kv, s), nv = kv8_rows(a.n_new, s, a.M);
+                const int c = chunk8(row_ctx(len, a.M - 1), a.M * gq);
+                tpos[s] = len; tval[s] = nv; tchk[s] = c;
+                if (nv > 0) {
+                    cnt[u] = (row_ctx(len, nv - 1) + c - 1) / c * a.Hkv * ((nv * gq + 8 * TILES - 1) / (8 * TILES));
+                    if (len + nv > max_tokens && blockIdx.x == 0) atomicOr(a.status, kDevBadPos);
+                }
+            }
+        }
+        int incl = cnt[0] + cnt[1];
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+            const int t = __shfl_up_sync(0xffffffffu, incl, o);
+            if (lane >= o) incl += t;
+        }
+        if (2 * lane <= a.B) prefix[2 * lane] = incl - cnt[0] - cnt[1];
+        if (2 * lane + 1 <= a.B) prefix[2 * lane + 1] = incl - cnt[1];
+        if (lane == 31 && a.B == 2 * 32) prefix[a.B] = incl;
+    }
+    __syncthreads();
+    const int n_items = prefix[a.B];
+    const int i_begin = (int)(((long long)blockIdx.x * n_items) / gridDim.x), i_end = (int)(((long long)(blockIdx.x + 1) * n_items) / gridDim.x);
+    auto load_item = [&](Item8 &it, int item) {
+        int s = it.seq;                              // items come in ascending order: search on from the last one
+        while (prefix[s + 1] <= item) ++s;
+        it.seq = s;
+        const int rem = item - prefix[s], nv = tval[s], c = tchk[s];
+        const int chunks = (row_ctx(tpos[s], nv - 1) + c - 1) / c, sets = (nv * gq + 8 * TILES - 1) / (8 * TILES);
+        it.chunk = rem % chunks;
+        const int t = rem / chunks;
+        it.set = t % sets;
+        it.kvh = t / sets;
+        it.t0 = it.chunk * c;
+        // what the set's last row sees of the chunk (nothing: t1 <= t0)
+        it.t1 = min(it.t0 + c, row_ctx(tpos[s], min(nv - 1, ((it.set + 1) * 8 * TILES - 1) / gq)));
+    };
+
+    // ---- copying: the next stage to ask for is block `ctok` of item `citem`; a lane holds where token `lane` of it lies
+    const uint64_t policy = l2_evict_first();
+    unsigned char *ring = smem + (size_t)wt * S * Lay::STAGE;
+    Item8 ci;
+    ci.seq = 0;
+    int citem = i_begin, ctok = 0, cpage = 0, cin = 0;
+    bool cmore = citem < i_end;
+    auto look_up = [&]() {
+        const int pos = min(ctok + lane, ci.t1 - 1), blk = page_of(pos, a.page, a.shift);
+        cin = pos - blk * a.page;
+        cpage = a.kv.block_table[(size_t)ci.seq * a.kv.max_pages + blk];
+    };
+    auto seek = [&]() {                              // from ctok on, the first block with tokens
+        while (cmore && ctok >= ci.t1) {
+            if (++citem >= i_end) { cmore = false; break; }
+            load_item(ci, citem);
+            ctok = ci.t0 + wt * kA8Blk;
+        }
+        if (cmore) look_up();
+    };
+    int cslot = 0;
+    auto copy_stage = [&]() {
+        if (cmore) {
+            if ((unsigned)cpage >= (unsigned)a.kv.num_pages) { atomicOr(a.status, kDevBadPage); cpage = 0; }
+            const uint32_t sb = smem_u32(ring + (size_t)cslot * Lay::STAGE);
+            const uint32_t slot = (uint32_t)cpage * (uint32_t)a.Hkv + (uint32_t)ci.kvh;
+            const uint32_t row = slot * (uint32_t)a.page + (uint32_t)cin;
+            constexpr int LPR = DH / 16, RPI = 32 / LPR;
+            const int piece = lane % LPR, sub = lane / LPR;
+#pragma unroll
+            for (int u = wr; u < kA8Blk / RPI; u += WR) {
+                const int t = u * RPI + sub;
+                const size_t off = (size_t)__shfl_sync(0xffffffffu, row, t) * DH + piece * 16;
+                const uint32_t d = sb + piece_at<DH>(t, piece), n = ctok + t < ci.t1 ? 16u : 0u;      // zeros beyond what is seen
+                cp_async16_off_hint<0>(d, a.kv.k_pages + off, n, policy);
+                cp_async16_off_hint<0>(d + Lay::KV, a.kv.v_pages + off, n, policy);
+            }
+            if (wr == 0) {
+                const uint32_t n = ctok + lane < ci.t1 ? 4u : 0u;
+                cp_async4(sb + 2 * Lay::KV + lane * 4, a.kv.k_scales + slot, n);
+                cp_async4(sb + 2 * Lay::KV + kA8Blk * 4 + lane * 4, a.kv.v_scales + slot, n);
+            }
+            if (++cslot == S) cslot = 0;
+            ctok += WT * kA8Blk;
+            seek();
+        }
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    if (cmore) {
+        load_item(ci, citem);
+        ctok = ci.t0 + wt * kA8Blk;
+        seek();
+    }
+#pragma unroll
+    for (int s = 0; s < S - 1; ++s) copy_stage();
+
+    // ---- computing
+    const int hrow = lane >> 2, kq = (lane & 3) * 2;
+    const float sm_scale = (1.0f / sqrtf((float)DH)) * 1.4426950408889634f;
+    // ldmatrix rows: K: tokens 0-7 of two pieces, then tokens 8-15 of them; V: four groups of eight tokens of one piece
+    const int ktok = (lane & 7) + ((lane >> 4) << 3), kpc = (lane >> 3) & 1;
+    uint32_t qa[RW][KS][4];
+    float fs[RW];                                    // score of a query's code times a key's code -> log2 units, without the K scale
+    int pn[RW];                                      // positions that the lane's pair sees (any, where there is no such pair)
+    int prow[RW];                                    // its row; the sequence's number of rows: no such pair
+    int qkey_seq = -1, qkey = -1, slot = 0;
+    Item8 it;
+    it.seq = 0;
+    for (int item = i_begin; item < i_end; ++item) {
+        load_item(it, item);
+        const int key = it.kvh * 4096 + it.set;      // (at most 64 * 8 / 8 sets)
+        const int nv = tval[it.seq];
+        if (it.seq != qkey_seq || key != qkey) {     // the queries stay in registers while the CTA's items are chunks of one context
+            qkey_seq = it.seq;
+            qkey = key;
+#pragma unroll
+            for (int r = 0; r < RW; ++r) {
+                const int pair = (it.set * TILES + wr * RW + r) * 8 + hrow, m = pair / gq, h = pair - m * gq;
+                const bool there = pair < nv * gq;
+                prow[r] = there ? m : nv;
+                pn[r] = there ? row_ctx(tpos[it.seq], m) : kMaxLen;
+                const bf16_t *qp = a.q + ((long long)it.seq * a.M + (there ? m : 0)) * a.ldq + (long long)(it.kvh * gq + (there ? h : 0)) * DH;
+                uint2 x[2 * KS];
+                uint32_t am = 0;
+#pragma unroll
+                for (int j = 0; j < 2 * KS; ++j) {
+                    x[j] = *reinterpret_cast<const uint2 *>(qp + j * 16 + kq * 2);
+                    am = finite_max(finite_max(am, x[j].x), x[j].y);
+                }
+                am = max(am & 0xffffu, am >> 16);
+                am = max(am, __shfl_xor_sync(0xffffffffu, am, 1));
+                am = max(am, __shfl_xor_sync(0xffffffffu, am, 2));
+                const float qs = scale_for(am), inv = 1.0f / qs;
+                fs[r] = qs * sm_scale;
+#pragma unroll
+                for (int j = 0; j < 2 * KS; ++j) {
+                    float y[4] = {bf16lo_f32(x[j].x), bf16hi_f32(x[j].x), bf16lo_f32(x[j].y), bf16hi_f32(x[j].y)};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) y[i] = fabsf(y[i]) < INFINITY ? y[i] * inv : __uint_as_float(0x7fffffffu);   // an infinite query: NaN
+                    const uint32_t p0 = split_e4m3(y[0], y[1], kQlo8), p1 = split_e4m3(y[2], y[3], kQlo8);
+                    qa[r][j >> 1][(j & 1) * 2] = __byte_perm(p0, p1, 0x5410);
+                    qa[r][j >> 1][(j & 1) * 2 + 1] = __byte_perm(p0, p1, 0x7632);
+                }
+            }
+        }
+        float m_run[RW], l_run[RW], o[RW][2 * ND][4];
+        float sv_run = 0.f;                          // largest V scale so far
+#pragma unroll
+        for (int r = 0; r < RW; ++r) {
+            m_run[r] = -INFINITY;
+            l_run[r] = 0.f;
+#pragma unroll
+            for (int i = 0; i < 2 * ND; ++i) o[r][i][0] = o[r][i][1] = o[r][i][2] = o[r][i][3] = 0.f;
+        }
+        int last_slot = slot;
+        for (int tb = it.t0 + wt * kA8Blk; tb < it.t1; tb += WT * kA8Blk) {
+            asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
+            if (WR > 1) bar_sync(1 + wt, WR * 32); else __syncwarp();
+            copy_stage();                            // into the stage that was read last
+            const uint32_t sb = smem_u32(ring + (size_t)slot * Lay::STAGE);
+            last_slot = slot;
+            if (++slot == S) slot = 0;
+            // ---- scores
+            float sc[RW][8];
+#pragma unroll
+            for (int g = 0; g < 2; ++g) {            // 16 tokens at a time
+                float c[RW][2][4];
+#pragma unroll
+                for (int r = 0; r < RW; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) c[r][0][i] = c[r][1][i] = 0.f;
+#pragma unroll
+                for (int ks = 0; ks < KS; ++ks) {
+                    uint32_t kf[4];
+                    ldsm4(sb + piece_at<DH>(g * 16 + ktok, 2 * ks + kpc), kf);
+#pragma unroll
+                    for (int r = 0; r < RW; ++r) {
+                        mma_e4m3(c[r][0], qa[r][ks][0], qa[r][ks][1], qa[r][ks][2], qa[r][ks][3], kf[0], kf[1]);
+                        mma_e4m3(c[r][1], qa[r][ks][0], qa[r][ks][1], qa[r][ks][2], qa[r][ks][3], kf[2], kf[3]);
+                    }
+                }
+#pragma unroll
+                for (int nt = 0; nt < 2; ++nt) {
+                    const float2 sk = lds64f(sb + 2 * Lay::KV + (g * 16 + nt * 8 + kq) * 4);
+#pragma unroll
+                    for (int r = 0; r < RW; ++r) {
+                        sc[r][g * 4 + nt * 2] = (c[r][nt][0] + c[r][nt][2] * (1.f / kQlo8)) * (fs[r] * sk.x);
+                        sc[r][g * 4 + nt * 2 + 1] = (c[r][nt][1] + c[r][nt][3] * (1.f / kQlo8)) * (fs[r] * sk.y);
+                    }
+                }
+            }
+            // ---- V scales of the lane's tokens over the largest seen so far
+            float sv[8], sv_new = sv_run;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const float2 x = lds64f(sb + 2 * Lay::KV + kA8Blk * 4 + (i * 8 + kq) * 4);
+                sv[2 * i] = x.x;
+                sv[2 * i + 1] = x.y;
+                sv_new = fmaxf(sv_new, fmaxf(x.x, x.y));
+            }
+            sv_new = fmaxf(sv_new, __shfl_xor_sync(0xffffffffu, sv_new, 1));
+            sv_new = fmaxf(sv_new, __shfl_xor_sync(0xffffffffu, sv_new, 2));
+            const float sv_inv = sv_new > 0.f ? 1.0f / sv_new : 0.f, sv_corr = sv_new == sv_run ? 1.0f : sv_run * sv_inv;
+            sv_run = sv_new;
+#pragma unroll
+            for (int i = 0; i < 8; ++i) sv[i] *= sv_inv * kP8;
+            // ---- probabilities
+            uint32_t pa[RW][4];
+            bool edge = false;
+#pragma unroll
+            for (int r = 0; r < RW; ++r) {
+                const int left = pn[r] - tb;         // tokens of the block that the pair sees
+                if (__any_sync(0xffffffffu, left < kA8Blk)) {
+                    edge = true;
+#pragma unroll
+                    for (int i = 0; i < 8; ++i)
+                        if ((i >> 1) * 8 + kq + (i & 1) >= left) sc[r][i] = -INFINITY;
+                }
+                float mx = fmaxf(fmaxf(fmaxf(sc[r][0], sc[r][1]), fmaxf(sc[r][2], sc[r][3])), fmaxf(fmaxf(sc[r][4], sc[r][5]), fmaxf(sc[r][6], sc[r][7])));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
+                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
+                const float m_new = fmaxf(m_run[r], mx);
+                const float m_use = m_new == -INFINITY ? 0.f : m_new;            // nothing seen yet: every probability is 2^-inf
+                const float corr = exp2_approx(m_run[r] - m_use);
+                m_run[r] = m_new;
+                float p[8];
+#pragma unroll
+                for (int i = 0; i < 8; ++i) p[i] = exp2_approx(sc[r][i] - m_use);
+                l_run[r] = l_run[r] * corr + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
+                const float oc = corr * sv_corr;
+                if (__any_sync(0xffffffffu, oc != 1.0f)) {
+#pragma unroll
+                    for (int i = 0; i < 2 * ND; ++i) { o[r][i][0] *= oc; o[r][i][1] *= oc; o[r][i][2] *= oc; o[r][i][3] *= oc; }
+                }
+#pragma unroll
+                for (int g = 0; g < 2; ++g) {
+                    const uint32_t p0 = split_e4m3(p[4 * g] * sv[4 * g], p[4 * g + 1] * sv[4 * g + 1], kPlo8);
+                    const uint32_t p1 = split_e4m3(p[4 * g + 2] * sv[4 * g + 2], p[4 * g + 3] * sv[4 * g + 3], kPlo8);
+                    pa[r][2 * g] = __byte_perm(p0, p1, 0x5410);
+                    pa[r][2 * g + 1] = __byte_perm(p0, p1, 0x7632);
+                }
+            }
+            // ---- weighted values
+            if (!edge) {
+#pragma unroll
+                for (int c = 0; c < ND; ++c) {
+                    uint32_t v[4];
+                    ldsm4_trans(sb + Lay::KV + piece_at<DH>(lane, c), v);
+                    const uint32_t e0 = __byte_perm(v[0], v[1], 0x6420), e1 = __byte_perm(v[2], v[3], 0x6420);       // dims 16c + 2u
+                    const uint32_t d0 = __byte_perm(v[0], v[1], 0x7531), d1 = __byte_perm(v[2], v[3], 0x7531);       // dims 16c + 2u + 1
+#pragma unroll
+                    for (int r = 0; r < RW; ++r) {
+                        mma_e4m3(o[r][2 * c], pa[r][0], pa[r][1], pa[r][2], pa[r][3], e0, e1);
+                        mma_e4m3(o[r][2 * c + 1], pa[r][0], pa[r][1], pa[r][2], pa[r][3], d0, d1);
+                    }
+                }
+            } else {
+                // Rows of the tiles see different parts of the block. What a row does not see is a later row's value, which need not be
+                // a number, so neither may a probability of 0 meet it nor another row's sum take part in its products: one pass per
+                // row, with the values that it does not see cleared, whose products only its own pairs add.
+#pragma unroll
+                for (int r = 0; r < RW; ++r) {
+                    const int m0 = __shfl_sync(0xffffffffu, prow[r], 0), m1 = min(__shfl_sync(0xffffffffu, prow[r], 28), nv - 1);
+#pragma unroll 1
+                    for (int m = m0; m <= m1; ++m) {
+                        const bool mine = prow[r] == m;
+                        const int left = row_ctx(tpos[it.seq], m) - tb;
+                        if (left <= 0) continue;
+                        uint32_t keep[2];
+#pragma unroll
+                        for (int g = 0; g < 2; ++g) {
+                            const int t = g * 16 + kq;
+                            keep[g] = (t < left ? 0xffu : 0u) | (t + 1 < left ? 0xff00u : 0u) | (t + 8 < left ? 0xff0000u : 0u) | (t + 9 < left ? 0xff000000u : 0u);
+                        }
+#pragma unroll
+                        for (int c = 0; c < ND; ++c) {
+                            uint32_t v[4];
+                            ldsm4_trans(sb + Lay::KV + piece_at<DH>(lane, c), v);
+                            float e[4] = {0.f, 0.f, 0.f, 0.f}, d[4] = {0.f, 0.f, 0.f, 0.f};
+                            mma_e4m3(e, pa[r][0], pa[r][1], pa[r][2], pa[r][3], __byte_perm(v[0], v[1], 0x6420) & keep[0], __byte_perm(v[2], v[3], 0x6420) & keep[1]);
+                            mma_e4m3(d, pa[r][0], pa[r][1], pa[r][2], pa[r][3], __byte_perm(v[0], v[1], 0x7531) & keep[0], __byte_perm(v[2], v[3], 0x7531) & keep[1]);
+                            if (mine) {
+#pragma unroll
+                                for (int i = 0; i < 4; ++i) { o[r][2 * c][i] += e[i]; o[r][2 * c + 1][i] += d[i]; }
+                            }
+                        }
+                    }
+                }
+            }
+        }
+        // ---- the chunk's partial result: o relative to the maximum, sum and maximum
+        const float of = sv_run * (1.f / kP8);
+#pragma unroll
+        for (int r = 0; r < RW; ++r) {
+            l_run[r] += __shfl_xor_sync(0xffffffffu, l_run[r], 1);
+            l_run[r] += __shfl_xor_sync(0xffffffffu, l_run[r], 2);
+        }
+        auto value = [&](int r, int c) -> float4 {   // dims 16c + 2 kq + 0..3 of the lane's pair
+            return make_float4((o[r][2 * c][0] + o[r][2 * c][2] * (1.f / kPlo8)) * of, (o[r][2 * c + 1][0] + o[r][2 * c + 1][2] * (1.f / kPlo8)) * of,
+                               (o[r][2 * c][1] + o[r][2 * c][3] * (1.f / kPlo8)) * of, (o[r][2 * c + 1][1] + o[r][2 * c + 1][3] * (1.f / kPlo8)) * of);
+        };
+        auto part_of = [&](int pair) -> float * {    // where a pair's partial goes
+            const int m = pair / gq, h = pair - m * gq;
+            return a.part + ((((size_t)it.seq * a.M + m) * a.Hq + (size_t)it.kvh * gq + h) * a.max_chunks + it.chunk) * (DH + 2);
+        };
+        if constexpr (WT == 1) {
+#pragma unroll
+            for (int r = 0; r < RW; ++r) {
+                if (prow[r] == nv || pn[r] <= it.t0) continue;       // no such pair, or it sees nothing of the chunk
+                float *out = part_of((it.set * TILES + wr * RW + r) * 8 + hrow);
+#pragma unroll
+                for (int c = 0; c < ND; ++c) {
+                    const float4 v = value(r, c);
+                    *reinterpret_cast<float2 *>(out + c * 16 + kq * 2) = make_float2(v.x, v.y);
+                    *reinterpret_cast<float2 *>(out + c * 16 + kq * 2 + 2) = make_float2(v.z, v.w);
+                }
+                if ((lane & 3) == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(m_run[r], l_run[r]);
+            }
+        } else {
+            // The WT groups' results are joined in shared memory: each warp leaves its own in the stage that it read last (free until
+            // its next copy), then all threads add them up in the groups' order.
+            static_assert(RW == 1 && 8 * (DH + 4) * 4 * WR <= Lay::STAGE, "partial results fit the stage read last");
+            float2 *ml = reinterpret_cast<float2 *>(smem + Lay::O_ML);
+            int *last = reinterpret_cast<int *>(smem + Lay::O_LAST);
+            const int blocks = (it.t1 - it.t0 + kA8Blk - 1) / kA8Blk;        // groups beyond have none of them
+            if (wt < blocks) {
+                if (WR > 1) bar_sync(1 + wt, WR * 32);                       // all readers of the stage are done
+                float *mine = reinterpret_cast<float *>(ring + (size_t)last_slot * Lay::STAGE) + (wr * 8 + hrow) * (DH + 4);
+#pragma unroll
+                for (int c = 0; c < ND; ++c) *reinterpret_cast<float4 *>(mine + c * 16 + kq * 2) = value(0, c);
+                if ((lane & 3) == 0) ml[warp * 8 + hrow] = make_float2(m_run[0], l_run[0]);
+                if (lane == 0) last[warp] = last_slot;
+            }
+            __syncthreads();
+            for (int i = threadIdx.x; i < WR * 8 * (DH / 4); i += kA8Threads) {              // four dims of a pair
+                const int ps = i / (DH / 4), d = (i - ps * (DH / 4)) * 4, w0 = ps >> 3, s = ps & 7;
+                const int pair = it.set * TILES * 8 + ps;
+                if (pair >= nv * gq || row_ctx(tpos[it.seq], pair / gq) <= it.t0) continue;
+                float mm = -INFINITY;
+#pragma unroll
+                for (int g = 0; g < WT; ++g)
+                    if (g < blocks) mm = fmaxf(mm, ml[(g * WR + w0) * 8 + s].x);
+                const float mu = mm == -INFINITY ? 0.f : mm;
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                float l = 0.f;
+#pragma unroll
+                for (int g = 0; g < WT; ++g) {
+                    if (g >= blocks) continue;
+                    const int w = g * WR + w0;
+                    const float2 x = ml[w * 8 + s];
+                    const float f = exp2_approx(x.x - mu);
+                    const float4 v = *reinterpret_cast<const float4 *>(smem + (size_t)(g * S + last[w]) * Lay::STAGE + ((size_t)(w0 * 8 + s) * (DH + 4) + d) * 4);
+                    acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
+                    l += x.y * f;
+                }
+                float *out = part_of(pair);
+                *reinterpret_cast<float2 *>(out + d) = make_float2(acc.x, acc.y);
+                *reinterpret_cast<float2 *>(out + d + 2) = make_float2(acc.z, acc.w);
+                if (d == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(mm, l);
+            }
+            __syncthreads();
+        }
+    }
+    asm volatile("cp.async.wait_all;" ::: "memory");
+}
+
+// ---- a row's chunks joined in ascending order. Block = (query head, row), a thread per element; a warp's lanes hold the weights of
+// 32 chunks, and a batch of the chunks' values is requested before they are known.
+template <int DH>
+__global__ void __launch_bounds__(DH) kv8_merge_kernel(const Attn8Args a) {
+    chain_release();
+    chain_wait();
+    const int head = blockIdx.x, r = blockIdx.y, j = threadIdx.x, lane = j & 31;
+    const int seq = r / a.M, m = r - seq * a.M;
+    if (m >= kv8_rows(a.n_new, seq, a.M)) return;    // padding: left as it was
+    const int max_tokens = min((int)min((long long)a.kv.max_pages * a.page, (long long)kMaxLen), a.max_ctx);
+    const int len = kv8_len(a.kv, seq);
+    const int n = min(len + m, max_tokens - 1) + 1, c = chunk8(min(len + a.M - 1, max_tokens - 1) + 1, a.M * a.gq);
+    const int chunks = (n + c - 1) / c;
+    constexpr int stride = DH + 2, G = 16;
+    const float *base = a.part + ((size_t)r * a.Hq + head) * a.max_chunks * stride;
+    float mx = -INFINITY;
+    for (int i = lane; i < chunks; i += 32) mx = fmaxf(mx, base[(size_t)i * stride + DH]);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+    const float mu = mx == -INFINITY ? 0.f : mx;
+    float acc = 0.f, l = 0.f;
+    for (int c0 = 0; c0 < chunks; c0 += 32) {
+        const int i = c0 + lane;
+        const float w = i < chunks ? exp2f(base[(size_t)i * stride + DH] - mu) : 0.f;
+        float lw = i < chunks ? base[(size_t)i * stride + DH + 1] * w : 0.f;
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) lw += __shfl_xor_sync(0xffffffffu, lw, o);
+        l += lw;
+#pragma unroll
+        for (int g0 = 0; g0 < 32; g0 += G) {
+            if (c0 + g0 >= chunks) break;
+            float v[G];
+#pragma unroll
+            for (int u = 0; u < G; ++u) v[u] = c0 + g0 + u < chunks ? base[(size_t)(c0 + g0 + u) * stride + j] : 0.f;
+#pragma unroll
+            for (int u = 0; u < G; ++u) acc += v[u] * __shfl_sync(0xffffffffu, w, g0 + u);
+        }
+    }
+    const float o = acc / l;
+    if (a.xop) {
+        uint16_t hi, lo;
+        split_bf16(o, hi, lo);
+        a.xop[(size_t)(2 * r) * a.ld_xop + head * DH + j] = hi;
+        a.xop[(size_t)(2 * r + 1) * a.ld_xop + head * DH + j] = lo;
+    } else {
+        a.out[((size_t)r * a.Hq + head) * DH + j] = f32_bf16bits(o);
+    }
+}
+
+template <int DH, int RW, int WR>
+int attn8_launch(const Attn8Args &a, int rows, int n_sm, cudaStream_t st) {
+    auto kern = kv8_attn_kernel<DH, RW, WR>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Attn8Smem<DH, WR>::TOTAL);
+    if (e == cudaSuccess) e = launch_chained(kern, dim3(2 * n_sm), dim3(kA8Threads), (size_t)Attn8Smem<DH, WR>::TOTAL, st, a);
+    if (e == cudaSuccess) e = launch_chained(kv8_merge_kernel<DH>, dim3(a.Hq, rows), dim3(DH), 0, st, a);
+    return (int)e;
+}
+
+template <int DH>
+int attn8_pick(const Attn8Args &a, int rows, int n_sm, cudaStream_t st) {
+    const int pairs = a.M * a.gq;
+    if (pairs <= 8) return attn8_launch<DH, 1, 1>(a, rows, n_sm, st);
+    if (pairs <= 16) return attn8_launch<DH, 1, 2>(a, rows, n_sm, st);
+    if (pairs <= 32) return attn8_launch<DH, 1, 4>(a, rows, n_sm, st);
+    return attn8_launch<DH, 2, 4>(a, rows, n_sm, st);
+}
+
+}  // namespace
+
+int kv8_append(const Kv8Shape &sh, const bf16_t *k, const bf16_t *v, long long ld, const Kv8Ptrs &kv, int B, int M, const int32_t *n_new,
+               uint32_t *status, cudaStream_t st, long long *launches) {
+    Append8Args a{};
+    a.Hkv = sh.Hkv; a.page = sh.page; a.shift = shift_of(sh.page); a.max_ctx = sh.max_ctx; a.B = B; a.M = M;
+    a.nb = (M + sh.page - 2) / sh.page + 1;
+    a.k = k; a.v = v; a.ld = ld; a.n_new = n_new; a.kv = kv; a.status = status;
+    const long long warps = (long long)B * a.nb * 2 * sh.Hkv, blocks = (warps + kAppendWarps - 1) / kAppendWarps;
+    if (blocks > 0x7fffffffll) return (int)cudaErrorInvalidConfiguration;
+    ++*launches;
+    auto kern = sh.dh == 128 ? kv8_append_kernel<128> : kv8_append_kernel<64>;
+    return (int)launch_chained(kern, dim3((unsigned)blocks), dim3(kAppendWarps * 32), 0, st, a);
+}
+
+int kv8_read(const Kv8Shape &sh, const Kv8Ptrs &kv, int B, int max_n, const int32_t *start, const int32_t *count, bf16_t *out_k, bf16_t *out_v,
+             uint32_t *status, cudaStream_t st, long long *launches) {
+    Read8Args a{};
+    a.Hkv = sh.Hkv; a.page = sh.page; a.shift = shift_of(sh.page); a.max_ctx = sh.max_ctx; a.B = B; a.max_n = max_n;
+    a.tiles = (max_n + 15) / 16; a.start = start; a.count = count; a.kv = kv; a.out_k = out_k; a.out_v = out_v; a.status = status;
+    const long long warps = (long long)B * a.tiles * sh.Hkv, blocks = (warps + kReadWarps - 1) / kReadWarps;
+    if (blocks > 0x7fffffffll) return (int)cudaErrorInvalidConfiguration;
+    ++*launches;
+    auto kern = sh.dh == 128 ? kv8_read_kernel<128> : kv8_read_kernel<64>;
+    return (int)launch_chained(kern, dim3((unsigned)blocks), dim3(kReadWarps * 32), 0, st, a);
+}
+
+int kv8_attention(const Kv8AttnCall &c, cudaStream_t st, long long *launches) {
+    Attn8Args a{};
+    a.Hq = c.sh.Hq; a.Hkv = c.sh.Hkv; a.gq = c.sh.Hq / c.sh.Hkv; a.page = c.sh.page; a.shift = shift_of(c.sh.page); a.max_ctx = c.sh.max_ctx;
+    a.max_chunks = c.max_chunks; a.B = c.B; a.M = c.M; a.q = c.q; a.ldq = c.ldq; a.n_new = c.n_new; a.kv = c.kv; a.part = c.part;
+    a.out = c.out; a.xop = c.xop; a.ld_xop = c.ld_xop; a.status = c.status;
+    *launches += 2;
+    return c.sh.dh == 128 ? attn8_pick<128>(a, c.B * c.M, c.n_sm, st) : attn8_pick<64>(a, c.B * c.M, c.n_sm, st);
+}
+
+}  // namespace fmtp

@@ -1,0 +1,34 @@
+// Log probabilities of given tokens, entropy and top alternatives of rows of logits: see include/fastmtp.h.
+#pragma once
+#include "mega.cuh"
+
+namespace fmtp {
+
+constexpr int kLpMaxRows = 4096;
+constexpr int kLpMaxTop = 32;
+
+// What a CTA knows of its part of a row.
+struct LpPart {
+    float m, s, t, pad;                              // maximum, sum of e^(x - m), sum of e^(x - m) (x - m)
+    unsigned long long top[kLpMaxTop];               // (value, id) keys, best first; 0: none
+};
+
+struct LpCall {
+    const void *logits;                              // [rows][ld], bf16 or fp32
+    int f32;
+    long long ld;
+    const int32_t *tokens;                           // [rows] or NULL
+    int rows, V, top;
+    float *out_logprob, *out_entropy;                // [rows] or NULL
+    int32_t *out_ids;                                // [rows][top]
+    float *out_tops;                                 // [rows][top]
+    LpPart *parts;                                   // [logprobs_slots(n_sm)]
+    uint32_t *counters;                              // [kLpMaxRows], zero between calls
+    uint32_t *status;
+    int n_sm;
+};
+
+int logprobs_slots(int n_sm);
+int logprobs_launch(const LpCall &c, cudaStream_t st);
+
+}  // namespace fmtp

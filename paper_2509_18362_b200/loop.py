@@ -16,7 +16,8 @@ from . import binding as Bd
 
 class Target:
     """Device copies of a target model's weights and per-layer paged caches (dicts of torch tensors as
-    produced by binding.to_device), stepped through fastmtp_target_step.
+    produced by binding.to_device), stepped through fastmtp_target_step, or through fastmtp_target_step_kv8 where
+    the caches are 8-bit ones (dicts that hold k_scales and v_scales too).
 
     All layers hold the same sequence lengths, so they share layer 0's seq_lens tensor: advancing the
     sequence is one device-side add, whose amount may itself be a device tensor (no host round trip)."""
@@ -29,7 +30,9 @@ class Target:
         self.seq_lens = dev_kvs[0]["seq_lens"]
         for k in dev_kvs[1:]:
             k["seq_lens"] = self.seq_lens
-        self._kvs = [Bd.kv(k) for k in dev_kvs]          # the structs hold addresses only: built once
+        kv8 = "k_scales" in dev_kvs[0]
+        self._kvs = [Bd.kv8(k) if kv8 else Bd.kv(k) for k in dev_kvs]          # the structs hold addresses only: built once
+        self._call = ctx.fastmtp_target_step_kv8 if kv8 else ctx.fastmtp_target_step
         self.status = torch.zeros(1, dtype=torch.int32, device="cuda")
         self.calls = 0
 
@@ -46,7 +49,7 @@ class Target:
         out_h = torch.empty((B, M, s.d), dtype=torch.bfloat16, device="cuda")
         out_l = torch.empty((B, M, s.vocab), dtype=torch.bfloat16, device="cuda") if want_logits else None
         out_a = torch.full((B, M), -1, dtype=torch.int32, device="cuda")
-        self.ctx.fastmtp_target_step(self.w, t, self._kvs, B, M, out_h, out_l, out_a, self.status)
+        self._call(self.w, t, self._kvs, B, M, out_h, out_l, out_a, self.status)
         self.calls += 1
         return out_h, out_l, out_a
 
