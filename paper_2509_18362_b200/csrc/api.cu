@@ -774,7 +774,9 @@ int fastmtp_kv8_attention(fmtp_ctx *c, const fmtp_bf16 *q, long long ldq, const 
     const int row = c->shape.n_q_heads * c->shape.head_dim;
     if (ldq < row || ldq % 8) return FMTP_EINVAL;
     if (!kv8_fits(c, *kv) || M > kBatchRows || (long long)B * M > c->shape.max_rows) return FMTP_ESHAPE;
-    const int Gs = kBatchRows / M;
+    // as many sequences per launch as the partial results have room for, 64 at most
+    const size_t fit = c->bws.part_rows / ((size_t)kv8_attention_slots(kv8_shape(c), M) * M);
+    const int Gs = fit < (size_t)kBatchRows ? (int)fit : kBatchRows;
     for (int b0 = 0; b0 < B; b0 += Gs) {
         Kv8AttnCall a;
         std::memset(&a, 0, sizeof(a));
@@ -783,7 +785,7 @@ int fastmtp_kv8_attention(fmtp_ctx *c, const fmtp_bf16 *q, long long ldq, const 
         a.q = q + (long long)b0 * M * ldq; a.ldq = ldq;
         a.B = B - b0 < Gs ? B - b0 : Gs; a.M = M;
         a.n_new = n_new ? n_new + b0 : nullptr;
-        a.part = c->bws.att_part; a.max_chunks = c->bws.max_chunks;
+        a.part = c->bws.att_part;
         a.out = out + (size_t)b0 * M * row;
         a.status = dev_status ? dev_status : c->s.status;
         a.n_sm = c->n_sm;

@@ -1202,7 +1202,10 @@ size_t batched_layout(BatchedWs &ws, unsigned char *base, const BatchedShape &sh
     ws.x = reinterpret_cast<float *>(take((size_t)rows * sh.d * 4));
     ws.hout = reinterpret_cast<float *>(take((size_t)rows * sh.d * 4));
     ws.q = reinterpret_cast<bf16_t *>(take((size_t)rows * 2 * qdim * 2));
-    ws.att_part = reinterpret_cast<float *>(take((size_t)rows * sh.Hq * ws.max_chunks * (sh.dh + 2) * 4));
+    // (attention over 8-bit caches cuts short contexts into more chunks)
+    const int slots8 = kv8_attention_slots(Kv8Shape{sh.Hq, sh.Hkv, sh.dh, sh.page, sh.max_ctx}, 1);
+    ws.part_rows = (size_t)rows * (ws.max_chunks > slots8 ? ws.max_chunks : slots8);
+    ws.att_part = reinterpret_cast<float *>(take(ws.part_rows * sh.Hq * (sh.dh + 2) * 4));
     ws.qkv = reinterpret_cast<bf16_t *>(take((size_t)rows * (qdim + 2 * kvdim) * 2));
     ws.keys_bytes = (size_t)(sh.max_K > 1 ? sh.max_K : 1) * kBatchRows * 8 + 256;
     ws.keys = reinterpret_cast<unsigned long long *>(take(ws.keys_bytes));
@@ -1410,7 +1413,7 @@ int batched_target(const BatchedTargetCall &c, cudaStream_t st, long long *launc
             if ((rc = kv8_append(s8, ws.qkv + qdim, ws.qkv + qdim + kvdim, ld, c.kv8s[l], c.B, c.M, nullptr, ws.status, st, launches))) return rc;
             Kv8AttnCall a{};
             a.sh = s8; a.kv = c.kv8s[l]; a.q = ws.qkv; a.ldq = ld; a.B = c.B; a.M = c.M;
-            a.part = ws.att_part; a.max_chunks = ws.max_chunks; a.xop = ws.xop0; a.ld_xop = ws.ld0; a.status = ws.status; a.n_sm = c.n_sm;
+            a.part = ws.att_part; a.xop = ws.xop0; a.ld_xop = ws.ld0; a.status = ws.status; a.n_sm = c.n_sm;
             if ((rc = kv8_attention(a, st, launches))) return rc;
         } else if ((rc = attention(sh, ws, kv, geo, R, c.n_sm, c.wait_limit_ns, 0, c.cache, st, launches))) return rc;
         g = GemmArgs{};

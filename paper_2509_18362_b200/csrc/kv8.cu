@@ -227,13 +227,13 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv8_read_kernel(const Read8Ar
 }
 
 // ---- attention. The (row, query head) pairs that share a KV head of a sequence are dealt to tiles of eight; a work item is one chunk of
-// a sequence's context for one KV head and a set of RW * WR tiles. A CTA of four warps walks a contiguous range of items: WR
-// warps take RW tiles each, and the context's 32-token blocks go round the WT = 4 / WR groups of such warps.
+// a sequence's context for one KV head and a set of RW * WR tiles. WR warps, RW tiles each, are a worker; a CTA of four warps holds
+// 4 / WR of them, which have nothing to do with each other: each walks a contiguous range of items with a ring of its own.
 //
-// Both products run on mma.sync.m16n8k32 with e4m3 operands (twice the rate of the 16-bit forms at twice the depth): K and V enter
+// Both products run on mma.sync.m16n8k32 with e4m3 operands (3.7 times the rate of the 16-bit form): K and V enter
 // as they lie in the cache, nothing is converted. The exact counterpart of an e4m3 code needs more than e4m3's four bits, so
 // the A operand carries a tile's eight pairs twice: rows 0-7 the high parts, rows 8-15 what is left, scaled up. Two parts hold a
-// bf16 query exactly (eight bits; the second one reaches 2^-23 of the head's largest element) and a probability to 2^-9 of
+// bf16 query exactly (eight bits; the second one reaches 2^-23 of the head's largest element) and a probability to 2^-8 of
 // itself or 2^-23 of the chunk's largest. The accumulator's lanes are the A operand's in both products, so probabilities
 // never leave their registers: a lane holds pair lane/4 and tokens 2q, 2q+1 (q = lane % 4) of each eight, and the contraction over
 // tokens takes them in that order: V's transposed 16-bit ldmatrix gives dims 2u, 2u+1 of two tokens in a word, and two byte
@@ -243,7 +243,7 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv8_read_kernel(const Read8Ar
 // A stage of the ring is 32 tokens of K and V with their scales, copied by the warps that read them (16-byte cp.async, any page
 // size: a lane looks up where one token lies, one stage ahead).
 struct Attn8Args {
-    int Hq, Hkv, gq, page, shift, max_ctx, max_chunks, B, M;
+    int Hq, Hkv, gq, page, shift, max_ctx, slots, B, M;       // slots: chunks of a context that `part` has room for
     const bf16_t *q;
     long long ldq;
     const int32_t *n_new;
@@ -256,29 +256,34 @@ struct Attn8Args {
 
 constexpr int kA8Warps = 4, kA8Threads = kA8Warps * 32;
 constexpr int kA8Blk = 32;                           // tokens of a stage
-constexpr float kP8 = 256.f, kPlo8 = 32.f, kQlo8 = 16.f;      // scales of a probability, of its second part, of a query's second part
+constexpr int kA8Chunk = 64;                         // tokens of the shortest chunk
+constexpr float kP8Log2 = 8.f;                       // a probability's scale is 2^8,
+constexpr float kPlo8 = 32.f, kQlo8 = 16.f;          // a second part's (of a probability, of a query) that much more
 
+// Most chunks that a context is cut into, by a sequence's pairs: a partial result costs dh + 2 fp32 values for each pair.
+__host__ __device__ __forceinline__ int cap8(int pairs) { return pairs <= 8 ? 32 : pairs <= 32 ? 16 : 8; }
 // Tokens of a chunk: a function of the sequence's committed length and of the call's rows per sequence, never of the batch.
 __host__ __device__ __forceinline__ int chunk8(int n_ctx, int pairs) {
-    int c = pairs > 32 ? 1024 : pairs > 8 ? 512 : 256;
-    while ((n_ctx + c - 1) / c > 64) c *= 2;
+    int c = kA8Chunk;
+    while ((n_ctx + c - 1) / c > cap8(pairs)) c *= 2;
     return c;
 }
 
 template <int DH, int WR>
 struct Attn8Smem {
-    static constexpr int WT = kA8Warps / WR;
-    static constexpr int S = WT == 4 ? 3 : WT == 2 ? 5 : 8;                  // stages
+    static constexpr int WT = kA8Warps / WR;                                 // workers of a CTA
+    static constexpr int S = WT == 4 ? 3 : WT == 2 ? 6 : 8;                  // stages
+    static constexpr int CTAS = DH == 128 ? 2 : 3;                           // resident per SM
     static constexpr int KV = kA8Blk * DH;                                   // bytes of a stage's K (or V) codes
     static constexpr int STAGE = 2 * KV + 2 * kA8Blk * 4;
-    static constexpr int O_ML = WT * S * STAGE;                              // [4 warps][8 pairs] (max, sum)
-    static constexpr int O_LAST = O_ML + kA8Warps * 8 * 8;                   // [4 warps] the stage that a warp read last
-    static constexpr int O_TAB = O_LAST + kA8Warps * 4;
-    static constexpr int TOTAL = O_TAB + (4 * kBatchRows + 1) * 4;
+    static constexpr int O_TAB = WT * S * STAGE;
+    static constexpr int TOTAL = O_TAB + (5 * kBatchRows + 1) * 4;
 };
 
+// Volatile: the compiler may move an asm statement without side effects into the branch that uses its result, and an MMA that not all
+// of the warp's lanes execute is an illegal instruction.
 __device__ __forceinline__ void mma_e4m3(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
@@ -304,6 +309,8 @@ __device__ __forceinline__ void cp_async4(uint32_t dst, const void *src, uint32_
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
 }
 // Two values as the two e4m3 parts: high parts in the low half of the result, what is left of them (times `up`) in the upper half.
+// (Conversions from fp32 only: with the fp16 form of the conversion, which saves four instructions here, the assembler of CUDA 12.9
+// made code that gave wrong second parts in one place and was illegal in another.)
 __device__ __forceinline__ uint32_t split_e4m3(float a, float b, float up) {
     const uint32_t hi = to_e4m3x2(a, b);
     float ha, hb;
@@ -316,12 +323,23 @@ __device__ __forceinline__ uint32_t piece_at(int t, int c) {
     return (uint32_t)(t * DH + ((DH == 128 ? (c ^ (t & 7)) : (c ^ ((t >> 1) & 3))) << 4));
 }
 
-struct Item8 {                                       // one (sequence, KV head, tile set, chunk)
-    int seq, kvh, set, chunk, t0, t1;                // tokens [t0, t1) of the context
+// Meeting of a worker's warps. Not the aligned form of the barrier, which the compiler does not know to need all lanes of a warp.
+template <int WR>
+__device__ __forceinline__ void worker_sync(int wt) {
+    __syncwarp();
+    if constexpr (WR == kA8Warps) __syncthreads();
+    else if constexpr (WR > 1) asm volatile("barrier.sync %0, %1;" ::"r"(1 + wt), "n"(WR * 32) : "memory");
+    __syncwarp();
+}
+
+// A worker's place in the list of items: sequences, their KV heads, tile sets, chunks (the chunks of one context follow each other).
+struct Item8 {
+    int seq, kvh, set, chunk;
+    int t0, t1;                                      // the chunk's tokens [t0, t1): never empty, the sequence's last row sees them all
 };
 
 template <int DH, int RW, int WR>
-__global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
+__global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
     chain_release();
     chain_wait();
     using Lay = Attn8Smem<DH, WR>;
@@ -331,6 +349,7 @@ __global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_co
     int *tpos = prefix + kBatchRows + 1;                                   // position of a sequence's row 0
     int *tval = tpos + kBatchRows;                                         // its rows that count
     int *tchk = tval + kBatchRows;                                         // tokens of its chunks
+    int *tnum = tchk + kBatchRows;                                         // chunks, sets << 16
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wr = warp % WR, wt = warp / WR;
     const int max_tokens = min((int)min((long long)a.kv.max_pages * a.page, (long long)kMaxLen), a.max_ctx);
     const int gq = a.gq;
@@ -346,7 +365,9 @@ __global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_co
                 const int c = chunk8(row_ctx(len, a.M - 1), a.M * gq);
                 tpos[s] = len; tval[s] = nv; tchk[s] = c;
                 if (nv > 0) {
-                    cnt[u] = (row_ctx(len, nv - 1) + c - 1) / c * a.Hkv * ((nv * gq + 8 * TILES - 1) / (8 * TILES));
+                    const int chunks = (row_ctx(len, nv - 1) + c - 1) / c, sets = (nv * gq + 8 * TILES - 1) / (8 * TILES);
+                    tnum[s] = chunks | (sets << 16);
+                    cnt[u] = chunks * a.Hkv * sets;
                     if (len + nv > max_tokens && blockIdx.x == 0) atomicOr(a.status, kDevBadPos);
                 }
             }
@@ -361,45 +382,52 @@ __global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_co
         if (2 * lane + 1 <= a.B) prefix[2 * lane + 1] = incl - cnt[1];
         if (lane == 31 && a.B == 2 * 32) prefix[a.B] = incl;
     }
+    __syncwarp();
     __syncthreads();
-    const int n_items = prefix[a.B];
-    const int i_begin = (int)(((long long)blockIdx.x * n_items) / gridDim.x), i_end = (int)(((long long)(blockIdx.x + 1) * n_items) / gridDim.x);
-    auto load_item = [&](Item8 &it, int item) {
-        int s = it.seq;                              // items come in ascending order: search on from the last one
-        while (prefix[s + 1] <= item) ++s;
-        it.seq = s;
-        const int rem = item - prefix[s], nv = tval[s], c = tchk[s];
-        const int chunks = (row_ctx(tpos[s], nv - 1) + c - 1) / c, sets = (nv * gq + 8 * TILES - 1) / (8 * TILES);
-        it.chunk = rem % chunks;
-        const int t = rem / chunks;
-        it.set = t % sets;
-        it.kvh = t / sets;
+    // workers are numbered across the CTAs first, so that few items lie on as many SMs
+    const int n_items = prefix[a.B], worker = wt * gridDim.x + blockIdx.x, workers = WT * gridDim.x;
+    const int i_begin = (int)(((long long)worker * n_items) / workers), i_end = (int)(((long long)(worker + 1) * n_items) / workers);
+    auto chunk_bounds = [&](Item8 &it) {
+        const int c = tchk[it.seq];
         it.t0 = it.chunk * c;
-        // what the set's last row sees of the chunk (nothing: t1 <= t0)
-        it.t1 = min(it.t0 + c, row_ctx(tpos[s], min(nv - 1, ((it.set + 1) * 8 * TILES - 1) / gq)));
+        it.t1 = min(it.t0 + c, row_ctx(tpos[it.seq], tval[it.seq] - 1));
     };
+    auto first_item = [&](Item8 &it) {
+        int s = 0;
+        while (prefix[s + 1] <= i_begin) ++s;
+        const int rem = i_begin - prefix[s], chunks = tnum[s] & 0xffff, sets = tnum[s] >> 16, t = rem / chunks;
+        it.seq = s;
+        it.chunk = rem - t * chunks;
+        it.kvh = t / sets;
+        it.set = t - it.kvh * sets;
+        chunk_bounds(it);
+    };
+    auto next_item = [&](Item8 &it) {
+        if (++it.chunk == (tnum[it.seq] & 0xffff)) {
+            it.chunk = 0;
+            if (++it.set == tnum[it.seq] >> 16) {
+                it.set = 0;
+                if (++it.kvh == a.Hkv) {
+                    it.kvh = 0;
+                    do ++it.seq; while (prefix[it.seq + 1] == prefix[it.seq]);       // (there is another item)
+                }
+            }
+        }
+        chunk_bounds(it);
+    };
+    if (i_begin >= i_end) return;                    // (no thread waits for another worker's from here on)
 
-    // ---- copying: the next stage to ask for is block `ctok` of item `citem`; a lane holds where token `lane` of it lies
+    // ---- copying: the next stage to ask for is the block of item `ci` at `ctok`; a lane holds where token `lane` of it lies
     const uint64_t policy = l2_evict_first();
     unsigned char *ring = smem + (size_t)wt * S * Lay::STAGE;
     Item8 ci;
-    ci.seq = 0;
-    int citem = i_begin, ctok = 0, cpage = 0, cin = 0;
-    bool cmore = citem < i_end;
+    int citem = i_begin, ctok = 0, cpage = 0, cin = 0, cslot = 0;
+    bool cmore = true;
     auto look_up = [&]() {
         const int pos = min(ctok + lane, ci.t1 - 1), blk = page_of(pos, a.page, a.shift);
         cin = pos - blk * a.page;
         cpage = a.kv.block_table[(size_t)ci.seq * a.kv.max_pages + blk];
     };
-    auto seek = [&]() {                              // from ctok on, the first block with tokens
-        while (cmore && ctok >= ci.t1) {
-            if (++citem >= i_end) { cmore = false; break; }
-            load_item(ci, citem);
-            ctok = ci.t0 + wt * kA8Blk;
-        }
-        if (cmore) look_up();
-    };
-    int cslot = 0;
     auto copy_stage = [&]() {
         if (cmore) {
             if ((unsigned)cpage >= (unsigned)a.kv.num_pages) { atomicOr(a.status, kDevBadPage); cpage = 0; }
@@ -409,8 +437,8 @@ __global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_co
             constexpr int LPR = DH / 16, RPI = 32 / LPR;
             const int piece = lane % LPR, sub = lane / LPR;
 #pragma unroll
-            for (int u = wr; u < kA8Blk / RPI; u += WR) {
-                const int t = u * RPI + sub;
+            for (int u = 0; u < kA8Blk / RPI / WR; ++u) {
+                const int t = (u * WR + wr) * RPI + sub;
                 const size_t off = (size_t)__shfl_sync(0xffffffffu, row, t) * DH + piece * 16;
                 const uint32_t d = sb + piece_at<DH>(t, piece), n = ctok + t < ci.t1 ? 16u : 0u;      // zeros beyond what is seen
                 cp_async16_off_hint<0>(d, a.kv.k_pages + off, n, policy);
@@ -422,17 +450,23 @@ __global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_co
                 cp_async4(sb + 2 * Lay::KV + kA8Blk * 4 + lane * 4, a.kv.v_scales + slot, n);
             }
             if (++cslot == S) cslot = 0;
-            ctok += WT * kA8Blk;
-            seek();
+            ctok += kA8Blk;
+            if (ctok >= ci.t1) {
+                cmore = ++citem < i_end;
+                if (cmore) {
+                    next_item(ci);
+                    ctok = ci.t0;
+                }
+            }
+            if (cmore) look_up();
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    if (cmore) {
-        load_item(ci, citem);
-        ctok = ci.t0 + wt * kA8Blk;
-        seek();
-    }
-#pragma unroll
+    first_item(ci);
+    Item8 it = ci;
+    ctok = ci.t0;
+    look_up();
+#pragma unroll 1
     for (int s = 0; s < S - 1; ++s) copy_stage();
 
     // ---- computing
@@ -441,26 +475,24 @@ __global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_co
     // ldmatrix rows: K: tokens 0-7 of two pieces, then tokens 8-15 of them; V: four groups of eight tokens of one piece
     const int ktok = (lane & 7) + ((lane >> 4) << 3), kpc = (lane >> 3) & 1;
     uint32_t qa[RW][KS][4];
-    float fs[RW];                                    // score of a query's code times a key's code -> log2 units, without the K scale
+    float fs[RW];                                    // a query code times a key code times the K scale -> log2 units
     int pn[RW];                                      // positions that the lane's pair sees (any, where there is no such pair)
     int prow[RW];                                    // its row; the sequence's number of rows: no such pair
-    int qkey_seq = -1, qkey = -1, slot = 0;
-    Item8 it;
-    it.seq = 0;
+    float *pout[RW];                                 // where its partial results go
+    bool fresh = true;
+    int slot = 0, nv = 0;
     for (int item = i_begin; item < i_end; ++item) {
-        load_item(it, item);
-        const int key = it.kvh * 4096 + it.set;      // (at most 64 * 8 / 8 sets)
-        const int nv = tval[it.seq];
-        if (it.seq != qkey_seq || key != qkey) {     // the queries stay in registers while the CTA's items are chunks of one context
-            qkey_seq = it.seq;
-            qkey = key;
+        if (fresh) {                                 // the queries stay in registers while the items are chunks of one context
+            nv = tval[it.seq];
 #pragma unroll
             for (int r = 0; r < RW; ++r) {
                 const int pair = (it.set * TILES + wr * RW + r) * 8 + hrow, m = pair / gq, h = pair - m * gq;
                 const bool there = pair < nv * gq;
                 prow[r] = there ? m : nv;
                 pn[r] = there ? row_ctx(tpos[it.seq], m) : kMaxLen;
-                const bf16_t *qp = a.q + ((long long)it.seq * a.M + (there ? m : 0)) * a.ldq + (long long)(it.kvh * gq + (there ? h : 0)) * DH;
+                const int row = it.seq * a.M + (there ? m : 0), head = it.kvh * gq + (there ? h : 0);
+                pout[r] = a.part + (((size_t)row * a.Hq + head) * a.slots) * (DH + 2) + kq * 2;
+                const bf16_t *qp = a.q + (long long)row * a.ldq + (long long)head * DH;
                 uint2 x[2 * KS];
                 uint32_t am = 0;
 #pragma unroll
@@ -484,7 +516,7 @@ __global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_co
                 }
             }
         }
-        float m_run[RW], l_run[RW], o[RW][2 * ND][4];
+        float m_run[RW], l_run[RW], o[RW][2 * ND][4];        // m: of scores not yet times fs
         float sv_run = 0.f;                          // largest V scale so far
 #pragma unroll
         for (int r = 0; r < RW; ++r) {
@@ -493,13 +525,12 @@ __global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_co
 #pragma unroll
             for (int i = 0; i < 2 * ND; ++i) o[r][i][0] = o[r][i][1] = o[r][i][2] = o[r][i][3] = 0.f;
         }
-        int last_slot = slot;
-        for (int tb = it.t0 + wt * kA8Blk; tb < it.t1; tb += WT * kA8Blk) {
+#pragma unroll 1
+        for (int tb = it.t0; tb < it.t1; tb += kA8Blk) {
             asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
-            if (WR > 1) bar_sync(1 + wt, WR * 32); else __syncwarp();
+            worker_sync<WR>(wt);
             copy_stage();                            // into the stage that was read last
             const uint32_t sb = smem_u32(ring + (size_t)slot * Lay::STAGE);
-            last_slot = slot;
             if (++slot == S) slot = 0;
             // ---- scores
             float sc[RW][8];
@@ -525,8 +556,8 @@ __global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_co
                     const float2 sk = lds64f(sb + 2 * Lay::KV + (g * 16 + nt * 8 + kq) * 4);
 #pragma unroll
                     for (int r = 0; r < RW; ++r) {
-                        sc[r][g * 4 + nt * 2] = (c[r][nt][0] + c[r][nt][2] * (1.f / kQlo8)) * (fs[r] * sk.x);
-                        sc[r][g * 4 + nt * 2 + 1] = (c[r][nt][1] + c[r][nt][3] * (1.f / kQlo8)) * (fs[r] * sk.y);
+                        sc[r][g * 4 + nt * 2] = fmaf(c[r][nt][2], 1.f / kQlo8, c[r][nt][0]) * sk.x;
+                        sc[r][g * 4 + nt * 2 + 1] = fmaf(c[r][nt][3], 1.f / kQlo8, c[r][nt][1]) * sk.y;
                     }
                 }
             }
@@ -541,10 +572,10 @@ __global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_co
             }
             sv_new = fmaxf(sv_new, __shfl_xor_sync(0xffffffffu, sv_new, 1));
             sv_new = fmaxf(sv_new, __shfl_xor_sync(0xffffffffu, sv_new, 2));
-            const float sv_inv = sv_new > 0.f ? 1.0f / sv_new : 0.f, sv_corr = sv_new == sv_run ? 1.0f : sv_run * sv_inv;
+            const float sv_inv = sv_new > 0.f ? __fdividef(1.0f, sv_new) : 0.f, sv_corr = sv_new == sv_run ? 1.0f : sv_run * sv_inv;
             sv_run = sv_new;
 #pragma unroll
-            for (int i = 0; i < 8; ++i) sv[i] *= sv_inv * kP8;
+            for (int i = 0; i < 8; ++i) sv[i] *= sv_inv;
             // ---- probabilities
             uint32_t pa[RW][4];
             bool edge = false;
@@ -562,14 +593,16 @@ __global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_co
                 mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
                 const float m_new = fmaxf(m_run[r], mx);
                 const float m_use = m_new == -INFINITY ? 0.f : m_new;            // nothing seen yet: every probability is 2^-inf
-                const float corr = exp2_approx(m_run[r] - m_use);
+                const float corr = exp2_approx((m_run[r] - m_use) * fs[r]);
+                const bool grown = m_run[r] > -INFINITY && corr * sv_corr != 1.0f;
                 m_run[r] = m_new;
+                const float mo = kP8Log2 - m_use * fs[r];
                 float p[8];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] = exp2_approx(sc[r][i] - m_use);
+                for (int i = 0; i < 8; ++i) p[i] = exp2_approx(fmaf(sc[r][i], fs[r], mo));
                 l_run[r] = l_run[r] * corr + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
-                const float oc = corr * sv_corr;
-                if (__any_sync(0xffffffffu, oc != 1.0f)) {
+                if (__any_sync(0xffffffffu, grown)) {
+                    const float oc = corr * sv_corr;
 #pragma unroll
                     for (int i = 0; i < 2 * ND; ++i) { o[r][i][0] *= oc; o[r][i][1] *= oc; o[r][i][2] *= oc; o[r][i][3] *= oc; }
                 }
@@ -581,125 +614,70 @@ __global__ void __launch_bounds__(kA8Threads, 2) kv8_attn_kernel(const __grid_co
                     pa[r][2 * g + 1] = __byte_perm(p0, p1, 0x7632);
                 }
             }
-            // ---- weighted values
-            if (!edge) {
+            // ---- weighted values. In a block that some row does not see whole, what it does not see is a later row's value and need not
+            // be a number: there a value that is no number counts as 0 in the products, and is put in afterwards where it is seen
+            uint32_t bad = 0;
 #pragma unroll
-                for (int c = 0; c < ND; ++c) {
-                    uint32_t v[4];
-                    ldsm4_trans(sb + Lay::KV + piece_at<DH>(lane, c), v);
-                    const uint32_t e0 = __byte_perm(v[0], v[1], 0x6420), e1 = __byte_perm(v[2], v[3], 0x6420);       // dims 16c + 2u
-                    const uint32_t d0 = __byte_perm(v[0], v[1], 0x7531), d1 = __byte_perm(v[2], v[3], 0x7531);       // dims 16c + 2u + 1
+            for (int c = 0; c < ND; ++c) {
+                uint32_t v[4];
+                ldsm4_trans(sb + Lay::KV + piece_at<DH>(lane, c), v);
+                if (edge) {
 #pragma unroll
-                    for (int r = 0; r < RW; ++r) {
-                        mma_e4m3(o[r][2 * c], pa[r][0], pa[r][1], pa[r][2], pa[r][3], e0, e1);
-                        mma_e4m3(o[r][2 * c + 1], pa[r][0], pa[r][1], pa[r][2], pa[r][3], d0, d1);
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t nan = __vcmpeq4(v[i] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+                        v[i] &= ~nan;
+                        bad |= nan;
                     }
                 }
-            } else {
-                // Rows of the tiles see different parts of the block. What a row does not see is a later row's value, which need not be
-                // a number, so neither may a probability of 0 meet it nor another row's sum take part in its products: one pass per
-                // row, with the values that it does not see cleared, whose products only its own pairs add.
+                const uint32_t e0 = __byte_perm(v[0], v[1], 0x6420), e1 = __byte_perm(v[2], v[3], 0x6420);       // dims 16c + 2u
+                const uint32_t d0 = __byte_perm(v[0], v[1], 0x7531), d1 = __byte_perm(v[2], v[3], 0x7531);       // dims 16c + 2u + 1
 #pragma unroll
                 for (int r = 0; r < RW; ++r) {
-                    const int m0 = __shfl_sync(0xffffffffu, prow[r], 0), m1 = min(__shfl_sync(0xffffffffu, prow[r], 28), nv - 1);
+                    mma_e4m3(o[r][2 * c], pa[r][0], pa[r][1], pa[r][2], pa[r][3], e0, e1);
+                    mma_e4m3(o[r][2 * c + 1], pa[r][0], pa[r][1], pa[r][2], pa[r][3], d0, d1);
+                }
+            }
+            if (edge && __any_sync(0xffffffffu, bad != 0u)) {
+#pragma unroll
+                for (int c = 0; c < ND; ++c)
 #pragma unroll 1
-                    for (int m = m0; m <= m1; ++m) {
-                        const bool mine = prow[r] == m;
-                        const int left = row_ctx(tpos[it.seq], m) - tb;
-                        if (left <= 0) continue;
-                        uint32_t keep[2];
+                    for (int t = 0; t < kA8Blk; ++t) {       // dims 16c + 2 kq + 0..3 of a token: those of o[..][2c][0], [2c + 1][0], [2c][1], [2c + 1][1]
+                        uint32_t w;
+                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(sb + Lay::KV + piece_at<DH>(t, c) + (uint32_t)(lane & 3) * 4) : "memory");
+                        const uint32_t nan = __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu);
 #pragma unroll
-                        for (int g = 0; g < 2; ++g) {
-                            const int t = g * 16 + kq;
-                            keep[g] = (t < left ? 0xffu : 0u) | (t + 1 < left ? 0xff00u : 0u) | (t + 8 < left ? 0xff0000u : 0u) | (t + 9 < left ? 0xff000000u : 0u);
-                        }
-#pragma unroll
-                        for (int c = 0; c < ND; ++c) {
-                            uint32_t v[4];
-                            ldsm4_trans(sb + Lay::KV + piece_at<DH>(lane, c), v);
-                            float e[4] = {0.f, 0.f, 0.f, 0.f}, d[4] = {0.f, 0.f, 0.f, 0.f};
-                            mma_e4m3(e, pa[r][0], pa[r][1], pa[r][2], pa[r][3], __byte_perm(v[0], v[1], 0x6420) & keep[0], __byte_perm(v[2], v[3], 0x6420) & keep[1]);
-                            mma_e4m3(d, pa[r][0], pa[r][1], pa[r][2], pa[r][3], __byte_perm(v[0], v[1], 0x7531) & keep[0], __byte_perm(v[2], v[3], 0x7531) & keep[1]);
-                            if (mine) {
-#pragma unroll
-                                for (int i = 0; i < 4; ++i) { o[r][2 * c][i] += e[i]; o[r][2 * c + 1][i] += d[i]; }
-                            }
+                        for (int r = 0; r < RW; ++r) {
+                            const uint32_t hit = t < pn[r] - tb ? nan : 0u;
+                            o[r][2 * c][0] += (hit & 0xffu) ? NAN : 0.f;
+                            o[r][2 * c + 1][0] += (hit & 0xff00u) ? NAN : 0.f;
+                            o[r][2 * c][1] += (hit & 0xff0000u) ? NAN : 0.f;
+                            o[r][2 * c + 1][1] += (hit & 0xff000000u) ? NAN : 0.f;
                         }
                     }
-                }
             }
         }
-        // ---- the chunk's partial result: o relative to the maximum, sum and maximum
-        const float of = sv_run * (1.f / kP8);
+        // ---- the chunk's partial result: o and the sum relative to the maximum, the maximum (log2 units)
 #pragma unroll
         for (int r = 0; r < RW; ++r) {
-            l_run[r] += __shfl_xor_sync(0xffffffffu, l_run[r], 1);
-            l_run[r] += __shfl_xor_sync(0xffffffffu, l_run[r], 2);
+            float l = l_run[r];
+            l += __shfl_xor_sync(0xffffffffu, l, 1);
+            l += __shfl_xor_sync(0xffffffffu, l, 2);
+            if (prow[r] < nv && pn[r] > it.t0) {     // (such a pair, and it sees something of the chunk)
+                float *out = pout[r] + (size_t)it.chunk * (DH + 2);
+#pragma unroll
+                for (int c = 0; c < ND; ++c) {       // dims 16c + 2 kq + 0..3
+                    const float *x = o[r][2 * c], *y = o[r][2 * c + 1];
+                    *reinterpret_cast<float2 *>(out + c * 16) = make_float2(fmaf(x[2], 1.f / kPlo8, x[0]) * sv_run, fmaf(y[2], 1.f / kPlo8, y[0]) * sv_run);
+                    *reinterpret_cast<float2 *>(out + c * 16 + 2) = make_float2(fmaf(x[3], 1.f / kPlo8, x[1]) * sv_run, fmaf(y[3], 1.f / kPlo8, y[1]) * sv_run);
+                }
+                if ((lane & 3) == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(m_run[r] * fs[r], l);
+            }
         }
-        auto value = [&](int r, int c) -> float4 {   // dims 16c + 2 kq + 0..3 of the lane's pair
-            return make_float4((o[r][2 * c][0] + o[r][2 * c][2] * (1.f / kPlo8)) * of, (o[r][2 * c + 1][0] + o[r][2 * c + 1][2] * (1.f / kPlo8)) * of,
-                               (o[r][2 * c][1] + o[r][2 * c][3] * (1.f / kPlo8)) * of, (o[r][2 * c + 1][1] + o[r][2 * c + 1][3] * (1.f / kPlo8)) * of);
-        };
-        auto part_of = [&](int pair) -> float * {    // where a pair's partial goes
-            const int m = pair / gq, h = pair - m * gq;
-            return a.part + ((((size_t)it.seq * a.M + m) * a.Hq + (size_t)it.kvh * gq + h) * a.max_chunks + it.chunk) * (DH + 2);
-        };
-        if constexpr (WT == 1) {
-#pragma unroll
-            for (int r = 0; r < RW; ++r) {
-                if (prow[r] == nv || pn[r] <= it.t0) continue;       // no such pair, or it sees nothing of the chunk
-                float *out = part_of((it.set * TILES + wr * RW + r) * 8 + hrow);
-#pragma unroll
-                for (int c = 0; c < ND; ++c) {
-                    const float4 v = value(r, c);
-                    *reinterpret_cast<float2 *>(out + c * 16 + kq * 2) = make_float2(v.x, v.y);
-                    *reinterpret_cast<float2 *>(out + c * 16 + kq * 2 + 2) = make_float2(v.z, v.w);
-                }
-                if ((lane & 3) == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(m_run[r], l_run[r]);
-            }
-        } else {
-            // The WT groups' results are joined in shared memory: each warp leaves its own in the stage that it read last (free until
-            // its next copy), then all threads add them up in the groups' order.
-            static_assert(RW == 1 && 8 * (DH + 4) * 4 * WR <= Lay::STAGE, "partial results fit the stage read last");
-            float2 *ml = reinterpret_cast<float2 *>(smem + Lay::O_ML);
-            int *last = reinterpret_cast<int *>(smem + Lay::O_LAST);
-            const int blocks = (it.t1 - it.t0 + kA8Blk - 1) / kA8Blk;        // groups beyond have none of them
-            if (wt < blocks) {
-                if (WR > 1) bar_sync(1 + wt, WR * 32);                       // all readers of the stage are done
-                float *mine = reinterpret_cast<float *>(ring + (size_t)last_slot * Lay::STAGE) + (wr * 8 + hrow) * (DH + 4);
-#pragma unroll
-                for (int c = 0; c < ND; ++c) *reinterpret_cast<float4 *>(mine + c * 16 + kq * 2) = value(0, c);
-                if ((lane & 3) == 0) ml[warp * 8 + hrow] = make_float2(m_run[0], l_run[0]);
-                if (lane == 0) last[warp] = last_slot;
-            }
-            __syncthreads();
-            for (int i = threadIdx.x; i < WR * 8 * (DH / 4); i += kA8Threads) {              // four dims of a pair
-                const int ps = i / (DH / 4), d = (i - ps * (DH / 4)) * 4, w0 = ps >> 3, s = ps & 7;
-                const int pair = it.set * TILES * 8 + ps;
-                if (pair >= nv * gq || row_ctx(tpos[it.seq], pair / gq) <= it.t0) continue;
-                float mm = -INFINITY;
-#pragma unroll
-                for (int g = 0; g < WT; ++g)
-                    if (g < blocks) mm = fmaxf(mm, ml[(g * WR + w0) * 8 + s].x);
-                const float mu = mm == -INFINITY ? 0.f : mm;
-                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                float l = 0.f;
-#pragma unroll
-                for (int g = 0; g < WT; ++g) {
-                    if (g >= blocks) continue;
-                    const int w = g * WR + w0;
-                    const float2 x = ml[w * 8 + s];
-                    const float f = exp2_approx(x.x - mu);
-                    const float4 v = *reinterpret_cast<const float4 *>(smem + (size_t)(g * S + last[w]) * Lay::STAGE + ((size_t)(w0 * 8 + s) * (DH + 4) + d) * 4);
-                    acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
-                    l += x.y * f;
-                }
-                float *out = part_of(pair);
-                *reinterpret_cast<float2 *>(out + d) = make_float2(acc.x, acc.y);
-                *reinterpret_cast<float2 *>(out + d + 2) = make_float2(acc.z, acc.w);
-                if (d == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(mm, l);
-            }
-            __syncthreads();
+        __syncwarp();
+        if (item + 1 < i_end) {
+            const int seq = it.seq, kvh = it.kvh, set = it.set;
+            next_item(it);
+            fresh = it.seq != seq || it.kvh != kvh || it.set != set;
         }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
@@ -719,7 +697,7 @@ __global__ void __launch_bounds__(DH) kv8_merge_kernel(const Attn8Args a) {
     const int n = min(len + m, max_tokens - 1) + 1, c = chunk8(min(len + a.M - 1, max_tokens - 1) + 1, a.M * a.gq);
     const int chunks = (n + c - 1) / c;
     constexpr int stride = DH + 2, G = 16;
-    const float *base = a.part + ((size_t)r * a.Hq + head) * a.max_chunks * stride;
+    const float *base = a.part + ((size_t)r * a.Hq + head) * a.slots * stride;
     float mx = -INFINITY;
     for (int i = lane; i < chunks; i += 32) mx = fmaxf(mx, base[(size_t)i * stride + DH]);
 #pragma unroll
@@ -758,7 +736,7 @@ template <int DH, int RW, int WR>
 int attn8_launch(const Attn8Args &a, int rows, int n_sm, cudaStream_t st) {
     auto kern = kv8_attn_kernel<DH, RW, WR>;
     cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Attn8Smem<DH, WR>::TOTAL);
-    if (e == cudaSuccess) e = launch_chained(kern, dim3(2 * n_sm), dim3(kA8Threads), (size_t)Attn8Smem<DH, WR>::TOTAL, st, a);
+    if (e == cudaSuccess) e = launch_chained(kern, dim3(Attn8Smem<DH, WR>::CTAS * n_sm), dim3(kA8Threads), (size_t)Attn8Smem<DH, WR>::TOTAL, st, a);
     if (e == cudaSuccess) e = launch_chained(kv8_merge_kernel<DH>, dim3(a.Hq, rows), dim3(DH), 0, st, a);
     return (int)e;
 }
@@ -767,9 +745,10 @@ template <int DH>
 int attn8_pick(const Attn8Args &a, int rows, int n_sm, cudaStream_t st) {
     const int pairs = a.M * a.gq;
     if (pairs <= 8) return attn8_launch<DH, 1, 1>(a, rows, n_sm, st);
-    if (pairs <= 16) return attn8_launch<DH, 1, 2>(a, rows, n_sm, st);
-    if (pairs <= 32) return attn8_launch<DH, 1, 4>(a, rows, n_sm, st);
-    return attn8_launch<DH, 2, 4>(a, rows, n_sm, st);
+    if (pairs <= 16) return attn8_launch<DH, 2, 1>(a, rows, n_sm, st);
+    if (pairs <= 32) return attn8_launch<DH, 2, 2>(a, rows, n_sm, st);
+    if constexpr (DH == 64) return attn8_launch<DH, 2, 2>(a, rows, n_sm, st);
+    else return attn8_launch<DH, 2, 4>(a, rows, n_sm, st);
 }
 
 }  // namespace
@@ -799,10 +778,15 @@ int kv8_read(const Kv8Shape &sh, const Kv8Ptrs &kv, int B, int max_n, const int3
     return (int)launch_chained(kern, dim3((unsigned)blocks), dim3(kReadWarps * 32), 0, st, a);
 }
 
+int kv8_attention_slots(const Kv8Shape &sh, int M) {
+    const int cap = cap8(M * (sh.Hq / sh.Hkv)), most = (sh.max_ctx + kA8Chunk - 1) / kA8Chunk;
+    return most < cap ? most : cap;
+}
+
 int kv8_attention(const Kv8AttnCall &c, cudaStream_t st, long long *launches) {
     Attn8Args a{};
     a.Hq = c.sh.Hq; a.Hkv = c.sh.Hkv; a.gq = c.sh.Hq / c.sh.Hkv; a.page = c.sh.page; a.shift = shift_of(c.sh.page); a.max_ctx = c.sh.max_ctx;
-    a.max_chunks = c.max_chunks; a.B = c.B; a.M = c.M; a.q = c.q; a.ldq = c.ldq; a.n_new = c.n_new; a.kv = c.kv; a.part = c.part;
+    a.slots = kv8_attention_slots(c.sh, c.M); a.B = c.B; a.M = c.M; a.q = c.q; a.ldq = c.ldq; a.n_new = c.n_new; a.kv = c.kv; a.part = c.part;
     a.out = c.out; a.xop = c.xop; a.ld_xop = c.ld_xop; a.status = c.status;
     *launches += 2;
     return c.sh.dh == 128 ? attn8_pick<128>(a, c.B * c.M, c.n_sm, st) : attn8_pick<64>(a, c.B * c.M, c.n_sm, st);
