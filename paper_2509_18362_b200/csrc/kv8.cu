@@ -230,18 +230,16 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv8_read_kernel(const Read8Ar
 // a sequence's context for one KV head and a set of RW * WR tiles. WR warps, RW tiles each, are a worker; a CTA of four warps holds
 // 4 / WR of them, which have nothing to do with each other: each walks a contiguous range of items with a ring of its own.
 //
-// Both products run on mma.sync.m16n8k32 with e4m3 operands (3.7 times the rate of the 16-bit form): K and V enter
-// as they lie in the cache, nothing is converted. The exact counterpart of an e4m3 code needs more than e4m3's four bits, so
-// the A operand carries a tile's eight pairs twice: rows 0-7 the high parts, rows 8-15 what is left, scaled up. Two parts hold a
-// bf16 query exactly (eight bits; the second one reaches 2^-23 of the head's largest element) and a probability to 2^-8 of
-// itself or 2^-23 of the chunk's largest. The accumulator's lanes are the A operand's in both products, so probabilities
-// never leave their registers: a lane holds pair lane/4 and tokens 2q, 2q+1 (q = lane % 4) of each eight, and the contraction over
-// tokens takes them in that order: V's transposed 16-bit ldmatrix gives dims 2u, 2u+1 of two tokens in a word, and two byte
-// permutations per two words sort them by dimension.
+// Both products run on mma.sync.m16n8k16 with f16 operands (sm_100a has no mma.sync on e4m3: the assembler emulates it with fifteen
+// instructions each). K and V are the A operand, 16 tokens or 16 dims, so that eight pairs fill the n side: S^T = K Q^T, O^T = V^T
+// P^T. An e4m3 code is exact in f16, a bf16 query (over a power of two, eight bits) as well; a probability is rounded to 2^-12 of
+// itself or 2^-39 of the chunk's largest. A word of K is four dims of a token, and the contraction takes them in the order in which a
+// lane holds them. V's transposed 16-bit ldmatrix gives dims 2u, 2u + 1 of two tokens in a word, which a byte permutation sorts;
+// movmatrix turns a tile of probabilities from the first product's layout into the second one's.
 //
 // Scores are scaled by the token's K scale, probabilities by its V scale over the largest seen so far (O carries both factors).
 // A stage of the ring is 32 tokens of K and V with their scales, copied by the warps that read them (16-byte cp.async, any page
-// size: a lane looks up where one token lies, one stage ahead).
+// size).
 struct Attn8Args {
     int Hq, Hkv, gq, page, shift, max_ctx, slots, B, M;       // slots: chunks of a context that `part` has room for
     const bf16_t *q;
@@ -256,16 +254,22 @@ struct Attn8Args {
 
 constexpr int kA8Warps = 4, kA8Threads = kA8Warps * 32;
 constexpr int kA8Blk = 32;                           // tokens of a stage
-constexpr int kA8Chunk = 64;                         // tokens of the shortest chunk
-constexpr float kP8Log2 = 8.f;                       // a probability's scale is 2^8,
-constexpr float kPlo8 = 32.f, kQlo8 = 16.f;          // a second part's (of a probability, of a query) that much more
+constexpr float kP8Log2 = 14.f;                      // probabilities are held times 2^14: f16 reaches from 2^16 down to 2^-24
+constexpr float kQ8 = 32.f;                          // queries below 448 * 32
 
-// Most chunks that a context is cut into, by a sequence's pairs: a partial result costs dh + 2 fp32 values for each pair.
-__host__ __device__ __forceinline__ int cap8(int pairs) { return pairs <= 8 ? 32 : pairs <= 32 ? 16 : 8; }
-// Tokens of a chunk: a function of the sequence's committed length and of the call's rows per sequence, never of the batch.
+// Tokens of a chunk: a function of the sequence's committed length and of the call's rows per sequence, never of the batch. Short
+// enough for a context to keep many workers busy, long enough for the partial results (dh + 2 fp32 values for each pair and chunk,
+// 512 bytes against 256 bytes of K/V per token at dh = 128) to stay a small part of the traffic: up to `few` chunks until a chunk is
+// `base` long, up to `most` chunks of that and more tokens beyond.
+struct Chunk8 { int first, few, base, most; };
+__host__ __device__ __forceinline__ Chunk8 chunk8_rule(int pairs) {
+    return pairs <= 8 ? Chunk8{64, 32, 256, 128} : pairs <= 32 ? Chunk8{128, 16, 512, 64} : Chunk8{256, 8, 512, 32};
+}
 __host__ __device__ __forceinline__ int chunk8(int n_ctx, int pairs) {
-    int c = kA8Chunk;
-    while ((n_ctx + c - 1) / c > cap8(pairs)) c *= 2;
+    const Chunk8 r = chunk8_rule(pairs);
+    int c = r.first;
+    while (c < r.base && n_ctx > c * r.few) c *= 2;
+    while ((n_ctx + c - 1) / c > r.most) c *= 2;
     return c;
 }
 
@@ -280,13 +284,25 @@ struct Attn8Smem {
     static constexpr int TOTAL = O_TAB + (5 * kBatchRows + 1) * 4;
 };
 
-// Volatile: the compiler may move an asm statement without side effects into the branch that uses its result, and an MMA that not all
-// of the warp's lanes execute is an illegal instruction.
-__device__ __forceinline__ void mma_e4m3(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
-    asm volatile("mma.sync.aligned.m16n8k32.row.col.f32.e4m3.e4m3.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+// (Warp-wide instructions are volatile: the compiler may move an asm statement without side effects into a branch that uses its result,
+// and all lanes have to execute them.)
+__device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
 }
+__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t v) {
+    uint32_t r;
+    asm volatile("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t pack_f16x2(float lo, float hi) {
+    uint32_t r;
+    asm("cvt.rn.f16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+    return r;
+}
+__device__ __forceinline__ uint32_t e4m3lo_f16x2(uint32_t w) { return e4m3x2_f16x2((uint16_t)(w & 0xffffu)); }
+__device__ __forceinline__ uint32_t e4m3hi_f16x2(uint32_t w) { return e4m3x2_f16x2((uint16_t)(w >> 16)); }
 __device__ __forceinline__ void ldsm4(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
@@ -295,9 +311,9 @@ __device__ __forceinline__ void ldsm4_trans(uint32_t addr, uint32_t (&r)[4]) {
     asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
                  : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) : "memory");
 }
-__device__ __forceinline__ float2 lds64f(uint32_t addr) {
-    float2 v;
-    asm volatile("ld.shared.v2.f32 {%0,%1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(addr) : "memory");
+__device__ __forceinline__ float lds32f(uint32_t addr) {
+    float v;
+    asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
     return v;
 }
 __device__ __forceinline__ float exp2_approx(float x) {      // 2^x; results below the normal range are zero, as is 2^-inf
@@ -307,15 +323,6 @@ __device__ __forceinline__ float exp2_approx(float x) {      // 2^x; results bel
 }
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void *src, uint32_t bytes) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-}
-// Two values as the two e4m3 parts: high parts in the low half of the result, what is left of them (times `up`) in the upper half.
-// (Conversions from fp32 only: with the fp16 form of the conversion, which saves four instructions here, the assembler of CUDA 12.9
-// made code that gave wrong second parts in one place and was illegal in another.)
-__device__ __forceinline__ uint32_t split_e4m3(float a, float b, float up) {
-    const uint32_t hi = to_e4m3x2(a, b);
-    float ha, hb;
-    f16x2_f32(e4m3x2_f16x2((uint16_t)hi), ha, hb);
-    return hi | (to_e4m3x2((a - ha) * up, (b - hb) * up) << 16);
 }
 // Byte position of 16-byte piece c of token row t: the eight rows an ldmatrix phase reads lie in different banks.
 template <int DH>
@@ -417,68 +424,79 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
     };
     if (i_begin >= i_end) return;                    // (no thread waits for another worker's from here on)
 
-    // ---- copying: the next stage to ask for is the block of item `ci` at `ctok`; a lane holds where token `lane` of it lies
+    // ---- copying. Block-table entries are read a segment ahead (a read queues behind the copies that are on their way, which takes
+    // longer than a stage): lane i holds the page of the segment's i-th block. A segment is part of one item: stages whose tokens lie in
+    // 32 blocks
     const uint64_t policy = l2_evict_first();
     unsigned char *ring = smem + (size_t)wt * S * Lay::STAGE;
-    Item8 ci;
-    int citem = i_begin, ctok = 0, cpage = 0, cin = 0, cslot = 0;
-    bool cmore = true;
-    auto look_up = [&]() {
-        const int pos = min(ctok + lane, ci.t1 - 1), blk = page_of(pos, a.page, a.shift);
-        cin = pos - blk * a.page;
-        cpage = a.kv.block_table[(size_t)ci.seq * a.kv.max_pages + blk];
+    struct Segment { int tok, end, t1, blk, kvh, page; };     // next stage's first token; behind the last one; end of what is seen; first block
+    Segment cur{}, nxt{};
+    Item8 li{};
+    int litem = i_begin, ltok = 0, cslot = 0;
+    auto load_segment = [&](Segment &g) {
+        if (litem >= i_end) { g.tok = g.end = 0; return; }
+        g.tok = ltok;
+        g.t1 = li.t1;
+        g.kvh = li.kvh;
+        g.blk = page_of(ltok, a.page, a.shift);
+        g.end = ltok + (int)min((((long long)g.blk + 32) * a.page - ltok) & ~(long long)(kA8Blk - 1), (long long)(li.t1 - ltok + kA8Blk - 1) & ~(long long)(kA8Blk - 1));
+        const int blk = min(g.blk + lane, page_of(li.t1 - 1, a.page, a.shift));
+        g.page = a.kv.block_table[(size_t)li.seq * a.kv.max_pages + blk];
+        ltok = g.end;
+        if (ltok >= li.t1 && ++litem < i_end) {
+            next_item(li);
+            ltok = li.t0;
+        }
     };
     auto copy_stage = [&]() {
-        if (cmore) {
-            if ((unsigned)cpage >= (unsigned)a.kv.num_pages) { atomicOr(a.status, kDevBadPage); cpage = 0; }
+        if (cur.tok < cur.end) {
+            const int pos = min(cur.tok + lane, cur.t1 - 1), blk = page_of(pos, a.page, a.shift);      // lane: a token of the stage
+            int page = __shfl_sync(0xffffffffu, cur.page, blk - cur.blk);
+            if ((unsigned)page >= (unsigned)a.kv.num_pages) { atomicOr(a.status, kDevBadPage); page = 0; }
             const uint32_t sb = smem_u32(ring + (size_t)cslot * Lay::STAGE);
-            const uint32_t slot = (uint32_t)cpage * (uint32_t)a.Hkv + (uint32_t)ci.kvh;
-            const uint32_t row = slot * (uint32_t)a.page + (uint32_t)cin;
+            const uint32_t slot = (uint32_t)page * (uint32_t)a.Hkv + (uint32_t)cur.kvh;
+            const uint32_t row = slot * (uint32_t)a.page + (uint32_t)(pos - blk * a.page);
             constexpr int LPR = DH / 16, RPI = 32 / LPR;
             const int piece = lane % LPR, sub = lane / LPR;
 #pragma unroll
             for (int u = 0; u < kA8Blk / RPI / WR; ++u) {
                 const int t = (u * WR + wr) * RPI + sub;
                 const size_t off = (size_t)__shfl_sync(0xffffffffu, row, t) * DH + piece * 16;
-                const uint32_t d = sb + piece_at<DH>(t, piece), n = ctok + t < ci.t1 ? 16u : 0u;      // zeros beyond what is seen
+                const uint32_t d = sb + piece_at<DH>(t, piece), n = cur.tok + t < cur.t1 ? 16u : 0u;      // zeros beyond what is seen
                 cp_async16_off_hint<0>(d, a.kv.k_pages + off, n, policy);
                 cp_async16_off_hint<0>(d + Lay::KV, a.kv.v_pages + off, n, policy);
             }
             if (wr == 0) {
-                const uint32_t n = ctok + lane < ci.t1 ? 4u : 0u;
+                const uint32_t n = cur.tok + lane < cur.t1 ? 4u : 0u;
                 cp_async4(sb + 2 * Lay::KV + lane * 4, a.kv.k_scales + slot, n);
                 cp_async4(sb + 2 * Lay::KV + kA8Blk * 4 + lane * 4, a.kv.v_scales + slot, n);
             }
             if (++cslot == S) cslot = 0;
-            ctok += kA8Blk;
-            if (ctok >= ci.t1) {
-                cmore = ++citem < i_end;
-                if (cmore) {
-                    next_item(ci);
-                    ctok = ci.t0;
-                }
+            cur.tok += kA8Blk;
+            if (cur.tok >= cur.end) {
+                cur = nxt;
+                load_segment(nxt);
             }
-            if (cmore) look_up();
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    first_item(ci);
-    Item8 it = ci;
-    ctok = ci.t0;
-    look_up();
+    first_item(li);
+    Item8 it = li;
+    ltok = li.t0;
+    load_segment(cur);
+    load_segment(nxt);
 #pragma unroll 1
     for (int s = 0; s < S - 1; ++s) copy_stage();
 
     // ---- computing
-    const int hrow = lane >> 2, kq = (lane & 3) * 2;
+    const int g = lane >> 2, kq = (lane & 3) * 2;    // of a tile's pairs, a lane has kq and kq + 1; as a B operand's column, g
     const float sm_scale = (1.0f / sqrtf((float)DH)) * 1.4426950408889634f;
-    // ldmatrix rows: K: tokens 0-7 of two pieces, then tokens 8-15 of them; V: four groups of eight tokens of one piece
-    const int ktok = (lane & 7) + ((lane >> 4) << 3), kpc = (lane >> 3) & 1;
-    uint32_t qa[RW][KS][4];
-    float fs[RW];                                    // a query code times a key code times the K scale -> log2 units
-    int pn[RW];                                      // positions that the lane's pair sees (any, where there is no such pair)
-    int prow[RW];                                    // its row; the sequence's number of rows: no such pair
-    float *pout[RW];                                 // where its partial results go
+    // ldmatrix rows: K: tokens 0-7 and 8-15 of one piece, then of the next; V: four groups of eight tokens of one piece
+    const int ktok = lane & 15, kpc = lane >> 4;
+    uint32_t qb[RW][2 * KS][2];
+    float fs[RW][2];                                 // a query element times a key code times the K scale -> log2 units
+    int pn[RW][2], prow[RW][2];                      // positions that a pair sees, its row (no such pair: any, the sequence's number of rows)
+    size_t pout[RW][2];                              // where its partial results go
     bool fresh = true;
     int slot = 0, nv = 0;
     for (int item = i_begin; item < i_end; ++item) {
@@ -486,12 +504,16 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
             nv = tval[it.seq];
 #pragma unroll
             for (int r = 0; r < RW; ++r) {
-                const int pair = (it.set * TILES + wr * RW + r) * 8 + hrow, m = pair / gq, h = pair - m * gq;
-                const bool there = pair < nv * gq;
-                prow[r] = there ? m : nv;
-                pn[r] = there ? row_ctx(tpos[it.seq], m) : kMaxLen;
-                const int row = it.seq * a.M + (there ? m : 0), head = it.kvh * gq + (there ? h : 0);
-                pout[r] = a.part + (((size_t)row * a.Hq + head) * a.slots) * (DH + 2) + kq * 2;
+                const int pair0 = (it.set * TILES + wr * RW + r) * 8;
+                auto pair_at = [&](int pair, int &m, int &row, int &head) -> bool {
+                    const bool there = pair < nv * gq;
+                    m = there ? pair / gq : 0;
+                    row = it.seq * a.M + m;
+                    head = it.kvh * gq + (there ? pair - m * gq : 0);
+                    return there;
+                };
+                int m, row, head;
+                pair_at(pair0 + g, m, row, head);
                 const bf16_t *qp = a.q + (long long)row * a.ldq + (long long)head * DH;
                 uint2 x[2 * KS];
                 uint32_t am = 0;
@@ -503,27 +525,33 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
                 am = max(am & 0xffffu, am >> 16);
                 am = max(am, __shfl_xor_sync(0xffffffffu, am, 1));
                 am = max(am, __shfl_xor_sync(0xffffffffu, am, 2));
-                const float qs = scale_for(am), inv = 1.0f / qs;
-                fs[r] = qs * sm_scale;
+                const float qs = scale_for(am), inv = kQ8 / qs;
 #pragma unroll
-                for (int j = 0; j < 2 * KS; ++j) {
+                for (int j = 0; j < 2 * KS; ++j) {   // (an infinite query becomes an infinite f16 and its scores NaN or infinite: NaN)
                     float y[4] = {bf16lo_f32(x[j].x), bf16hi_f32(x[j].x), bf16lo_f32(x[j].y), bf16hi_f32(x[j].y)};
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) y[i] = fabsf(y[i]) < INFINITY ? y[i] * inv : __uint_as_float(0x7fffffffu);   // an infinite query: NaN
-                    const uint32_t p0 = split_e4m3(y[0], y[1], kQlo8), p1 = split_e4m3(y[2], y[3], kQlo8);
-                    qa[r][j >> 1][(j & 1) * 2] = __byte_perm(p0, p1, 0x5410);
-                    qa[r][j >> 1][(j & 1) * 2 + 1] = __byte_perm(p0, p1, 0x7632);
+                    for (int i = 0; i < 4; ++i) y[i] = fabsf(y[i]) < INFINITY ? y[i] * inv : __uint_as_float(0x7fffffffu);
+                    qb[r][j][0] = pack_f16x2(y[0], y[1]);
+                    qb[r][j][1] = pack_f16x2(y[2], y[3]);
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    fs[r][e] = __shfl_sync(0xffffffffu, qs, (kq + e) * 4) * (sm_scale / kQ8);
+                    const bool there = pair_at(pair0 + kq + e, m, row, head);
+                    prow[r][e] = there ? m : nv;
+                    pn[r][e] = there ? row_ctx(tpos[it.seq], m) : kMaxLen;
+                    pout[r][e] = ((size_t)row * a.Hq + head) * a.slots * (DH + 2);
                 }
             }
         }
-        float m_run[RW], l_run[RW], o[RW][2 * ND][4];        // m: of scores not yet times fs
+        float m_run[RW][2], l_run[RW][2], o[RW][ND][4];      // m: of scores not yet times fs
         float sv_run = 0.f;                          // largest V scale so far
 #pragma unroll
         for (int r = 0; r < RW; ++r) {
-            m_run[r] = -INFINITY;
-            l_run[r] = 0.f;
+            m_run[r][0] = m_run[r][1] = -INFINITY;
+            l_run[r][0] = l_run[r][1] = 0.f;
 #pragma unroll
-            for (int i = 0; i < 2 * ND; ++i) o[r][i][0] = o[r][i][1] = o[r][i][2] = o[r][i][3] = 0.f;
+            for (int i = 0; i < ND; ++i) o[r][i][0] = o[r][i][1] = o[r][i][2] = o[r][i][3] = 0.f;
         }
 #pragma unroll 1
         for (int tb = it.t0; tb < it.t1; tb += kA8Blk) {
@@ -532,90 +560,91 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
             copy_stage();                            // into the stage that was read last
             const uint32_t sb = smem_u32(ring + (size_t)slot * Lay::STAGE);
             if (++slot == S) slot = 0;
-            // ---- scores
-            float sc[RW][8];
+            // ---- scores: tokens 16 h + g, 16 h + 8 + g of pairs kq, kq + 1
+            float sc[RW][2][4];
 #pragma unroll
-            for (int g = 0; g < 2; ++g) {            // 16 tokens at a time
-                float c[RW][2][4];
+            for (int h = 0; h < 2; ++h) {
 #pragma unroll
-                for (int r = 0; r < RW; ++r)
+                for (int r = 0; r < RW; ++r) sc[r][h][0] = sc[r][h][1] = sc[r][h][2] = sc[r][h][3] = 0.f;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) c[r][0][i] = c[r][1][i] = 0.f;
-#pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {
+                for (int ks = 0; ks < KS; ++ks) {    // 32 dims
                     uint32_t kf[4];
-                    ldsm4(sb + piece_at<DH>(g * 16 + ktok, 2 * ks + kpc), kf);
+                    ldsm4(sb + piece_at<DH>(h * 16 + ktok, 2 * ks + kpc), kf);
 #pragma unroll
-                    for (int r = 0; r < RW; ++r) {
-                        mma_e4m3(c[r][0], qa[r][ks][0], qa[r][ks][1], qa[r][ks][2], qa[r][ks][3], kf[0], kf[1]);
-                        mma_e4m3(c[r][1], qa[r][ks][0], qa[r][ks][1], qa[r][ks][2], qa[r][ks][3], kf[2], kf[3]);
-                    }
-                }
+                    for (int u = 0; u < 2; ++u) {
+                        const uint32_t a0 = e4m3lo_f16x2(kf[2 * u]), a2 = e4m3hi_f16x2(kf[2 * u]), a1 = e4m3lo_f16x2(kf[2 * u + 1]), a3 = e4m3hi_f16x2(kf[2 * u + 1]);
 #pragma unroll
-                for (int nt = 0; nt < 2; ++nt) {
-                    const float2 sk = lds64f(sb + 2 * Lay::KV + (g * 16 + nt * 8 + kq) * 4);
-#pragma unroll
-                    for (int r = 0; r < RW; ++r) {
-                        sc[r][g * 4 + nt * 2] = fmaf(c[r][nt][2], 1.f / kQlo8, c[r][nt][0]) * sk.x;
-                        sc[r][g * 4 + nt * 2 + 1] = fmaf(c[r][nt][3], 1.f / kQlo8, c[r][nt][1]) * sk.y;
+                        for (int r = 0; r < RW; ++r) mma_f16(sc[r][h], a0, a1, a2, a3, qb[r][2 * ks + u][0], qb[r][2 * ks + u][1]);
                     }
                 }
             }
-            // ---- V scales of the lane's tokens over the largest seen so far
-            float sv[8], sv_new = sv_run;
+            // ---- scales of the lane's tokens; V's over the largest seen so far
+            float sv[2][2], sv_new = sv_run;
 #pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                const float2 x = lds64f(sb + 2 * Lay::KV + kA8Blk * 4 + (i * 8 + kq) * 4);
-                sv[2 * i] = x.x;
-                sv[2 * i + 1] = x.y;
-                sv_new = fmaxf(sv_new, fmaxf(x.x, x.y));
-            }
-            sv_new = fmaxf(sv_new, __shfl_xor_sync(0xffffffffu, sv_new, 1));
-            sv_new = fmaxf(sv_new, __shfl_xor_sync(0xffffffffu, sv_new, 2));
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    const uint32_t at = sb + 2 * Lay::KV + (h * 16 + e * 8 + g) * 4;
+                    const float sk = lds32f(at);
+                    sv[h][e] = lds32f(at + kA8Blk * 4);
+                    sv_new = fmaxf(sv_new, sv[h][e]);
+#pragma unroll
+                    for (int r = 0; r < RW; ++r) {
+                        sc[r][h][2 * e] *= sk;
+                        sc[r][h][2 * e + 1] *= sk;
+                    }
+                }
+#pragma unroll
+            for (int x = 4; x < 32; x <<= 1) sv_new = fmaxf(sv_new, __shfl_xor_sync(0xffffffffu, sv_new, x));
             const float sv_inv = sv_new > 0.f ? __fdividef(1.0f, sv_new) : 0.f, sv_corr = sv_new == sv_run ? 1.0f : sv_run * sv_inv;
             sv_run = sv_new;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) sv[i] *= sv_inv;
             // ---- probabilities
-            uint32_t pa[RW][4];
+            uint32_t pb[RW][2][2];
             bool edge = false;
 #pragma unroll
             for (int r = 0; r < RW; ++r) {
-                const int left = pn[r] - tb;         // tokens of the block that the pair sees
-                if (__any_sync(0xffffffffu, left < kA8Blk)) {
+                if (__any_sync(0xffffffffu, min(pn[r][0], pn[r][1]) - tb < kA8Blk)) {
                     edge = true;
 #pragma unroll
-                    for (int i = 0; i < 8; ++i)
-                        if ((i >> 1) * 8 + kq + (i & 1) >= left) sc[r][i] = -INFINITY;
-                }
-                float mx = fmaxf(fmaxf(fmaxf(sc[r][0], sc[r][1]), fmaxf(sc[r][2], sc[r][3])), fmaxf(fmaxf(sc[r][4], sc[r][5]), fmaxf(sc[r][6], sc[r][7])));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 1));
-                mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, 2));
-                const float m_new = fmaxf(m_run[r], mx);
-                const float m_use = m_new == -INFINITY ? 0.f : m_new;            // nothing seen yet: every probability is 2^-inf
-                const float corr = exp2_approx((m_run[r] - m_use) * fs[r]);
-                const bool grown = m_run[r] > -INFINITY && corr * sv_corr != 1.0f;
-                m_run[r] = m_new;
-                const float mo = kP8Log2 - m_use * fs[r];
-                float p[8];
+                    for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int i = 0; i < 8; ++i) p[i] = exp2_approx(fmaf(sc[r][i], fs[r], mo));
-                l_run[r] = l_run[r] * corr + (((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7])));
+                        for (int i = 0; i < 4; ++i)
+                            if (tb + h * 16 + (i >> 1) * 8 + g >= pn[r][i & 1]) sc[r][h][i] = -INFINITY;
+                }
+                float corr[2], mo[2];
+                bool grown = false;
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    float mx = fmaxf(fmaxf(sc[r][0][e], sc[r][0][2 + e]), fmaxf(sc[r][1][e], sc[r][1][2 + e]));
+#pragma unroll
+                    for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
+                    const float m_new = fmaxf(m_run[r][e], mx);
+                    const float m_use = m_new == -INFINITY ? 0.f : m_new;        // nothing seen yet: every probability is 2^-inf
+                    corr[e] = exp2_approx((m_run[r][e] - m_use) * fs[r][e]);
+                    grown |= m_run[r][e] > -INFINITY && corr[e] * sv_corr != 1.0f;
+                    m_run[r][e] = m_new;
+                    mo[e] = kP8Log2 - m_use * fs[r][e];
+                    l_run[r][e] *= corr[e];
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        const float p0 = exp2_approx(fmaf(sc[r][h][2 * u], fs[r][0], mo[0])), p1 = exp2_approx(fmaf(sc[r][h][2 * u + 1], fs[r][1], mo[1]));
+                        l_run[r][0] += p0;
+                        l_run[r][1] += p1;
+                        const float f = sv[h][u] * sv_inv;
+                        pb[r][h][u] = movmatrix_trans(pack_f16x2(p0 * f, p1 * f));
+                    }
                 if (__any_sync(0xffffffffu, grown)) {
-                    const float oc = corr * sv_corr;
+                    const float c0 = corr[0] * sv_corr, c1 = corr[1] * sv_corr;
 #pragma unroll
-                    for (int i = 0; i < 2 * ND; ++i) { o[r][i][0] *= oc; o[r][i][1] *= oc; o[r][i][2] *= oc; o[r][i][3] *= oc; }
-                }
-#pragma unroll
-                for (int g = 0; g < 2; ++g) {
-                    const uint32_t p0 = split_e4m3(p[4 * g] * sv[4 * g], p[4 * g + 1] * sv[4 * g + 1], kPlo8);
-                    const uint32_t p1 = split_e4m3(p[4 * g + 2] * sv[4 * g + 2], p[4 * g + 3] * sv[4 * g + 3], kPlo8);
-                    pa[r][2 * g] = __byte_perm(p0, p1, 0x5410);
-                    pa[r][2 * g + 1] = __byte_perm(p0, p1, 0x7632);
+                    for (int i = 0; i < ND; ++i) { o[r][i][0] *= c0; o[r][i][1] *= c1; o[r][i][2] *= c0; o[r][i][3] *= c1; }
                 }
             }
-            // ---- weighted values. In a block that some row does not see whole, what it does not see is a later row's value and need not
-            // be a number: there a value that is no number counts as 0 in the products, and is put in afterwards where it is seen
+            // ---- weighted values: dims 16 c + 2 g, 16 c + 2 g + 1 of pairs kq, kq + 1. In a block that some row does not see whole, what
+            // it does not see is a later row's value and need not be a number: there a value that is no number counts as 0 in the
+            // products, and is put in afterwards where it is seen
             uint32_t bad = 0;
 #pragma unroll
             for (int c = 0; c < ND; ++c) {
@@ -629,50 +658,48 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
                         bad |= nan;
                     }
                 }
-                const uint32_t e0 = __byte_perm(v[0], v[1], 0x6420), e1 = __byte_perm(v[2], v[3], 0x6420);       // dims 16c + 2u
-                const uint32_t d0 = __byte_perm(v[0], v[1], 0x7531), d1 = __byte_perm(v[2], v[3], 0x7531);       // dims 16c + 2u + 1
 #pragma unroll
-                for (int r = 0; r < RW; ++r) {
-                    mma_e4m3(o[r][2 * c], pa[r][0], pa[r][1], pa[r][2], pa[r][3], e0, e1);
-                    mma_e4m3(o[r][2 * c + 1], pa[r][0], pa[r][1], pa[r][2], pa[r][3], d0, d1);
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t w0 = __byte_perm(v[2 * h], 0, 0x3120), w1 = __byte_perm(v[2 * h + 1], 0, 0x3120);       // tokens 8 more
+                    const uint32_t a0 = e4m3lo_f16x2(w0), a1 = e4m3hi_f16x2(w0), a2 = e4m3lo_f16x2(w1), a3 = e4m3hi_f16x2(w1);
+#pragma unroll
+                    for (int r = 0; r < RW; ++r) mma_f16(o[r][c], a0, a1, a2, a3, pb[r][h][0], pb[r][h][1]);
                 }
             }
             if (edge && __any_sync(0xffffffffu, bad != 0u)) {
 #pragma unroll
                 for (int c = 0; c < ND; ++c)
 #pragma unroll 1
-                    for (int t = 0; t < kA8Blk; ++t) {       // dims 16c + 2 kq + 0..3 of a token: those of o[..][2c][0], [2c + 1][0], [2c][1], [2c + 1][1]
-                        uint32_t w;
-                        asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w) : "r"(sb + Lay::KV + piece_at<DH>(t, c) + (uint32_t)(lane & 3) * 4) : "memory");
-                        const uint32_t nan = __vcmpeq4(w & 0x7f7f7f7fu, 0x7f7f7f7fu);
+                    for (int t = 0; t < kA8Blk; ++t) {
+                        uint16_t w;
+                        asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(sb + Lay::KV + piece_at<DH>(t, c) + (uint32_t)g * 2) : "memory");
+                        const bool n0 = (w & 0x7fu) == 0x7fu, n1 = (w & 0x7f00u) == 0x7f00u;
 #pragma unroll
-                        for (int r = 0; r < RW; ++r) {
-                            const uint32_t hit = t < pn[r] - tb ? nan : 0u;
-                            o[r][2 * c][0] += (hit & 0xffu) ? NAN : 0.f;
-                            o[r][2 * c + 1][0] += (hit & 0xff00u) ? NAN : 0.f;
-                            o[r][2 * c][1] += (hit & 0xff0000u) ? NAN : 0.f;
-                            o[r][2 * c + 1][1] += (hit & 0xff000000u) ? NAN : 0.f;
-                        }
+                        for (int r = 0; r < RW; ++r)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const bool seen = tb + t < pn[r][e];
+                                o[r][c][e] += seen && n0 ? NAN : 0.f;
+                                o[r][c][2 + e] += seen && n1 ? NAN : 0.f;
+                            }
                     }
             }
         }
         // ---- the chunk's partial result: o and the sum relative to the maximum, the maximum (log2 units)
 #pragma unroll
-        for (int r = 0; r < RW; ++r) {
-            float l = l_run[r];
-            l += __shfl_xor_sync(0xffffffffu, l, 1);
-            l += __shfl_xor_sync(0xffffffffu, l, 2);
-            if (prow[r] < nv && pn[r] > it.t0) {     // (such a pair, and it sees something of the chunk)
-                float *out = pout[r] + (size_t)it.chunk * (DH + 2);
+        for (int r = 0; r < RW; ++r)
 #pragma unroll
-                for (int c = 0; c < ND; ++c) {       // dims 16c + 2 kq + 0..3
-                    const float *x = o[r][2 * c], *y = o[r][2 * c + 1];
-                    *reinterpret_cast<float2 *>(out + c * 16) = make_float2(fmaf(x[2], 1.f / kPlo8, x[0]) * sv_run, fmaf(y[2], 1.f / kPlo8, y[0]) * sv_run);
-                    *reinterpret_cast<float2 *>(out + c * 16 + 2) = make_float2(fmaf(x[3], 1.f / kPlo8, x[1]) * sv_run, fmaf(y[3], 1.f / kPlo8, y[1]) * sv_run);
+            for (int e = 0; e < 2; ++e) {
+                float l = l_run[r][e];
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
+                if (prow[r][e] < nv && pn[r][e] > it.t0) {       // such a pair, and it sees something of the chunk
+                    float *out = a.part + pout[r][e] + (size_t)it.chunk * (DH + 2);
+#pragma unroll
+                    for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(out + c * 16 + g * 2) = make_float2(o[r][c][e] * sv_run, o[r][c][2 + e] * sv_run);
+                    if (g == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(m_run[r][e] * fs[r][e], l);
                 }
-                if ((lane & 3) == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(m_run[r] * fs[r], l);
             }
-        }
         __syncwarp();
         if (item + 1 < i_end) {
             const int seq = it.seq, kvh = it.kvh, set = it.set;
@@ -779,8 +806,11 @@ int kv8_read(const Kv8Shape &sh, const Kv8Ptrs &kv, int B, int max_n, const int3
 }
 
 int kv8_attention_slots(const Kv8Shape &sh, int M) {
-    const int cap = cap8(M * (sh.Hq / sh.Hkv)), most = (sh.max_ctx + kA8Chunk - 1) / kA8Chunk;
-    return most < cap ? most : cap;
+    // the largest number of chunks of any context up to max_ctx
+    const Chunk8 r = chunk8_rule(M * (sh.Hq / sh.Hkv));
+    auto up = [](int n, int c) { return (n + c - 1) / c; };
+    const int few = up(sh.max_ctx, r.first) < r.few ? up(sh.max_ctx, r.first) : r.few, most = up(sh.max_ctx, r.base) < r.most ? up(sh.max_ctx, r.base) : r.most;
+    return few > most ? few : most;
 }
 
 int kv8_attention(const Kv8AttnCall &c, cudaStream_t st, long long *launches) {
