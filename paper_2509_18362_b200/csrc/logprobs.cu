@@ -1,13 +1,13 @@
 // Log probabilities of given tokens with entropy and top alternatives, in one pass over the logits.
 //
-// With m = max x, S = sum e^(x - m), T = sum e^(x - m) (x - m): log p(i) = (x_i - m) - ln S, entropy = ln S - T / S. Every thread
-// keeps its own running (m, S, T) in fp32, rescaled when its maximum grows (once per slice, the slice's maximum is known before
-// its exponentials); parts are joined in a fixed order.
+// In powers of two, against a whole number c near max x * log2(e): y = x log2(e) - c (one rounding), S = sum 2^y, T = sum 2^y y;
+// log p(i) = ln2 (y_i - log2 S), entropy = ln2 (log2 S - T / S). Every thread keeps its own (c, S, T) in fp32 and rescales when its
+// maximum grows (a power of two, exact; once per slice, whose maximum is known before its exponentials); parts are joined in a fixed
+// order. Two elements at a time (fma.f32x2): 4.5 instructions each, of which one is the exponential (16 per clock and SM).
 //
-// The top n: a CTA keeps the n best (value, id) keys of its part so far. A slice can only matter where a thread's maximum reaches
-// the n-th best, which after the first slices is rare, so the usual cost is one comparison per thread and slice. Where it happens
-// the threads that can contribute push their elements above a lower bound of the slice's own n-th best (see collect), and
-// the list is ranked by counting.
+// The top n: the first slice of a CTA's part of a row gives a list of its n best (value, id) keys (collect). Later slices push
+// what reaches the list's n-th best into shared memory without meeting; after slices 2, 4, 8 ... the list is made anew
+// from both by counting. A thread finds its candidates by the maxima of its 16-byte vectors and reads those vectors again.
 //
 // Slices are as in verify.cu: a launch has up to two CTAs per SM, each takes a contiguous range of slices and publishes a part
 // for every row that it meets; the CTA that completes a row joins the row's parts and writes its outputs.
@@ -22,27 +22,27 @@ namespace {
 constexpr uint32_t kDevBadToken = 0x1u, kDevAllNan = 0x10u;
 constexpr int kLpThreads = 256, kLpCtasPerSm = 2, kLpWarps = kLpThreads / 32;
 constexpr int kLpCap = kLpMaxTop * 64;               // candidates of a slice: n threads' elements at most
-constexpr float kLpFar = 1e30f;                      // beyond: see finish
+constexpr float kLpLow = -2097152.f;                 // lower values count as this in the sums: as nothing, but for rows that finish() adds up anew
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+constexpr float kLpMaxRef = 4194304.f, kLpMinRef = -3000000.f;        // references c outside: likewise
 
 // Key of a value: larger value, larger key; minus infinity and NaN have the same, the smallest (1).
 __device__ __forceinline__ uint32_t lp_order(float v) { return v > -INFINITY ? float_order_key(v + 0.0f) : 1u; }       // + 0: -0 and +0 are one value
 __device__ __forceinline__ float lp_value(uint32_t k) { return k <= 1u ? -INFINITY : __uint_as_float((k & 0x80000000u) ? k ^ 0x80000000u : ~k); }
-__device__ __forceinline__ unsigned long long lp_key(float v, int id) { return ((unsigned long long)lp_order(v) << 32) | (0xffffffffu - (uint32_t)id); }
 
 template <bool F32> struct Elem;
 template <> struct Elem<false> {
     typedef bf16_t T;
     static constexpr int N = 8;                      // elements of a 16-byte vector
     static constexpr uint32_t NONE = 0xff80ff80u;    // minus infinity
-    static constexpr float LOWEST = -3.3895313892515355e38f;
     static __device__ __forceinline__ float at(const uint4 &v, int i) {
         const uint32_t w = i < 2 ? v.x : i < 4 ? v.y : i < 6 ? v.z : v.w;
         return (i & 1) ? bf16hi_f32(w) : bf16lo_f32(w);
     }
     static __device__ __forceinline__ float one(const T *p) { return bf16bits_f32(*p); }
-    // NaN and minus infinity become the type's lowest number
+    // NaN, minus infinity and what is below it become kLpLow
     static __device__ __forceinline__ void clean(uint4 &v) {
-        constexpr uint32_t low = 0xff7fff7fu;
+        constexpr uint32_t low = 0xca00ca00u;
         asm("max.bf16x2 %0, %0, %1;" : "+r"(v.x) : "r"(low));
         asm("max.bf16x2 %0, %0, %1;" : "+r"(v.y) : "r"(low));
         asm("max.bf16x2 %0, %0, %1;" : "+r"(v.z) : "r"(low));
@@ -60,11 +60,10 @@ template <> struct Elem<true> {
     typedef float T;
     static constexpr int N = 4;
     static constexpr uint32_t NONE = 0xff800000u;
-    static constexpr float LOWEST = -3.4028234663852886e38f;
     static __device__ __forceinline__ float at(const uint4 &v, int i) { return __uint_as_float(i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w); }
     static __device__ __forceinline__ float one(const T *p) { return *p; }
     static __device__ __forceinline__ void clean(uint4 &v) {
-        constexpr float low = LOWEST;
+        constexpr float low = kLpLow;
         v.x = __float_as_uint(fmaxf(__uint_as_float(v.x), low)); v.y = __float_as_uint(fmaxf(__uint_as_float(v.y), low));
         v.z = __float_as_uint(fmaxf(__uint_as_float(v.z), low)); v.w = __float_as_uint(fmaxf(__uint_as_float(v.w), low));
     }
@@ -87,25 +86,50 @@ struct LpShared {
     unsigned long long bound;
 };
 
-// Takes up to n best of the threads' elements and of the list into the list. The threads' elements are what each(f) hands to f as
-// (value, id) keys; the order key of the thread's largest value is `top` at most and `sure` at least (0: it has no element). Every
-// thread calls it.
+__device__ __forceinline__ void push(LpShared &sh, unsigned long long key) {
+    const int at = atomicAdd(&sh.n_cand, 1);
+    if (at < kLpCap) sh.cand[at] = key;
+}
+
+// The n best of the candidates and of the list become the list, best first; no candidates are left. Every thread calls it, with all
+// candidates visible.
+__device__ __forceinline__ void rank(LpShared &sh, int n) {
+    const int tid = threadIdx.x, nc = min(sh.n_cand, kLpCap), nl = sh.n_list, all = nc + nl;
+    for (int i = tid; i < all; i += kLpThreads) {    // keys differ: an entry's place is the number of larger ones
+        const unsigned long long key = i < nc ? sh.cand[i] : sh.list[i - nc];
+        int above = 0;
+#pragma unroll 4
+        for (int u = 0; u < nc; ++u) above += sh.cand[u] > key;
+#pragma unroll 4
+        for (int u = 0; u < nl; ++u) above += sh.list[u] > key;
+        if (above < n) sh.next[above] = key;
+    }
+    __syncthreads();
+    const int nn = min(all, n);
+    if (tid < nn) sh.list[tid] = sh.next[tid];
+    if (tid == 0) { sh.n_list = nn; sh.n_cand = 0; }
+    __syncthreads();
+}
+
+// Takes up to n best of the threads' elements and of the list into the list, whatever the elements are. each(bound, f) hands f the
+// thread's elements as (value, id) keys, all whose order key is `bound` or more at least; the order key of the thread's largest value
+// is `top` at most and `sure` at least (0: it has no element). Every thread calls it, with no candidates left over.
 template <typename Each>
 __device__ __forceinline__ void collect(LpShared &sh, int n, uint32_t top, uint32_t sure, Each each) {
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const unsigned long long floor_key = sh.n_list == n ? sh.list[n - 1] : 0ull;             // an element has to be above this
-    const bool may = top != 0u && top >= (uint32_t)(floor_key >> 32);
+    const bool may = top != 0u && top >= (uint32_t)(floor_key >> 32), whole = __all_sync(0xffffffffu, may);
     const int cnt = __syncthreads_count(may);
     if (cnt == 0) return;
     // Lower bound of the n-th best: of the f warps all of whose lanes may have something, the smallest of their ceil(n / f)-th
     // largest maxima: n threads at least hold a value as large
     uint32_t bound = 0u;
     if (cnt > n) {
-        const int full = __syncthreads_count(__all_sync(0xffffffffu, may)) / 32;
+        const int full = __syncthreads_count(whole) / 32;
         if (full > 0) {
             const int rounds = (n + full - 1) / full;
             uint32_t k = may ? sure : 0u, b = 0xffffffffu;
-            if (__all_sync(0xffffffffu, may))
+            if (whole)
                 for (int r = 0; r < rounds; ++r) {
                     b = __reduce_max_sync(0xffffffffu, k);
                     const uint32_t who = __ballot_sync(0xffffffffu, k == b);
@@ -118,21 +142,15 @@ __device__ __forceinline__ void collect(LpShared &sh, int n, uint32_t top, uint3
             for (int w = 1; w < kLpWarps; ++w) bound = min(bound, sh.warp_bound[w]);
         }
     }
-    if (tid == 0) sh.n_cand = 0;
-    __syncthreads();
     if (may && top >= bound)
-        each([&](unsigned long long key) {
-            if ((uint32_t)(key >> 32) >= bound && key > floor_key) {
-                const int at = atomicAdd(&sh.n_cand, 1);
-                if (at < kLpCap) sh.cand[at] = key;
-            }
-        });
+        each(bound, [&](unsigned long long key) { if ((uint32_t)(key >> 32) >= bound && key > floor_key) push(sh, key); });
     __syncthreads();
     if (sh.n_cand > kLpCap) {
-        // Too many equal values (or one warp with nothing near): the exact n-th best of the threads' own best keys bounds the
+        // Too many equal values (or no warp to take a bound from): the exact n-th best of the threads' own best keys bounds the
         // candidates to the elements of n threads
+        __syncthreads();
         unsigned long long mine = 0ull;
-        if (may) each([&](unsigned long long key) { mine = key > mine ? key : mine; });
+        if (may) each(0u, [&](unsigned long long key) { mine = key > mine ? key : mine; });
         sh.best[tid] = mine;
         if (tid == 0) { sh.n_cand = 0; sh.bound = 0ull; }
         __syncthreads();
@@ -142,27 +160,10 @@ __device__ __forceinline__ void collect(LpShared &sh, int n, uint32_t top, uint3
         __syncthreads();
         const unsigned long long lo = sh.bound;
         if (mine != 0ull && mine >= lo)
-            each([&](unsigned long long key) {
-                if (key >= lo && key > floor_key) {
-                    const int at = atomicAdd(&sh.n_cand, 1);
-                    if (at < kLpCap) sh.cand[at] = key;
-                }
-            });
+            each((uint32_t)(lo >> 32), [&](unsigned long long key) { if (key >= lo && key > floor_key) push(sh, key); });
         __syncthreads();
     }
-    const int nc = min(sh.n_cand, kLpCap), nl = sh.n_list, all = nc + nl;
-    for (int i = tid; i < all; i += kLpThreads) {    // keys differ: an entry's place is the number of larger ones
-        const unsigned long long key = i < nc ? sh.cand[i] : sh.list[i - nc];
-        int above = 0;
-        for (int u = 0; u < nc; ++u) above += sh.cand[u] > key;
-        for (int u = 0; u < nl; ++u) above += sh.list[u] > key;
-        if (above < n) sh.next[above] = key;
-    }
-    __syncthreads();
-    const int nn = min(all, n);
-    if (tid < nn) sh.list[tid] = sh.next[tid];
-    if (tid == 0) sh.n_list = nn;
-    __syncthreads();
+    rank(sh, n);
 }
 
 // Sum over the block in a fixed order, and maximum; every thread gets them.
@@ -189,11 +190,28 @@ __device__ __forceinline__ float lp_max(float v, float *red) {
     return t;
 }
 
-constexpr float kLog2e = 1.4426950408889634f;
 __device__ __forceinline__ float lp_exp2(float x) {
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
+}
+// Two fp32 values at a time.
+typedef unsigned long long f32x2;
+__device__ __forceinline__ f32x2 pair(float a, float b) {
+    f32x2 r;
+    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+    return r;
+}
+__device__ __forceinline__ void unpair(f32x2 v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
+__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
+    f32x2 r;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+    return r;
+}
+__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
+    f32x2 r;
+    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+    return r;
 }
 
 template <bool F32, int NV>
@@ -213,99 +231,163 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprobs_kernel(cons
     // Slice s of a row starts s * SLICE elements behind the 16-byte boundary at or below the row; a vector that lies across one of
     // the row's ends is put together from single elements, minus infinity for what is outside
     auto row_ptr = [&](int row) -> const T * { return logits + (long long)row * c.ld; };
-    auto offset_of = [&](const T *p) -> int { return (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T)); };
+    auto first_of = [&](int row, int slice) -> int {          // the thread's first element in a slice
+        return slice * SLICE + tid * EV - (int)((reinterpret_cast<uintptr_t>(row_ptr(row)) & 15u) / sizeof(T));
+    };
+    auto load_vec = [&](const T *p, int e) -> uint4 {
+        if (e >= 0 && e + EV <= V) return ldnc128(p + e);
+        uint32_t w[4] = {El::NONE, El::NONE, El::NONE, El::NONE};
+        if (e + EV > 0 && e < V) {
+#pragma unroll
+            for (int q = 0; q < EV; ++q)
+                if ((unsigned)(e + q) < (unsigned)V) {
+                    if constexpr (F32) w[q] = __float_as_uint(p[e + q]);
+                    else w[q >> 1] = (q & 1) ? (w[q >> 1] & 0xffffu) | ((uint32_t)p[e + q] << 16) : (w[q >> 1] & 0xffff0000u) | p[e + q];
+                }
+        }
+        return make_uint4(w[0], w[1], w[2], w[3]);
+    };
     auto load = [&](int row, int slice, uint4 (&v)[NV]) {
         const T *p = row_ptr(row);
-        const int off = offset_of(p);
+        const int e0 = first_of(row, slice);
+        if (__all_sync(0xffffffffu, e0 >= 0 && e0 + (NV - 1) * kLpThreads * EV + EV <= V)) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            const int e = slice * SLICE + (j * kLpThreads + tid) * EV - off;      // the vector's first element
-            if (e >= 0 && e + EV <= V) v[j] = ldnc128(p + e);
-            else {
-                uint32_t w[4] = {El::NONE, El::NONE, El::NONE, El::NONE};
-                if (e + EV > 0 && e < V) {
+            for (int j = 0; j < NV; ++j) v[j] = ldnc128(p + e0 + j * kLpThreads * EV);
+        } else {
 #pragma unroll
-                    for (int q = 0; q < EV; ++q)
-                        if ((unsigned)(e + q) < (unsigned)V) {
-                            if constexpr (F32) w[q] = __float_as_uint(p[e + q]);
-                            else w[q >> 1] = (q & 1) ? (w[q >> 1] & 0xffffu) | ((uint32_t)p[e + q] << 16) : (w[q >> 1] & 0xffff0000u) | p[e + q];
-                        }
-                }
-                v[j] = make_uint4(w[0], w[1], w[2], w[3]);
+            for (int j = 0; j < NV; ++j) v[j] = load_vec(p, e0 + j * kLpThreads * EV);
+        }
+    };
+    // the elements of the thread's vectors in `mask` (read once more) whose order key is `bound` or more
+    auto scan = [&](int row, int slice, uint32_t mask, uint32_t bound, auto f) {
+        const T *p = row_ptr(row);
+        const int e0 = first_of(row, slice);
+        while (mask) {
+            const int j = __ffs(mask) - 1, e = e0 + j * kLpThreads * EV;
+            mask &= mask - 1;
+            const uint4 v = load_vec(p, e);
+#pragma unroll
+            for (int q = 0; q < EV; ++q) {
+                const float x = El::at(v, q);
+                const uint32_t k = lp_order(x);
+                if (k >= bound && (unsigned)(e + q) < (unsigned)V) f(((unsigned long long)k << 32) | (0xffffffffu - (uint32_t)(e + q)));
             }
         }
+    };
+    // which of the vectors hold a value whose order key is `bound` or more, or might (all of them where that is hard to tell)
+    auto vectors = [&](const uint4 (&v)[NV], uint32_t bound) -> uint32_t {
+        uint32_t mask = 0;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            uint4 x = v[j];
+            El::clean(x);
+            mask |= (lp_order(El::vec_max(x)) >= bound ? 1u : 0u) << j;
+        }
+        return mask;
+    };
+    // collect() on a slice in registers
+    auto collect_slice = [&](int row, int slice, const uint4 (&v)[NV]) {
+        float bm = kLpLow;
+#pragma unroll
+        for (int j = 0; j < NV; ++j) {
+            uint4 x = v[j];
+            El::clean(x);
+            bm = fmaxf(bm, El::vec_max(x));
+        }
+        const bool some = first_of(row, slice) < V;          // (a row's first vector may begin before the row)
+        collect(sh, n, some ? lp_order(bm) : 0u, !some ? 0u : bm > kLpLow ? lp_order(bm) : 1u,
+                [&](uint32_t bound, auto f) { scan(row, slice, vectors(v, bound), bound, f); });
     };
 
     uint4 cur[NV], nxt[NV];
     int row = (int)(i0 / a.spr), slice = (int)(i0 - (long long)row * a.spr);
     if (i0 < i1) load(row, slice, cur);
-    float m = -INFINITY, S = 0.f, Tt = 0.f;          // the thread's part of the current row
-    if (tid == 0) sh.n_list = 0;
+    float ref = -1e30f;                              // the thread's part of the current row
+    f32x2 S2 = 0ull, T2 = 0ull;
+    int k = 0, slice0 = slice;                       // slices of the row so far, the first one
+    float tau = 0.f;                                 // the list's n-th best value once there is one
+    if (tid == 0) { sh.n_list = 0; sh.n_cand = 0; }
     __syncthreads();
     for (long long item = i0; item < i1; ++item) {
         int nrow = row, nslice = slice + 1;
         if (nslice == a.spr) { nslice = 0; ++nrow; }
         if (item + 1 < i1) load(nrow, nslice, nxt);  // the next slice's loads go out before this one's values are used
+        const bool ends = nrow != row || item + 1 == i1;
+        ++k;
         // ---- sums
-        float bm = -INFINITY;
+        uint32_t hits = 0;
         {
             uint4 x[NV];
+            float bm = kLpLow;
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
                 x[j] = cur[j];
                 El::clean(x[j]);
-                bm = fmaxf(bm, El::vec_max(x[j]));
+                const float vm = El::vec_max(x[j]);
+                hits |= (vm >= tau ? 1u : 0u) << j;
+                bm = fmaxf(bm, vm);
             }
-            if (bm > m) {
-                const float d = m - bm, f = lp_exp2(d * kLog2e);                  // (0 for the first slice)
-                Tt = f > 0.f ? f * (Tt + S * d) : 0.f;
-                S *= f;
-                m = bm;
+            const float want = rintf(bm * kLog2e);
+            if (want > ref) {
+                const float d = ref - want, f = lp_exp2(d);
+                float s0, s1, t0, t1;
+                unpair(S2, s0, s1);
+                unpair(T2, t0, t1);
+                T2 = pair(f * fmaf(s0, d, t0), f * fmaf(s1, d, t1));
+                S2 = pair(f * s0, f * s1);
+                ref = want;
             }
-            float s0 = 0.f, s1 = 0.f, t0 = 0.f, t1 = 0.f;
+            const f32x2 L2 = pair(kLog2e, kLog2e), R2 = pair(-ref, -ref);
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int q = 0; q < EV; q += 2) {
-                    const float d0 = El::at(x[j], q) - m, d1 = El::at(x[j], q + 1) - m;
-                    const float e0 = lp_exp2(d0 * kLog2e), e1 = lp_exp2(d1 * kLog2e);
-                    s0 += e0; s1 += e1;
-                    t0 = fmaf(e0, d0, t0); t1 = fmaf(e1, d1, t1);
+                    const f32x2 y = fma2(pair(El::at(x[j], q), El::at(x[j], q + 1)), L2, R2);
+                    float y0, y1;
+                    unpair(y, y0, y1);
+                    const f32x2 e = pair(lp_exp2(y0), lp_exp2(y1));
+                    S2 = add2(S2, e);
+                    T2 = fma2(e, y, T2);
                 }
-            S += s0 + s1;
-            Tt += t0 + t1;
         }
-        // ---- top candidates (of the values as they are: minus infinity is below the lowest number)
+        // ---- top candidates (of the values as they are)
         if (n > 0) {
-            const int first = slice * SLICE + tid * EV - offset_of(row_ptr(row));
-            const bool some = first < V;             // (a row's first vector may begin before the row)
-            collect(sh, n, some ? lp_order(bm) : 0u, !some ? 0u : bm > El::LOWEST ? lp_order(bm) : 1u, [&](auto f) {
-#pragma unroll 1
-                for (int j = 0; j < NV; ++j) {
-                    uint4 v = cur[0];
-#pragma unroll
-                    for (int u = 1; u < NV; ++u) if (u == j) v = cur[u];
-#pragma unroll
-                    for (int q = 0; q < EV; ++q) {
-                        const int id = first + j * kLpThreads * EV + q;
-                        if ((unsigned)id < (unsigned)V) f(lp_key(El::at(v, q), id));
+            if (k == 1) collect_slice(row, slice, cur);
+            else if (hits) scan(row, slice, hits, sh.n_list == n ? (uint32_t)(sh.list[n - 1] >> 32) : 0u, [&](unsigned long long key) { push(sh, key); });
+            if (k > 1 && ((k & (k - 1)) == 0 || ends)) {
+                __syncthreads();
+                if (sh.n_cand <= kLpCap) rank(sh, n);
+                else {                               // every slice beats the ones before by far: over again, slice by slice
+                    __syncthreads();
+                    if (tid == 0) { sh.n_cand = 0; sh.n_list = 0; }
+                    __syncthreads();
+                    for (int q = slice0; q <= slice; ++q) {
+                        load(row, q, cur);
+                        collect_slice(row, q, cur);
                     }
                 }
-            });
+            }
+            // a list that is not full (a part shorter than n) takes everything
+            if ((k & (k - 1)) == 0) tau = sh.n_list == n ? lp_value((uint32_t)(sh.list[n - 1] >> 32)) : -INFINITY;
         }
-        if (nrow != row || item + 1 == i1) {
+        if (ends) {
             // ---- this CTA's part of the row is done
             const long long r0 = (long long)row * a.spr;
             const int c_first = (int)(((r0 + 1) * G - 1) / N), c_last = (int)(((r0 + a.spr) * G - 1) / N), parts = c_last - c_first + 1;
-            float M = lp_max(m, sh.red[0]);
-            const float f = m > -INFINITY ? lp_exp2((m - M) * kLog2e) : 0.f;
-            const float dm = m - M;
-            float Tr = lp_sum(S > 0.f && f > 0.f ? f * (Tt + S * dm) : 0.f, sh.red[1]);
-            float Sr = lp_sum(S > 0.f ? f * S : 0.f, sh.red[2]);
+            float R = lp_max(ref, sh.red[0]);
+            float Sr, Tr;
+            {
+                const float d = ref - R, f = lp_exp2(d);
+                float s0, s1, t0, t1;
+                unpair(S2, s0, s1);
+                unpair(T2, t0, t1);
+                Tr = lp_sum(f * fmaf(s0 + s1, d, t0 + t1), sh.red[1]);
+                Sr = lp_sum(f * (s0 + s1), sh.red[2]);
+            }
             bool finish = parts == 1;
             if (!finish) {
                 LpPart *p = c.parts + row + blockIdx.x;
-                if (tid == 0) { p->m = M; p->s = Sr; p->t = Tr; }
+                if (tid == 0) { p->m = R; p->s = Sr; p->t = Tr; }
                 if (tid < n) p->top[tid] = tid < sh.n_list ? sh.list[tid] : 0ull;
                 __threadfence();
                 __syncthreads();
@@ -319,15 +401,14 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprobs_kernel(cons
                 if (finish) {
                     __threadfence();
                     const LpPart *p0 = c.parts + row + c_first;
-                    float mm = -INFINITY;
+                    float mm = -1e30f;
                     for (int i = tid; i < parts; i += kLpThreads) mm = fmaxf(mm, ldcg_f32(&p0[i].m));
-                    M = lp_max(mm, sh.red[0]);
+                    R = lp_max(mm, sh.red[0]);
                     float s = 0.f, t = 0.f;
                     for (int i = tid; i < parts; i += kLpThreads) {
-                        const float pm = ldcg_f32(&p0[i].m), ps = ldcg_f32(&p0[i].s), pt = ldcg_f32(&p0[i].t);
-                        const float d = pm - M, e = pm > -INFINITY ? lp_exp2(d * kLog2e) : 0.f;
-                        s += e * ps;
-                        t += e > 0.f ? e * (pt + ps * d) : 0.f;
+                        const float ps = ldcg_f32(&p0[i].s), pt = ldcg_f32(&p0[i].t), d = ldcg_f32(&p0[i].m) - R, f = lp_exp2(d);
+                        s += f * ps;
+                        t += f * fmaf(ps, d, pt);
                     }
                     Sr = lp_sum(s, sh.red[1]);
                     Tr = lp_sum(t, sh.red[2]);
@@ -335,10 +416,10 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprobs_kernel(cons
                         const int keys = parts * n;
                         uint32_t top = 0u;
                         for (int i = tid; i < keys; i += kLpThreads) top = max(top, (uint32_t)(ldcg_u64(&p0[i / n].top[i % n]) >> 32));
-                        collect(sh, n, top, top, [&](auto f2) {
+                        collect(sh, n, top, top, [&](uint32_t bound, auto f) {
                             for (int i = tid; i < keys; i += kLpThreads) {
                                 const unsigned long long key = ldcg_u64(&p0[i / n].top[i % n]);
-                                if (key) f2(key);
+                                if (key && (uint32_t)(key >> 32) >= bound) f(key);
                             }
                         });
                     }
@@ -346,21 +427,30 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprobs_kernel(cons
             }
             if (finish) {
                 const T *p = row_ptr(row);
-                // Far from zero two different values are so far apart that only the largest count; there a sum of its own, which also
-                // tells the type's lowest number from minus infinity and takes an infinite maximum
+                // Rows whose maximum is too far from zero for the sums above (or infinite) are added up anew, against the maximum itself
+                const bool far = !(R > kLpMinRef && R < kLpMaxRef);
                 bool nothing = false;
-                if (!(fabsf(M) < kLpFar)) {
+                float M = 0.f;
+                if (far) {
                     float mx = -INFINITY;
                     for (int i = tid; i < V; i += kLpThreads) mx = fmaxf(mx, El::one(p + i));
                     M = lp_max(mx, sh.red[0]);
-                    int cnt = 0;
-                    for (int i = tid; i < V; i += kLpThreads) cnt += El::one(p + i) == M;
-                    Sr = lp_sum((float)cnt, sh.red[1]);
-                    Tr = 0.f;
                     nothing = M == -INFINITY;
+                    float s = 0.f, t = 0.f;
+                    for (int i = tid; i < V; i += kLpThreads) {
+                        const float x = El::one(p + i), y = (x - M) * kLog2e;
+                        if (x == M) s += 1.f;
+                        else if (y > -200.f) { s += lp_exp2(y); t = fmaf(lp_exp2(y), y, t); }
+                    }
+                    Sr = lp_sum(s, sh.red[1]);
+                    Tr = lp_sum(t, sh.red[2]);
                 }
-                const float lnS = logf(Sr);
-                auto logprob = [&](float x) -> float { return nothing || !(x > -INFINITY) ? -INFINITY : x == M ? -lnS : (x - M) - lnS; };
+                const float lgS = log2f(Sr);
+                auto logprob = [&](float x) -> float {
+                    if (nothing || !(x > -INFINITY)) return -INFINITY;
+                    if (far) return (x == M ? 0.f : x - M) - kLn2 * lgS;
+                    return x < kLpLow ? x - kLn2 * (R + lgS) : kLn2 * (fmaf(x, kLog2e, -R) - lgS);
+                };
                 if (tid == 0) {
                     if (nothing) atomicOr(c.status, kDevAllNan);
                     if (c.out_logprob) {
@@ -368,7 +458,7 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprobs_kernel(cons
                         if ((unsigned)tok >= (unsigned)V) { atomicOr(c.status, kDevBadToken); tok = 0; }
                         c.out_logprob[row] = logprob(El::one(p + tok));
                     }
-                    if (c.out_entropy) c.out_entropy[row] = nothing ? 0.f : fmaxf(lnS - Tr / Sr, 0.f);
+                    if (c.out_entropy) c.out_entropy[row] = nothing ? 0.f : fmaxf(kLn2 * (lgS - Tr / Sr), 0.f);
                 }
                 if (tid < n) {                       // (V >= n: the list is full)
                     const unsigned long long key = sh.list[tid];
@@ -378,9 +468,13 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprobs_kernel(cons
                 }
             }
             __syncthreads();
-            if (tid == 0) sh.n_list = 0;
+            if (tid == 0) { sh.n_list = 0; sh.n_cand = 0; }
             __syncthreads();
-            m = -INFINITY; S = 0.f; Tt = 0.f;
+            ref = -1e30f;
+            S2 = T2 = 0ull;
+            k = 0;
+            slice0 = nslice;
+            tau = 0.f;
         }
         row = nrow;
         slice = nslice;
