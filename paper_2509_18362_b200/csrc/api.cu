@@ -32,7 +32,7 @@ struct fmtp_ctx {
     unsigned long long *vkeys;
     uint32_t *vcounter;
     LpPart *lp_parts;          // fastmtp_logprobs
-    uint32_t *lp_counters;
+    uint32_t *lp_counters, *lp_strips;
     // staging for the *_host entry points (device side inside the workspace, host side pinned)
     bf16_t *st_h;
     int32_t *st_tok, *st_next, *st_out;
@@ -120,6 +120,7 @@ size_t layout(fmtp_ctx *c, unsigned char *base) {
     c->vkeys = cv.take<unsigned long long>(kVerifyMaxRows);
     c->vcounter = cv.take<uint32_t>(1);
     c->lp_parts = cv.take<LpPart>((size_t)logprobs_slots(c->n_sm));
+    c->lp_strips = cv.take<uint32_t>((size_t)logprobs_slots(c->n_sm) * kLpStrips);
     c->lp_counters = cv.take<uint32_t>(kLpMaxRows);
     c->st_h = cv.take<bf16_t>((size_t)RB * d);
     c->st_tok = cv.take<int32_t>((size_t)RB);
@@ -806,7 +807,7 @@ int fastmtp_logprobs(fmtp_ctx *c, const void *logits, int f32, long long ld, con
     std::memset(&a, 0, sizeof(a));
     a.logits = logits; a.f32 = f32 != 0; a.ld = ld; a.tokens = tokens; a.rows = rows; a.V = V; a.top = top_n;
     a.out_logprob = out_logprob; a.out_entropy = out_entropy; a.out_ids = out_top_ids; a.out_tops = out_top_logprobs;
-    a.parts = c->lp_parts; a.counters = c->lp_counters; a.status = dev_status ? dev_status : c->s.status; a.n_sm = c->n_sm;
+    a.parts = c->lp_parts; a.counters = c->lp_counters; a.strips = c->lp_strips; a.status = dev_status ? dev_status : c->s.status; a.n_sm = c->n_sm;
     int err = logprobs_launch(a, static_cast<cudaStream_t>(stream));
     if (err) return cuda_fail(c, (cudaError_t)err);
     c->launches++;

@@ -3,13 +3,15 @@
 // In powers of two, against a whole number c near max x * log2(e): y = x log2(e) - c (one rounding), S = sum 2^y, T = sum 2^y y;
 // log p(i) = ln2 (y_i - log2 S), entropy = ln2 (log2 S - T / S). Every thread keeps its own (c, S, T) in fp32 and rescales when its
 // maximum grows (a power of two, exact; once per slice, whose maximum is known before its exponentials); parts are joined in a fixed
-// order. Two elements at a time (fma.f32x2): 4.5 instructions each, of which one is the exponential (16 per clock and SM).
+// order.
 //
-// The top n: the first slice of a CTA's part of a row gives a list of its n best (value, id) keys (collect). Later slices push
-// what reaches the list's n-th best into shared memory without meeting; after slices 2, 4, 8 ... the list is made anew
-// from both by counting. A thread finds its candidates by the maxima of its 16-byte vectors and reads those vectors again.
+// The top n: the pass itself only keeps every strip's maximum (a strip: what one thread has of a row in a CTA's part of it, or one
+// warp where parts are short). The CTA that completes a row finds a lower bound of the n-th best value from the maxima, which leaves
+// a few more than n strips, and reads those again (from L2): their elements that reach the bound are ranked by counting. Where
+// equal values leave too many strips, only the strips above the bound are read, and the bound's own ids are looked for from the
+// row's beginning.
 //
-// Slices are as in verify.cu: a launch has up to two CTAs per SM, each takes a contiguous range of slices and publishes a part
+// Slices are as in verify.cu: a launch has up to four CTAs per SM, each takes a contiguous range of slices and publishes a part
 // for every row that it meets; the CTA that completes a row joins the row's parts and writes its outputs.
 #include "logprobs.cuh"
 #include "ptx.cuh"
@@ -20,8 +22,9 @@ namespace fmtp {
 namespace {
 
 constexpr uint32_t kDevBadToken = 0x1u, kDevAllNan = 0x10u;
-constexpr int kLpThreads = 256, kLpCtasPerSm = 2, kLpWarps = kLpThreads / 32;
-constexpr int kLpCap = kLpMaxTop * 64;               // candidates of a slice: n threads' elements at most
+constexpr int kLpThreads = kLpStrips, kLpCtasPerSm = 4, kLpWarps = kLpThreads / 32;
+constexpr int kLpCap = kLpMaxTop * 64;               // candidates that are ranked at once
+constexpr int kLpStripCap = 256;                     // strips that are read again
 constexpr float kLpLow = -2097152.f;                 // lower values count as this in the sums: as nothing, but for rows that finish() adds up anew
 constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
 constexpr float kLpMaxRef = 4194304.f, kLpMinRef = -3000000.f;        // references c outside: likewise
@@ -48,7 +51,7 @@ template <> struct Elem<false> {
         asm("max.bf16x2 %0, %0, %1;" : "+r"(v.z) : "r"(low));
         asm("max.bf16x2 %0, %0, %1;" : "+r"(v.w) : "r"(low));
     }
-    static __device__ __forceinline__ float vec_max(const uint4 &v) {        // of a cleaned vector
+    static __device__ __forceinline__ float vec_max(const uint4 &v) {        // (NaN only if nothing else)
         uint32_t a, b;
         asm("max.bf16x2 %0, %1, %2;" : "=r"(a) : "r"(v.x), "r"(v.y));
         asm("max.bf16x2 %0, %1, %2;" : "=r"(b) : "r"(v.z), "r"(v.w));
@@ -75,15 +78,16 @@ template <> struct Elem<true> {
 struct LpArgs {
     LpCall c;
     int spr;                                         // slices per row
+    int warp_strips;                                 // strips are warps' (else threads'): parts are short and many
     long long n_items;                               // slices of all rows
 };
 
 struct LpShared {
-    unsigned long long cand[kLpCap], list[kLpMaxTop], next[kLpMaxTop], best[kLpThreads];
+    unsigned long long cand[kLpCap], list[kLpMaxTop], next[kLpMaxTop], best[kLpThreads], bound64;
     float red[3][kLpWarps];
-    uint32_t warp_bound[kLpWarps];
-    int n_cand, n_list, last;
-    unsigned long long bound;
+    uint32_t warp_bound[kLpWarps], strip_key[kLpStripCap], bound;
+    int strip[kLpStripCap];
+    int n_cand, n_list, n_strip, last;
 };
 
 __device__ __forceinline__ void push(LpShared &sh, unsigned long long key) {
@@ -111,58 +115,41 @@ __device__ __forceinline__ void rank(LpShared &sh, int n) {
     __syncthreads();
 }
 
-// Takes up to n best of the threads' elements and of the list into the list, whatever the elements are. each(bound, f) hands f the
-// thread's elements as (value, id) keys, all whose order key is `bound` or more at least; the order key of the thread's largest value
-// is `top` at most and `sure` at least (0: it has no element). Every thread calls it, with no candidates left over.
-template <typename Each>
-__device__ __forceinline__ void collect(LpShared &sh, int n, uint32_t top, uint32_t sure, Each each) {
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    const unsigned long long floor_key = sh.n_list == n ? sh.list[n - 1] : 0ull;             // an element has to be above this
-    const bool may = top != 0u && top >= (uint32_t)(floor_key >> 32), whole = __all_sync(0xffffffffu, may);
-    const int cnt = __syncthreads_count(may);
-    if (cnt == 0) return;
-    // Lower bound of the n-th best: of the f warps all of whose lanes may have something, the smallest of their ceil(n / f)-th
-    // largest maxima: n threads at least hold a value as large
-    uint32_t bound = 0u;
-    if (cnt > n) {
-        const int full = __syncthreads_count(whole) / 32;
-        if (full > 0) {
-            const int rounds = (n + full - 1) / full;
-            uint32_t k = may ? sure : 0u, b = 0xffffffffu;
-            if (whole)
-                for (int r = 0; r < rounds; ++r) {
-                    b = __reduce_max_sync(0xffffffffu, k);
-                    const uint32_t who = __ballot_sync(0xffffffffu, k == b);
-                    if (lane == __ffs(who) - 1) k = 0u;
-                }
-            if (lane == 0) sh.warp_bound[warp] = b;
-            __syncthreads();
-            bound = sh.warp_bound[0];
-#pragma unroll
-            for (int w = 1; w < kLpWarps; ++w) bound = min(bound, sh.warp_bound[w]);
-        }
+// Lower bound of the n-th largest of the threads' keys (0: none), n <= 32: the smallest, over the warps, of a warp's ceil(n / 8)-th
+// largest key. Every thread calls it.
+__device__ __forceinline__ uint32_t nth_bound(LpShared &sh, int n, uint32_t k) {
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint32_t b = 0;
+    for (int r = (n + kLpWarps - 1) / kLpWarps; r > 0; --r) {
+        b = __reduce_max_sync(0xffffffffu, k);
+        const uint32_t who = __ballot_sync(0xffffffffu, k == b);
+        if (lane == __ffs(who) - 1) k = 0u;
     }
-    if (may && top >= bound)
-        each(bound, [&](unsigned long long key) { if ((uint32_t)(key >> 32) >= bound && key > floor_key) push(sh, key); });
+    if (lane == 0) sh.warp_bound[warp] = b;
     __syncthreads();
-    if (sh.n_cand > kLpCap) {
-        // Too many equal values (or no warp to take a bound from): the exact n-th best of the threads' own best keys bounds the
-        // candidates to the elements of n threads
-        __syncthreads();
-        unsigned long long mine = 0ull;
-        if (may) each(0u, [&](unsigned long long key) { mine = key > mine ? key : mine; });
-        sh.best[tid] = mine;
-        if (tid == 0) { sh.n_cand = 0; sh.bound = 0ull; }
-        __syncthreads();
-        int above = 0;
-        for (int u = 0; u < kLpThreads; ++u) above += sh.best[u] > mine;
-        if (mine != 0ull && above == n - 1) sh.bound = mine;
-        __syncthreads();
-        const unsigned long long lo = sh.bound;
-        if (mine != 0ull && mine >= lo)
-            each((uint32_t)(lo >> 32), [&](unsigned long long key) { if (key >= lo && key > floor_key) push(sh, key); });
-        __syncthreads();
-    }
+    b = sh.warp_bound[0];
+#pragma unroll
+    for (int w = 1; w < kLpWarps; ++w) b = min(b, sh.warp_bound[w]);
+    return b;
+}
+
+// Takes the n best of a slice's elements and of the list into the list, whatever they are: the exact n-th best of the threads' best
+// keys leaves n threads, whose elements are candidates. each(f) hands f the thread's elements as (value, id) keys.
+template <typename Each>
+__device__ __forceinline__ void collect(LpShared &sh, int n, Each each) {
+    const int tid = threadIdx.x;
+    unsigned long long mine = 0ull;
+    each([&](unsigned long long key) { mine = key > mine ? key : mine; });
+    sh.best[tid] = mine;
+    if (tid == 0) { sh.n_cand = 0; sh.bound64 = 0ull; }
+    __syncthreads();
+    int above = 0;
+    for (int u = 0; u < kLpThreads; ++u) above += sh.best[u] > mine;
+    if (mine != 0ull && above == n - 1) sh.bound64 = mine;
+    __syncthreads();
+    const unsigned long long lo = sh.bound64;
+    if (mine != 0ull && mine >= lo) each([&](unsigned long long key) { if (key >= lo) push(sh, key); });
+    __syncthreads();
     rank(sh, n);
 }
 
@@ -195,25 +182,6 @@ __device__ __forceinline__ float lp_exp2(float x) {
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
-// Two fp32 values at a time.
-typedef unsigned long long f32x2;
-__device__ __forceinline__ f32x2 pair(float a, float b) {
-    f32x2 r;
-    asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-    return r;
-}
-__device__ __forceinline__ void unpair(f32x2 v, float &a, float &b) { asm("mov.b64 {%0, %1}, %2;" : "=f"(a), "=f"(b) : "l"(v)); }
-__device__ __forceinline__ f32x2 fma2(f32x2 a, f32x2 b, f32x2 c) {
-    f32x2 r;
-    asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-    return r;
-}
-__device__ __forceinline__ f32x2 add2(f32x2 a, f32x2 b) {
-    f32x2 r;
-    asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-    return r;
-}
-
 template <bool F32, int NV>
 __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprobs_kernel(const __grid_constant__ LpArgs a) {
     chain_release();
@@ -258,149 +226,79 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprobs_kernel(cons
             for (int j = 0; j < NV; ++j) v[j] = load_vec(p, e0 + j * kLpThreads * EV);
         }
     };
-    // the elements of the thread's vectors in `mask` (read once more) whose order key is `bound` or more
-    auto scan = [&](int row, int slice, uint32_t mask, uint32_t bound, auto f) {
-        const T *p = row_ptr(row);
-        const int e0 = first_of(row, slice);
-        while (mask) {
-            const int j = __ffs(mask) - 1, e = e0 + j * kLpThreads * EV;
-            mask &= mask - 1;
-            const uint4 v = load_vec(p, e);
+    // hands f the elements of the vector at element e as (value, id) keys
+    auto keys_of = [&](const T *p, int e, auto f) {
+        const uint4 v = load_vec(p, e);
 #pragma unroll
-            for (int q = 0; q < EV; ++q) {
-                const float x = El::at(v, q);
-                const uint32_t k = lp_order(x);
-                if (k >= bound && (unsigned)(e + q) < (unsigned)V) f(((unsigned long long)k << 32) | (0xffffffffu - (uint32_t)(e + q)));
-            }
-        }
+        for (int q = 0; q < EV; ++q)
+            if ((unsigned)(e + q) < (unsigned)V) f(((unsigned long long)lp_order(El::at(v, q)) << 32) | (0xffffffffu - (uint32_t)(e + q)));
     };
-    // which of the vectors hold a value whose order key is `bound` or more, or might (all of them where that is hard to tell)
-    auto vectors = [&](const uint4 (&v)[NV], uint32_t bound) -> uint32_t {
-        uint32_t mask = 0;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) {
-            uint4 x = v[j];
-            El::clean(x);
-            mask |= (lp_order(El::vec_max(x)) >= bound ? 1u : 0u) << j;
-        }
-        return mask;
-    };
-    // collect() on a slice in registers
-    auto collect_slice = [&](int row, int slice, const uint4 (&v)[NV]) {
+    const bool by_warp = a.warp_strips != 0;
+
+    uint4 cur[NV];
+    int row = (int)(i0 / a.spr), slice = (int)(i0 - (long long)row * a.spr);
+    float ref = -1e30f, S0 = 0.f, S1 = 0.f, T0 = 0.f, T1 = 0.f;          // the thread's part of the current row
+    float top = -INFINITY;                           // its largest value
+    for (long long item = i0; item < i1; ++item) {
+        load(row, slice, cur);
+        int nrow = row, nslice = slice + 1;
+        if (nslice == a.spr) { nslice = 0; ++nrow; }
+        // ---- sums
         float bm = kLpLow;
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            uint4 x = v[j];
-            El::clean(x);
-            bm = fmaxf(bm, El::vec_max(x));
+            top = fmaxf(top, El::vec_max(cur[j]));
+            El::clean(cur[j]);
         }
-        const bool some = first_of(row, slice) < V;          // (a row's first vector may begin before the row)
-        collect(sh, n, some ? lp_order(bm) : 0u, !some ? 0u : bm > kLpLow ? lp_order(bm) : 1u,
-                [&](uint32_t bound, auto f) { scan(row, slice, vectors(v, bound), bound, f); });
-    };
-
-    uint4 cur[NV], nxt[NV];
-    int row = (int)(i0 / a.spr), slice = (int)(i0 - (long long)row * a.spr);
-    if (i0 < i1) load(row, slice, cur);
-    float ref = -1e30f;                              // the thread's part of the current row
-    f32x2 S2 = 0ull, T2 = 0ull;
-    int k = 0, slice0 = slice;                       // slices of the row so far, the first one
-    float tau = 0.f;                                 // the list's n-th best value once there is one
-    if (tid == 0) { sh.n_list = 0; sh.n_cand = 0; }
-    __syncthreads();
-    for (long long item = i0; item < i1; ++item) {
-        int nrow = row, nslice = slice + 1;
-        if (nslice == a.spr) { nslice = 0; ++nrow; }
-        if (item + 1 < i1) load(nrow, nslice, nxt);  // the next slice's loads go out before this one's values are used
-        const bool ends = nrow != row || item + 1 == i1;
-        ++k;
-        // ---- sums
-        uint32_t hits = 0;
-        {
-            uint4 x[NV];
-            float bm = kLpLow;
-#pragma unroll
-            for (int j = 0; j < NV; ++j) {
-                x[j] = cur[j];
-                El::clean(x[j]);
-                const float vm = El::vec_max(x[j]);
-                hits |= (vm >= tau ? 1u : 0u) << j;
-                bm = fmaxf(bm, vm);
-            }
-            const float want = rintf(bm * kLog2e);
-            if (want > ref) {
-                const float d = ref - want, f = lp_exp2(d);
-                float s0, s1, t0, t1;
-                unpair(S2, s0, s1);
-                unpair(T2, t0, t1);
-                T2 = pair(f * fmaf(s0, d, t0), f * fmaf(s1, d, t1));
-                S2 = pair(f * s0, f * s1);
-                ref = want;
-            }
-            const f32x2 L2 = pair(kLog2e, kLog2e), R2 = pair(-ref, -ref);
-#pragma unroll
-            for (int j = 0; j < NV; ++j)
-#pragma unroll
-                for (int q = 0; q < EV; q += 2) {
-                    const f32x2 y = fma2(pair(El::at(x[j], q), El::at(x[j], q + 1)), L2, R2);
-                    float y0, y1;
-                    unpair(y, y0, y1);
-                    const f32x2 e = pair(lp_exp2(y0), lp_exp2(y1));
-                    S2 = add2(S2, e);
-                    T2 = fma2(e, y, T2);
-                }
+        bm = fmaxf(bm, top);
+        const float want = rintf(bm * kLog2e);
+        if (want > ref) {
+            const float d = ref - want, f = lp_exp2(d);
+            T0 = f * fmaf(S0, d, T0); T1 = f * fmaf(S1, d, T1);
+            S0 *= f; S1 *= f;
+            ref = want;
         }
-        // ---- top candidates (of the values as they are)
-        if (n > 0) {
-            if (k == 1) collect_slice(row, slice, cur);
-            else if (hits) scan(row, slice, hits, sh.n_list == n ? (uint32_t)(sh.list[n - 1] >> 32) : 0u, [&](unsigned long long key) { push(sh, key); });
-            if (k > 1 && ((k & (k - 1)) == 0 || ends)) {
-                __syncthreads();
-                if (sh.n_cand <= kLpCap) rank(sh, n);
-                else {                               // every slice beats the ones before by far: over again, slice by slice
-                    __syncthreads();
-                    if (tid == 0) { sh.n_cand = 0; sh.n_list = 0; }
-                    __syncthreads();
-                    for (int q = slice0; q <= slice; ++q) {
-                        load(row, q, cur);
-                        collect_slice(row, q, cur);
-                    }
-                }
+#pragma unroll
+        for (int j = 0; j < NV; ++j)
+#pragma unroll
+            for (int q = 0; q < EV; q += 2) {
+                const float y0 = fmaf(El::at(cur[j], q), kLog2e, -ref), y1 = fmaf(El::at(cur[j], q + 1), kLog2e, -ref);
+                const float e0 = lp_exp2(y0), e1 = lp_exp2(y1);
+                S0 += e0; S1 += e1;
+                T0 = fmaf(e0, y0, T0); T1 = fmaf(e1, y1, T1);
             }
-            // a list that is not full (a part shorter than n) takes everything
-            if ((k & (k - 1)) == 0) tau = sh.n_list == n ? lp_value((uint32_t)(sh.list[n - 1] >> 32)) : -INFINITY;
-        }
-        if (ends) {
+        if (nrow != row || item + 1 == i1) {
             // ---- this CTA's part of the row is done
             const long long r0 = (long long)row * a.spr;
             const int c_first = (int)(((r0 + 1) * G - 1) / N), c_last = (int)(((r0 + a.spr) * G - 1) / N), parts = c_last - c_first + 1;
-            float R = lp_max(ref, sh.red[0]);
-            float Sr, Tr;
-            {
-                const float d = ref - R, f = lp_exp2(d);
-                float s0, s1, t0, t1;
-                unpair(S2, s0, s1);
-                unpair(T2, t0, t1);
-                Tr = lp_sum(f * fmaf(s0 + s1, d, t0 + t1), sh.red[1]);
-                Sr = lp_sum(f * (s0 + s1), sh.red[2]);
+            const size_t slot0 = (size_t)row + c_first;
+            if (n > 0) {
+                uint32_t k = lp_order(top);
+                uint32_t *strips = c.strips + ((size_t)row + blockIdx.x) * kLpStrips;
+                if (by_warp) {
+                    k = __reduce_max_sync(0xffffffffu, k);
+                    if ((tid & 31) == 0) strips[tid >> 5] = k;
+                } else strips[tid] = k;
             }
+            float R = lp_max(ref, sh.red[0]);
+            const float dr = ref - R, fr = lp_exp2(dr);
+            float Tr = lp_sum(fr * fmaf(S0 + S1, dr, T0 + T1), sh.red[1]);
+            float Sr = lp_sum(fr * (S0 + S1), sh.red[2]);
             bool finish = parts == 1;
             if (!finish) {
                 LpPart *p = c.parts + row + blockIdx.x;
                 if (tid == 0) { p->m = R; p->s = Sr; p->t = Tr; }
-                if (tid < n) p->top[tid] = tid < sh.n_list ? sh.list[tid] : 0ull;
                 __threadfence();
                 __syncthreads();
                 if (tid == 0) {
                     sh.last = atomicAdd(c.counters + row, 1u) == (uint32_t)(parts - 1);
                     if (sh.last) c.counters[row] = 0u;
-                    sh.n_list = 0;
                 }
                 __syncthreads();
                 finish = sh.last;
                 if (finish) {
                     __threadfence();
-                    const LpPart *p0 = c.parts + row + c_first;
+                    const LpPart *p0 = c.parts + slot0;
                     float mm = -1e30f;
                     for (int i = tid; i < parts; i += kLpThreads) mm = fmaxf(mm, ldcg_f32(&p0[i].m));
                     R = lp_max(mm, sh.red[0]);
@@ -412,21 +310,89 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprobs_kernel(cons
                     }
                     Sr = lp_sum(s, sh.red[1]);
                     Tr = lp_sum(t, sh.red[2]);
-                    if (n > 0) {
-                        const int keys = parts * n;
-                        uint32_t top = 0u;
-                        for (int i = tid; i < keys; i += kLpThreads) top = max(top, (uint32_t)(ldcg_u64(&p0[i / n].top[i % n]) >> 32));
-                        collect(sh, n, top, top, [&](uint32_t bound, auto f) {
-                            for (int i = tid; i < keys; i += kLpThreads) {
-                                const unsigned long long key = ldcg_u64(&p0[i / n].top[i % n]);
-                                if (key && (uint32_t)(key >> 32) >= bound) f(key);
-                            }
-                        });
-                    }
                 }
             }
             if (finish) {
                 const T *p = row_ptr(row);
+                const int off = (int)((reinterpret_cast<uintptr_t>(p) & 15u) / sizeof(T));
+                if (n > 0) {
+                    __syncthreads();                 // (a row of one part: its strips are written)
+                    // strips of the row, numbered part by part
+                    const int PER = by_warp ? kLpWarps : kLpThreads;
+                    const int n_strips = parts * PER;
+                    auto strip_key = [&](int i) -> uint32_t { return ldcg_u32(c.strips + (slot0 + i / PER) * kLpStrips + i % PER); };
+                    uint32_t mx = 0;
+                    for (int i = tid; i < n_strips; i += kLpThreads) mx = max(mx, strip_key(i));
+                    if (tid == 0) { sh.n_strip = 0; sh.n_cand = 0; sh.n_list = 0; sh.bound = 0; }
+                    uint32_t bound = nth_bound(sh, n, mx);
+                    auto take = [&](uint32_t lo) {   // the strips that reach lo
+                        for (int i = tid; i < n_strips; i += kLpThreads) {
+                            const uint32_t k = strip_key(i);
+                            if (k >= lo) {
+                                const int at = atomicAdd(&sh.n_strip, 1);
+                                if (at < kLpStripCap) { sh.strip[at] = i; sh.strip_key[at] = k; }
+                            }
+                        }
+                        __syncthreads();
+                    };
+                    take(bound);
+                    int ns = sh.n_strip;
+                    bool ties = ns > kLpStripCap;    // too many strips hold the bound itself
+                    if (!ties) {
+                        // the n-th largest of their maxima is a closer bound
+                        int above = 0, same = 0;
+                        const uint32_t k = tid < ns ? sh.strip_key[tid] : 0u;
+                        if (tid < ns)
+                            for (int u = 0; u < ns; ++u) { above += sh.strip_key[u] > k; same += sh.strip_key[u] == k; }
+                        if (tid < ns && above < n && above + same >= n) sh.bound = k;
+                        __syncthreads();
+                        bound = max(bound, sh.bound);
+                    } else {
+                        __syncthreads();
+                        if (tid == 0) sh.n_strip = 0;
+                        __syncthreads();
+                        take(bound + 1u);
+                        ns = sh.n_strip;
+                    }
+                    if (ns <= kLpStripCap) {
+                        const uint32_t lo = ties ? bound + 1u : bound;
+                        const int most = (int)((N + G - 1) / G);                 // slices of a part at most
+                        const int vecs = (most < a.spr ? most : a.spr) * NV * (by_warp ? 32 : 1);
+                        for (int i = tid; i < ns * vecs; i += kLpThreads) {
+                            const int q = i / vecs, s = sh.strip[q];
+                            int v = i - q * vecs, t = s % PER;
+                            if (sh.strip_key[q] < lo) continue;
+                            if (by_warp) { t = t * 32 + (v & 31); v >>= 5; }
+                            const long long part = c_first + s / PER;
+                            const long long from = part * N / G - r0, to = (part + 1) * N / G - r0;
+                            const int sl = (int)(from > 0 ? from : 0) + v / NV;
+                            if (sl >= to || sl >= a.spr) continue;
+                            keys_of(p, sl * SLICE + ((v % NV) * kLpThreads + t) * EV - off, [&](unsigned long long key) { if ((uint32_t)(key >> 32) >= lo) push(sh, key); });
+                        }
+                        __syncthreads();
+                        if (ties) {
+                            // the bound's own ids, from the row's beginning, until the list is full
+                            const int have = sh.n_cand;
+                            int width = 32;          // vectors of a step: few at first, they are dense or there would not be so many strips
+                            for (int e = -off; e < V; e += width * EV, width = min(2 * width, kLpThreads)) {
+                                __syncthreads();
+                                if (have >= n || sh.n_cand >= n) break;
+                                __syncthreads();
+                                if (tid < width) keys_of(p, e + tid * EV, [&](unsigned long long key) { if ((uint32_t)(key >> 32) == bound) push(sh, key); });
+                            }
+                            __syncthreads();
+                        }
+                    }
+                    if (ns > kLpStripCap || sh.n_cand > kLpCap) {
+                        // hardly ever: slice by slice, whatever the elements are
+                        __syncthreads();
+                        for (int e = -off; e < V; e += SLICE)
+                            collect(sh, n, [&](auto f) {
+#pragma unroll 1
+                                for (int j = 0; j < NV; ++j) keys_of(p, e + (j * kLpThreads + tid) * EV, f);
+                            });
+                    } else rank(sh, n);
+                }
                 // Rows whose maximum is too far from zero for the sums above (or infinite) are added up anew, against the maximum itself
                 const bool far = !(R > kLpMinRef && R < kLpMaxRef);
                 bool nothing = false;
@@ -466,20 +432,14 @@ __global__ void __launch_bounds__(kLpThreads, kLpCtasPerSm) logprobs_kernel(cons
                     if (c.out_ids) c.out_ids[o] = (int32_t)argmax_key_id(key);
                     if (c.out_tops) c.out_tops[o] = logprob(lp_value((uint32_t)(key >> 32)));
                 }
+                __syncthreads();
             }
-            __syncthreads();
-            if (tid == 0) { sh.n_list = 0; sh.n_cand = 0; }
-            __syncthreads();
             ref = -1e30f;
-            S2 = T2 = 0ull;
-            k = 0;
-            slice0 = nslice;
-            tau = 0.f;
+            S0 = S1 = T0 = T1 = 0.f;
+            top = -INFINITY;
         }
         row = nrow;
         slice = nslice;
-#pragma unroll
-        for (int j = 0; j < NV; ++j) cur[j] = nxt[j];
     }
 }
 
@@ -498,6 +458,9 @@ int logprobs_launch(const LpCall &c, cudaStream_t st) {
     a.spr = per_row(nv);
     a.n_items = (long long)c.rows * a.spr;
     const int grid = (int)(a.n_items < ctas ? a.n_items : ctas);
+    // a few hundred strips per row are enough to leave little to read again, and few enough for one CTA to look through
+    const long long per_part = (a.n_items + grid - 1) / grid;
+    a.warp_strips = (a.spr + per_part - 1) / per_part >= 32;
     void (*kern)(LpArgs);
     if (c.f32) kern = nv == 8 ? logprobs_kernel<true, 8> : nv == 4 ? logprobs_kernel<true, 4> : nv == 2 ? logprobs_kernel<true, 2> : logprobs_kernel<true, 1>;
     else kern = nv == 8 ? logprobs_kernel<false, 8> : nv == 4 ? logprobs_kernel<false, 4> : nv == 2 ? logprobs_kernel<false, 2> : logprobs_kernel<false, 1>;

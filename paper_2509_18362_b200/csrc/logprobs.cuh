@@ -6,11 +6,11 @@ namespace fmtp {
 
 constexpr int kLpMaxRows = 4096;
 constexpr int kLpMaxTop = 32;
+constexpr int kLpStrips = 256;                       // maxima of a part (see logprobs.cu)
 
 // What a CTA knows of its part of a row.
 struct LpPart {
-    float m, s, t, pad;                              // maximum, sum of e^(x - m), sum of e^(x - m) (x - m)
-    unsigned long long top[kLpMaxTop];               // (value, id) keys, best first; 0: none
+    float m, s, t, pad;                              // with y = x log2(e) - m: sum of 2^y, sum of 2^y y
 };
 
 struct LpCall {
@@ -23,6 +23,7 @@ struct LpCall {
     int32_t *out_ids;                                // [rows][top]
     float *out_tops;                                 // [rows][top]
     LpPart *parts;                                   // [logprobs_slots(n_sm)]
+    uint32_t *strips;                                // [logprobs_slots(n_sm)][kLpStrips]
     uint32_t *counters;                              // [kLpMaxRows], zero between calls
     uint32_t *status;
     int n_sm;
