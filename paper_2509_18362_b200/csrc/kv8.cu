@@ -273,11 +273,11 @@ __host__ __device__ __forceinline__ int chunk8(int n_ctx, int pairs) {
     return c;
 }
 
-template <int DH, int WR>
+template <int DH, int RW, int WR>
 struct Attn8Smem {
     static constexpr int WT = kA8Warps / WR;                                 // workers of a CTA
-    static constexpr int S = WT == 4 ? 3 : WT == 2 ? 6 : 8;                  // stages
-    static constexpr int CTAS = DH == 128 ? 2 : 3;                           // resident per SM
+    static constexpr int CTAS = DH == 128 ? (RW == 1 ? 3 : 2) : (RW == 1 ? 4 : 3);       // resident per SM
+    static constexpr int S = WT == 4 ? (CTAS > 2 && DH == 128 ? 2 : 3) : WT == 2 ? (DH == 128 ? 6 : 7) : 8;      // stages
     static constexpr int KV = kA8Blk * DH;                                   // bytes of a stage's K (or V) codes
     static constexpr int STAGE = 2 * KV + 2 * kA8Blk * 4;
     static constexpr int O_TAB = WT * S * STAGE;
@@ -346,10 +346,9 @@ struct Item8 {
 };
 
 template <int DH, int RW, int WR>
-__global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
-    chain_release();
+__global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
     chain_wait();
-    using Lay = Attn8Smem<DH, WR>;
+    using Lay = Attn8Smem<DH, RW, WR>;
     constexpr int WT = Lay::WT, S = Lay::S, KS = DH / 32, ND = DH / 16, TILES = RW * WR;
     extern __shared__ __align__(128) unsigned char smem[];
     int *prefix = reinterpret_cast<int *>(smem + Lay::O_TAB);              // [B + 1] items before a sequence
@@ -422,7 +421,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
         }
         chunk_bounds(it);
     };
-    if (i_begin >= i_end) return;                    // (no thread waits for another worker's from here on)
+    if (i_begin >= i_end) return;                    // (no thread waits for another worker's from here on; an exit releases the successor as well)
 
     // ---- copying. Block-table entries are read a segment ahead (a read queues behind the copies that are on their way, which takes
     // longer than a stage): lane i holds the page of the segment's i-th block. A segment is part of one item: stages whose tokens lie in
@@ -708,6 +707,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
         }
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    chain_release();
 }
 
 // ---- a row's chunks joined in ascending order. Block = (query head, row), a thread per element; a warp's lanes hold the weights of
@@ -762,8 +762,8 @@ __global__ void __launch_bounds__(DH) kv8_merge_kernel(const Attn8Args a) {
 template <int DH, int RW, int WR>
 int attn8_launch(const Attn8Args &a, int rows, int n_sm, cudaStream_t st) {
     auto kern = kv8_attn_kernel<DH, RW, WR>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Attn8Smem<DH, WR>::TOTAL);
-    if (e == cudaSuccess) e = launch_chained(kern, dim3(Attn8Smem<DH, WR>::CTAS * n_sm), dim3(kA8Threads), (size_t)Attn8Smem<DH, WR>::TOTAL, st, a);
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Attn8Smem<DH, RW, WR>::TOTAL);
+    if (e == cudaSuccess) e = launch_chained(kern, dim3(Attn8Smem<DH, RW, WR>::CTAS * n_sm), dim3(kA8Threads), (size_t)Attn8Smem<DH, RW, WR>::TOTAL, st, a);
     if (e == cudaSuccess) e = launch_chained(kv8_merge_kernel<DH>, dim3(a.Hq, rows), dim3(DH), 0, st, a);
     return (int)e;
 }
