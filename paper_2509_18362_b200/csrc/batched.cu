@@ -1202,9 +1202,12 @@ size_t batched_layout(BatchedWs &ws, unsigned char *base, const BatchedShape &sh
     ws.x = reinterpret_cast<float *>(take((size_t)rows * sh.d * 4));
     ws.hout = reinterpret_cast<float *>(take((size_t)rows * sh.d * 4));
     ws.q = reinterpret_cast<bf16_t *>(take((size_t)rows * 2 * qdim * 2));
-    // (attention over 8-bit caches cuts short contexts into more chunks)
-    const int slots8 = kv8_attention_slots(Kv8Shape{sh.Hq, sh.Hkv, sh.dh, sh.page, sh.max_ctx}, 1);
-    ws.part_rows = (size_t)rows * (ws.max_chunks > slots8 ? ws.max_chunks : slots8);
+    // (attention over 8-bit caches: at least as many chunks, and 256 rows of prompts at once)
+    const Kv8Shape s8{sh.Hq, sh.Hkv, sh.dh, sh.page, sh.max_ctx};
+    const int slots1 = kv8_attention_slots(s8, 1);
+    const size_t decode = (size_t)rows * (ws.max_chunks > slots1 ? ws.max_chunks : slots1);
+    const size_t prompt = (size_t)(sh.max_rows < 256 ? sh.max_rows : 256) * kv8_attention_slots(s8, kBatchRows);
+    ws.part_rows = decode > prompt ? decode : prompt;
     ws.att_part = reinterpret_cast<float *>(take(ws.part_rows * sh.Hq * (sh.dh + 2) * 4));
     ws.qkv = reinterpret_cast<bf16_t *>(take((size_t)rows * (qdim + 2 * kvdim) * 2));
     ws.keys_bytes = (size_t)(sh.max_K > 1 ? sh.max_K : 1) * kBatchRows * 8 + 256;

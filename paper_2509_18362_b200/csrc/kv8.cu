@@ -227,8 +227,10 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv8_read_kernel(const Read8Ar
 }
 
 // ---- attention. The (row, query head) pairs that share a KV head of a sequence are dealt to tiles of eight; a work item is one chunk of
-// a sequence's context for one KV head and a set of RW * WR tiles. WR warps, RW tiles each, are a worker; a CTA of four warps holds
-// 4 / WR of them, which have nothing to do with each other: each walks a contiguous range of items with a ring of its own.
+// a sequence's context for one KV head and a set of RW * WR tiles. A CTA of four warps walks a contiguous range of items. Its
+// WT = 4 / WR groups of WR warps take the chunk's 32-token stages in turn, each with a ring of its own, and meet at the chunk's end,
+// where their results are joined in shared memory; a group's warps take RW tiles each. (A warp for an item kept the SMs busy
+// for three quarters of the time: an item of 256 tokens took it 25 us.)
 //
 // Both products run on mma.sync.m16n8k16 with f16 operands (sm_100a has no mma.sync on e4m3: the assembler emulates it with fifteen
 // instructions each). K and V are the A operand, 16 tokens or 16 dims, so that eight pairs fill the n side: S^T = K Q^T, O^T = V^T
@@ -258,12 +260,12 @@ constexpr float kP8Log2 = 14.f;                      // probabilities are held t
 constexpr float kQ8 = 32.f;                          // queries below 448 * 32
 
 // Tokens of a chunk: a function of the sequence's committed length and of the call's rows per sequence, never of the batch. Short
-// enough for a context to keep many workers busy, long enough for the partial results (dh + 2 fp32 values for each pair and chunk,
+// enough for a context to keep many CTAs busy, long enough for the partial results (dh + 2 fp32 values for each pair and chunk,
 // 512 bytes against 256 bytes of K/V per token at dh = 128) to stay a small part of the traffic: up to `few` chunks until a chunk is
 // `base` long, up to `most` chunks of that and more tokens beyond.
 struct Chunk8 { int first, few, base, most; };
 __host__ __device__ __forceinline__ Chunk8 chunk8_rule(int pairs) {
-    return pairs <= 8 ? Chunk8{64, 32, 256, 128} : pairs <= 32 ? Chunk8{128, 16, 512, 64} : Chunk8{256, 8, 512, 32};
+    return pairs <= 8 ? Chunk8{128, 16, 512, 128} : pairs <= 32 ? Chunk8{128, 16, 512, 64} : Chunk8{256, 8, 512, 32};
 }
 __host__ __device__ __forceinline__ int chunk8(int n_ctx, int pairs) {
     const Chunk8 r = chunk8_rule(pairs);
@@ -276,12 +278,14 @@ __host__ __device__ __forceinline__ int chunk8(int n_ctx, int pairs) {
 template <int DH, int RW, int WR>
 struct Attn8Smem {
     static constexpr int WT = kA8Warps / WR;                                 // workers of a CTA
-    static constexpr int CTAS = DH == 128 ? (RW == 1 ? 3 : 2) : (RW == 1 ? 4 : 3);       // resident per SM
-    static constexpr int S = WT == 4 ? (CTAS > 2 && DH == 128 ? 2 : 3) : WT == 2 ? (DH == 128 ? 6 : 7) : 8;      // stages
+    static constexpr int CTAS = DH == 128 ? 3 : 4;                           // resident per SM
+    static constexpr int S = DH == 128 ? 8 / WT : 12 / WT;                   // stages
     static constexpr int KV = kA8Blk * DH;                                   // bytes of a stage's K (or V) codes
     static constexpr int STAGE = 2 * KV + 2 * kA8Blk * 4;
-    static constexpr int O_TAB = WT * S * STAGE;
-    static constexpr int TOTAL = O_TAB + (5 * kBatchRows + 1) * 4;
+    static constexpr int O_ML = WT * S * STAGE;                              // [4 warps][8 pairs] maximum, sum
+    static constexpr int O_LAST = O_ML + kA8Warps * 8 * 8;                   // [WT] the stage that a group read last
+    static constexpr int O_TAB = O_LAST + kA8Warps * 4;
+    static constexpr int TOTAL = O_TAB + (6 * kBatchRows + 2) * 4;
 };
 
 // (Warp-wide instructions are volatile: the compiler may move an asm statement without side effects into a branch that uses its result,
@@ -330,16 +334,16 @@ __device__ __forceinline__ uint32_t piece_at(int t, int c) {
     return (uint32_t)(t * DH + ((DH == 128 ? (c ^ (t & 7)) : (c ^ ((t >> 1) & 3))) << 4));
 }
 
-// Meeting of a worker's warps. Not the aligned form of the barrier, which the compiler does not know to need all lanes of a warp.
+// Meeting of a group's warps. Not the aligned form of the barrier, which the compiler does not know to need all lanes of a warp.
 template <int WR>
-__device__ __forceinline__ void worker_sync(int wt) {
+__device__ __forceinline__ void group_sync(int wt) {
     __syncwarp();
     if constexpr (WR == kA8Warps) __syncthreads();
     else if constexpr (WR > 1) asm volatile("barrier.sync %0, %1;" ::"r"(1 + wt), "n"(WR * 32) : "memory");
     __syncwarp();
 }
 
-// A worker's place in the list of items: sequences, their KV heads, tile sets, chunks (the chunks of one context follow each other).
+// A place in the list of items: sequences, their KV heads, tile sets, chunks (the chunks of one context follow each other).
 struct Item8 {
     int seq, kvh, set, chunk;
     int t0, t1;                                      // the chunk's tokens [t0, t1): never empty, the sequence's last row sees them all
@@ -352,7 +356,8 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
     constexpr int WT = Lay::WT, S = Lay::S, KS = DH / 32, ND = DH / 16, TILES = RW * WR;
     extern __shared__ __align__(128) unsigned char smem[];
     int *prefix = reinterpret_cast<int *>(smem + Lay::O_TAB);              // [B + 1] items before a sequence
-    int *tpos = prefix + kBatchRows + 1;                                   // position of a sequence's row 0
+    int *pcost = prefix + kBatchRows + 1;                                  // [B + 1] their cost: a group's stages, and one for each item
+    int *tpos = pcost + kBatchRows + 1;                                    // position of a sequence's row 0
     int *tval = tpos + kBatchRows;                                         // its rows that count
     int *tchk = tval + kBatchRows;                                         // tokens of its chunks
     int *tnum = tchk + kBatchRows;                                         // chunks, sets << 16
@@ -360,39 +365,56 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
     const int max_tokens = min((int)min((long long)a.kv.max_pages * a.page, (long long)kMaxLen), a.max_ctx);
     const int gq = a.gq;
     auto row_ctx = [&](int pos0, int m) -> int { return min(pos0 + m, max_tokens - 1) + 1; };     // positions that row m sees
+    constexpr int STRIDE = WT * kA8Blk;              // tokens from one stage of a group to its next
     if (warp == 0) {                                 // two sequences per lane
-        int cnt[2];
+        int cnt[2], cost[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
             const int s = 2 * lane + u;
-            cnt[u] = 0;
+            cnt[u] = cost[u] = 0;
             if (s < a.B) {
                 const int len = kv8_len(a.kv, s), nv = kv8_rows(a.n_new, s, a.M);
                 const int c = chunk8(row_ctx(len, a.M - 1), a.M * gq);
                 tpos[s] = len; tval[s] = nv; tchk[s] = c;
+                tnum[s] = 0;
                 if (nv > 0) {
-                    const int chunks = (row_ctx(len, nv - 1) + c - 1) / c, sets = (nv * gq + 8 * TILES - 1) / (8 * TILES);
+                    const int n = row_ctx(len, nv - 1), chunks = (n + c - 1) / c, sets = (nv * gq + 8 * TILES - 1) / (8 * TILES);
                     tnum[s] = chunks | (sets << 16);
                     cnt[u] = chunks * a.Hkv * sets;
+                    cost[u] = (chunks + (n + STRIDE - 1) / STRIDE) * a.Hkv * sets;
                     if (len + nv > max_tokens && blockIdx.x == 0) atomicOr(a.status, kDevBadPos);
                 }
             }
         }
-        int incl = cnt[0] + cnt[1];
+        int incl = cnt[0] + cnt[1], icost = cost[0] + cost[1];
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
-            const int t = __shfl_up_sync(0xffffffffu, incl, o);
-            if (lane >= o) incl += t;
+            const int t = __shfl_up_sync(0xffffffffu, incl, o), tc = __shfl_up_sync(0xffffffffu, icost, o);
+            if (lane >= o) { incl += t; icost += tc; }
         }
-        if (2 * lane <= a.B) prefix[2 * lane] = incl - cnt[0] - cnt[1];
-        if (2 * lane + 1 <= a.B) prefix[2 * lane + 1] = incl - cnt[1];
-        if (lane == 31 && a.B == 2 * 32) prefix[a.B] = incl;
+#pragma unroll
+        for (int u = 0; u < 2; ++u) {
+            const int s = 2 * lane + u;
+            if (s < a.B) {
+                prefix[s + 1] = u ? incl : incl - cnt[1];
+                pcost[s + 1] = u ? icost : icost - cost[1];
+            }
+        }
+        if (lane == 0) prefix[0] = pcost[0] = 0;
     }
     __syncwarp();
     __syncthreads();
-    // workers are numbered across the CTAs first, so that few items lie on as many SMs
-    const int n_items = prefix[a.B], worker = wt * gridDim.x + blockIdx.x, workers = WT * gridDim.x;
-    const int i_begin = (int)(((long long)worker * n_items) / workers), i_end = (int)(((long long)(worker + 1) * n_items) / workers);
+    // CTAs' shares of the list have the same cost up to an item: a CTA begins with the first item that starts at or behind its share
+    const int n_items = prefix[a.B], n_cost = pcost[a.B];
+    auto item_at = [&](long long x) -> int {
+        if (x >= n_cost) return n_items;
+        int s = 0;
+        while (pcost[s + 1] <= x) ++s;
+        const int rem = (int)x - pcost[s], chunks = tnum[s] & 0xffff, contexts = (prefix[s + 1] - prefix[s]) / chunks;
+        const int cost = (pcost[s + 1] - pcost[s]) / contexts, ctx = rem / cost, one = tchk[s] / STRIDE + 1;
+        return prefix[s] + ctx * chunks + min((rem - ctx * cost + one - 1) / one, chunks);
+    };
+    const int i_begin = item_at((long long)blockIdx.x * n_cost / gridDim.x), i_end = item_at((long long)(blockIdx.x + 1) * n_cost / gridDim.x);
     auto chunk_bounds = [&](Item8 &it) {
         const int c = tchk[it.seq];
         it.t0 = it.chunk * c;
@@ -421,7 +443,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
         }
         chunk_bounds(it);
     };
-    if (i_begin >= i_end) return;                    // (no thread waits for another worker's from here on; an exit releases the successor as well)
+    if (i_begin >= i_end) return;                    // (an exit releases the successor as well)
 
     // ---- copying. Block-table entries are read a segment ahead (a read queues behind the copies that are on their way, which takes
     // longer than a stage): lane i holds the page of the segment's i-th block. A segment is part of one item: stages whose tokens lie in
@@ -433,19 +455,23 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
     Item8 li{};
     int litem = i_begin, ltok = 0, cslot = 0;
     auto load_segment = [&](Segment &g) {
+        while (litem < i_end && ltok >= li.t1) {     // (an item may be too short for this group)
+            if (++litem < i_end) {
+                next_item(li);
+                ltok = li.t0 + wt * kA8Blk;
+            }
+        }
         if (litem >= i_end) { g.tok = g.end = 0; return; }
         g.tok = ltok;
         g.t1 = li.t1;
         g.kvh = li.kvh;
         g.blk = page_of(ltok, a.page, a.shift);
-        g.end = ltok + (int)min((((long long)g.blk + 32) * a.page - ltok) & ~(long long)(kA8Blk - 1), (long long)(li.t1 - ltok + kA8Blk - 1) & ~(long long)(kA8Blk - 1));
+        // stages whose tokens lie in the 32 blocks (the first one does) and in the chunk
+        const long long room = ((long long)g.blk + 32) * a.page - ltok - kA8Blk;
+        g.end = ltok + min((int)min(room / STRIDE, 1ll << 20) + 1, (li.t1 - ltok + STRIDE - 1) / STRIDE) * STRIDE;
         const int blk = min(g.blk + lane, page_of(li.t1 - 1, a.page, a.shift));
         g.page = a.kv.block_table[(size_t)li.seq * a.kv.max_pages + blk];
         ltok = g.end;
-        if (ltok >= li.t1 && ++litem < i_end) {
-            next_item(li);
-            ltok = li.t0;
-        }
     };
     auto copy_stage = [&]() {
         if (cur.tok < cur.end) {
@@ -471,7 +497,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                 cp_async4(sb + 2 * Lay::KV + kA8Blk * 4 + lane * 4, a.kv.v_scales + slot, n);
             }
             if (++cslot == S) cslot = 0;
-            cur.tok += kA8Blk;
+            cur.tok += STRIDE;
             if (cur.tok >= cur.end) {
                 cur = nxt;
                 load_segment(nxt);
@@ -481,7 +507,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
     };
     first_item(li);
     Item8 it = li;
-    ltok = li.t0;
+    ltok = li.t0 + wt * kA8Blk;
     load_segment(cur);
     load_segment(nxt);
 #pragma unroll 1
@@ -497,7 +523,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
     int pn[RW][2], prow[RW][2];                      // positions that a pair sees, its row (no such pair: any, the sequence's number of rows)
     size_t pout[RW][2];                              // where its partial results go
     bool fresh = true;
-    int slot = 0, nv = 0;
+    int slot = 0, last_slot = 0, nv = 0;
     for (int item = i_begin; item < i_end; ++item) {
         if (fresh) {                                 // the queries stay in registers while the items are chunks of one context
             nv = tval[it.seq];
@@ -553,11 +579,12 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
             for (int i = 0; i < ND; ++i) o[r][i][0] = o[r][i][1] = o[r][i][2] = o[r][i][3] = 0.f;
         }
 #pragma unroll 1
-        for (int tb = it.t0; tb < it.t1; tb += kA8Blk) {
+        for (int tb = it.t0 + wt * kA8Blk; tb < it.t1; tb += STRIDE) {
             asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
-            worker_sync<WR>(wt);
+            group_sync<WR>(wt);
             copy_stage();                            // into the stage that was read last
             const uint32_t sb = smem_u32(ring + (size_t)slot * Lay::STAGE);
+            last_slot = slot;
             if (++slot == S) slot = 0;
             // ---- scores: tokens 16 h + g, 16 h + 8 + g of pairs kq, kq + 1
             float sc[RW][2][4];
@@ -685,20 +712,72 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
             }
         }
         // ---- the chunk's partial result: o and the sum relative to the maximum, the maximum (log2 units)
+        const int groups = min(WT, (it.t1 - it.t0 + kA8Blk - 1) / kA8Blk);       // the others had none of the chunk's stages
 #pragma unroll
-        for (int r = 0; r < RW; ++r)
+        for (int r = 0; r < RW; ++r) {
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                float l = l_run[r][e];
 #pragma unroll
-                for (int x = 4; x < 32; x <<= 1) l += __shfl_xor_sync(0xffffffffu, l, x);
-                if (prow[r][e] < nv && pn[r][e] > it.t0) {       // such a pair, and it sees something of the chunk
-                    float *out = a.part + pout[r][e] + (size_t)it.chunk * (DH + 2);
-#pragma unroll
-                    for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(out + c * 16 + g * 2) = make_float2(o[r][c][e] * sv_run, o[r][c][2 + e] * sv_run);
-                    if (g == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(m_run[r][e] * fs[r][e], l);
-                }
+                for (int x = 4; x < 32; x <<= 1) l_run[r][e] += __shfl_xor_sync(0xffffffffu, l_run[r][e], x);
             }
+            if (WT == 1 || groups == 1) {
+                if (wt == 0) {
+#pragma unroll
+                    for (int e = 0; e < 2; ++e)
+                        if (prow[r][e] < nv && pn[r][e] > it.t0) {       // such a pair, and it sees something of the chunk
+                            float *out = a.part + pout[r][e] + (size_t)it.chunk * (DH + 2);
+#pragma unroll
+                            for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(out + c * 16 + g * 2) = make_float2(o[r][c][e] * sv_run, o[r][c][2 + e] * sv_run);
+                            if (g == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(m_run[r][e] * fs[r][e], l_run[r][e]);
+                        }
+                }
+            } else {
+                // Each warp leaves a tile's result in the stage that its group read last (free until the group's next copy), and the
+                // threads of the tile's WT warps add them up in the groups' order: an eighth of a pair's dims at a time
+                constexpr int LD = DH + 4;           // (rows of pairs start in different banks)
+                static_assert(WT == 1 || 8 * LD * 4 * WR <= Lay::STAGE, "a tile of each warp fits the stage");
+                float2 *ml = reinterpret_cast<float2 *>(smem + Lay::O_ML);
+                int *last = reinterpret_cast<int *>(smem + Lay::O_LAST);
+                if (r == 0) group_sync<WR>(wt);     // all readers of the stage are done
+                if (wt < groups) {
+                    float *mine = reinterpret_cast<float *>(ring + (size_t)last_slot * Lay::STAGE) + wr * 8 * LD;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(mine + (kq + e) * LD + c * 16 + g * 2) = make_float2(o[r][c][e] * sv_run, o[r][c][2 + e] * sv_run);
+                        if (g == 0) ml[warp * 8 + kq + e] = make_float2(m_run[r][e] * fs[r][e], l_run[r][e]);
+                    }
+                    if (lane == 0 && wr == 0) last[wt] = last_slot;
+                }
+                __syncthreads();
+                // this warp's pairs of tile (wr, r): two for WT = 4, four for WT = 2; a pair's lanes take four dims each
+                constexpr int LPP = DH / 4, PPW = 8 / WT;        // lanes per pair, pairs per warp
+#pragma unroll
+                for (int q0 = 0; q0 < PPW; q0 += 32 / LPP) {
+                    const int q = wt * PPW + q0 + lane / LPP, d = lane % LPP * 4, pair = ((it.set * WR + wr) * RW + r) * 8 + q;
+                    float mm = -INFINITY;
+                    for (int x = 0; x < groups; ++x) mm = fmaxf(mm, ml[(x * WR + wr) * 8 + q].x);
+                    const float mu = mm == -INFINITY ? 0.f : mm;
+                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                    float l = 0.f;
+                    for (int x = 0; x < groups; ++x) {
+                        const float2 y = ml[(x * WR + wr) * 8 + q];
+                        const float f = exp2_approx(y.x - mu);
+                        const float4 v = *reinterpret_cast<const float4 *>(smem + (size_t)(x * S + last[x]) * Lay::STAGE + ((wr * 8 + q) * LD + d) * 4);
+                        acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
+                        l += y.y * f;
+                    }
+                    const int m = pair / gq;
+                    if (pair < nv * gq && row_ctx(tpos[it.seq], m) > it.t0) {
+                        float *out = a.part + (((size_t)(it.seq * a.M + m) * a.Hq + it.kvh * gq + (pair - m * gq)) * a.slots + it.chunk) * (DH + 2);
+                        *reinterpret_cast<float2 *>(out + d) = make_float2(acc.x, acc.y);
+                        *reinterpret_cast<float2 *>(out + d + 2) = make_float2(acc.z, acc.w);
+                        if (d == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(mm, l);
+                    }
+                }
+                __syncthreads();
+            }
+        }
         __syncwarp();
         if (item + 1 < i_end) {
             const int seq = it.seq, kvh = it.kvh, set = it.set;
@@ -772,10 +851,9 @@ template <int DH>
 int attn8_pick(const Attn8Args &a, int rows, int n_sm, cudaStream_t st) {
     const int pairs = a.M * a.gq;
     if (pairs <= 8) return attn8_launch<DH, 1, 1>(a, rows, n_sm, st);
-    if (pairs <= 16) return attn8_launch<DH, 2, 1>(a, rows, n_sm, st);
-    if (pairs <= 32) return attn8_launch<DH, 2, 2>(a, rows, n_sm, st);
-    if constexpr (DH == 64) return attn8_launch<DH, 2, 2>(a, rows, n_sm, st);
-    else return attn8_launch<DH, 2, 4>(a, rows, n_sm, st);
+    if (DH == 64 || pairs <= 16) return attn8_launch<DH, 1, 2>(a, rows, n_sm, st);
+    if constexpr (DH == 128) return attn8_launch<DH, 1, 4>(a, rows, n_sm, st);
+    return (int)cudaErrorInvalidConfiguration;
 }
 
 }  // namespace
