@@ -1202,12 +1202,14 @@ size_t batched_layout(BatchedWs &ws, unsigned char *base, const BatchedShape &sh
     ws.x = reinterpret_cast<float *>(take((size_t)rows * sh.d * 4));
     ws.hout = reinterpret_cast<float *>(take((size_t)rows * sh.d * 4));
     ws.q = reinterpret_cast<bf16_t *>(take((size_t)rows * 2 * qdim * 2));
-    // (attention over 8-bit caches: at least as many chunks, and 256 rows of prompts at once)
+    // (attention over 8-bit caches: room for 64 rows of decoding, or 256 of scoring or prompts, in one launch)
     const Kv8Shape s8{sh.Hq, sh.Hkv, sh.dh, sh.page, sh.max_ctx};
-    const int slots1 = kv8_attention_slots(s8, 1);
-    const size_t decode = (size_t)rows * (ws.max_chunks > slots1 ? ws.max_chunks : slots1);
-    const size_t prompt = (size_t)(sh.max_rows < 256 ? sh.max_rows : 256) * kv8_attention_slots(s8, kBatchRows);
-    ws.part_rows = decode > prompt ? decode : prompt;
+    ws.part_rows = (size_t)rows * ws.max_chunks;
+    for (int m : {1, 2, 4, 8, kBatchRows}) {
+        const int r = m == 1 ? rows : sh.max_rows < 256 ? sh.max_rows : 256;
+        const size_t need = (size_t)r * kv8_attention_slots(s8, m);
+        if (need > ws.part_rows) ws.part_rows = need;
+    }
     ws.att_part = reinterpret_cast<float *>(take(ws.part_rows * sh.Hq * (sh.dh + 2) * 4));
     ws.qkv = reinterpret_cast<bf16_t *>(take((size_t)rows * (qdim + 2 * kvdim) * 2));
     ws.keys_bytes = (size_t)(sh.max_K > 1 ? sh.max_K : 1) * kBatchRows * 8 + 256;

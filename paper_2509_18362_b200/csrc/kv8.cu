@@ -227,23 +227,26 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv8_read_kernel(const Read8Ar
 }
 
 // ---- attention. The (row, query head) pairs that share a KV head of a sequence are dealt to tiles of eight; a work item is one chunk of
-// a sequence's context for one KV head and a set of RW * WR tiles. A CTA of four warps walks a contiguous range of items. Its
+// a sequence's context for one KV head and a set of WR tiles. A CTA of four warps walks a contiguous range of items. Its
 // WT = 4 / WR groups of WR warps take the chunk's 32-token stages in turn, each with a ring of its own, and meet at the chunk's end,
-// where their results are joined in shared memory; a group's warps take RW tiles each. (A warp for an item kept the SMs busy
+// where their results are joined in shared memory; a group's warps take a tile each. (A warp for an item kept the SMs busy
 // for three quarters of the time: an item of 256 tokens took it 25 us.)
 //
 // Both products run on mma.sync.m16n8k16 with f16 operands (sm_100a has no mma.sync on e4m3: the assembler emulates it with fifteen
 // instructions each). K and V are the A operand, 16 tokens or 16 dims, so that eight pairs fill the n side: S^T = K Q^T, O^T = V^T
 // P^T. An e4m3 code is exact in f16, a bf16 query (over a power of two, eight bits) as well; a probability is rounded to 2^-12 of
-// itself or 2^-39 of the chunk's largest. A word of K is four dims of a token, and the contraction takes them in the order in which a
+// itself or 2^-31 of the chunk's largest at least. A word of K is four dims of a token, and the contraction takes them in the order in which a
 // lane holds them. V's transposed 16-bit ldmatrix gives dims 2u, 2u + 1 of two tokens in a word, which a byte permutation sorts;
 // movmatrix turns a tile of probabilities from the first product's layout into the second one's.
 //
-// Scores are scaled by the token's K scale, probabilities by its V scale over the largest seen so far (O carries both factors).
+// Scores are scaled by the token's K scale, probabilities by its V scale over the largest seen so far (O carries the factor). The
+// reference of the exponentials is the maximum of a group's first stage and is moved only when a score lies 2^9 above it, so most
+// stages need neither the maximum over all lanes nor a rescaling (partial results carry their reference).
 // A stage of the ring is 32 tokens of K and V with their scales, copied by the warps that read them (16-byte cp.async, any page
 // size).
 struct Attn8Args {
     int Hq, Hkv, gq, page, shift, max_ctx, slots, B, M;       // slots: chunks of a context that `part` has room for
+    int tiles16;                                     // blocks are whole 16-token tiles
     const bf16_t *q;
     long long ldq;
     const int32_t *n_new;
@@ -256,7 +259,8 @@ struct Attn8Args {
 
 constexpr int kA8Warps = 4, kA8Threads = kA8Warps * 32;
 constexpr int kA8Blk = 32;                           // tokens of a stage
-constexpr float kP8Log2 = 14.f;                      // probabilities are held times 2^14: f16 reaches from 2^16 down to 2^-24
+constexpr float kP8Log2 = 6.f;                       // probabilities relative to the reference are held times 2^6: f16 reaches down to 2^-24,
+constexpr float kP8Max = 15.f;                       // and the reference is moved when one comes out above 2^15
 constexpr float kQ8 = 32.f;                          // queries below 448 * 32
 
 // Tokens of a chunk: a function of the sequence's committed length and of the call's rows per sequence, never of the batch. Short
@@ -275,7 +279,7 @@ __host__ __device__ __forceinline__ int chunk8(int n_ctx, int pairs) {
     return c;
 }
 
-template <int DH, int RW, int WR>
+template <int DH, int WR>
 struct Attn8Smem {
     static constexpr int WT = kA8Warps / WR;                                 // workers of a CTA
     static constexpr int CTAS = DH == 128 ? 3 : 4;                           // resident per SM
@@ -338,8 +342,7 @@ __device__ __forceinline__ uint32_t piece_at(int t, int c) {
 template <int WR>
 __device__ __forceinline__ void group_sync(int wt) {
     __syncwarp();
-    if constexpr (WR == kA8Warps) __syncthreads();
-    else if constexpr (WR > 1) asm volatile("barrier.sync %0, %1;" ::"r"(1 + wt), "n"(WR * 32) : "memory");
+    if constexpr (WR > 1) asm volatile("barrier.sync %0, %1;" ::"r"(1 + wt), "n"(WR * 32) : "memory");
     __syncwarp();
 }
 
@@ -349,11 +352,11 @@ struct Item8 {
     int t0, t1;                                      // the chunk's tokens [t0, t1): never empty, the sequence's last row sees them all
 };
 
-template <int DH, int RW, int WR>
-__global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
+template <int DH, int WR>
+__global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
     chain_wait();
-    using Lay = Attn8Smem<DH, RW, WR>;
-    constexpr int WT = Lay::WT, S = Lay::S, KS = DH / 32, ND = DH / 16, TILES = RW * WR;
+    using Lay = Attn8Smem<DH, WR>;
+    constexpr int WT = Lay::WT, S = Lay::S, KS = DH / 32, ND = DH / 16;
     extern __shared__ __align__(128) unsigned char smem[];
     int *prefix = reinterpret_cast<int *>(smem + Lay::O_TAB);              // [B + 1] items before a sequence
     int *pcost = prefix + kBatchRows + 1;                                  // [B + 1] their cost: a group's stages, and one for each item
@@ -378,7 +381,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                 tpos[s] = len; tval[s] = nv; tchk[s] = c;
                 tnum[s] = 0;
                 if (nv > 0) {
-                    const int n = row_ctx(len, nv - 1), chunks = (n + c - 1) / c, sets = (nv * gq + 8 * TILES - 1) / (8 * TILES);
+                    const int n = row_ctx(len, nv - 1), chunks = (n + c - 1) / c, sets = (nv * gq + 8 * WR - 1) / (8 * WR);
                     tnum[s] = chunks | (sets << 16);
                     cnt[u] = chunks * a.Hkv * sets;
                     cost[u] = (chunks + (n + STRIDE - 1) / STRIDE) * a.Hkv * sets;
@@ -481,15 +484,31 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
             const uint32_t sb = smem_u32(ring + (size_t)cslot * Lay::STAGE);
             const uint32_t slot = (uint32_t)page * (uint32_t)a.Hkv + (uint32_t)cur.kvh;
             const uint32_t row = slot * (uint32_t)a.page + (uint32_t)(pos - blk * a.page);
-            constexpr int LPR = DH / 16, RPI = 32 / LPR;
+            constexpr int LPR = DH / 16, RPI = 32 / LPR;         // lanes per token, tokens per step of a warp
             const int piece = lane % LPR, sub = lane / LPR;
+            if (a.tiles16 && cur.tok + kA8Blk <= cur.t1) {
+                // whole tiles of 16 tokens, which lie together: two addresses for K and two for V
+                const size_t at0 = (size_t)__shfl_sync(0xffffffffu, row, 0) * DH + lane * 16 + wr * 512, at1 = (size_t)__shfl_sync(0xffffffffu, row, 16) * DH + lane * 16 + wr * 512;
+                const uint32_t d0 = sb + piece_at<DH>(wr * RPI + sub, piece);
 #pragma unroll
-            for (int u = 0; u < kA8Blk / RPI / WR; ++u) {
-                const int t = (u * WR + wr) * RPI + sub;
-                const size_t off = (size_t)__shfl_sync(0xffffffffu, row, t) * DH + piece * 16;
-                const uint32_t d = sb + piece_at<DH>(t, piece), n = cur.tok + t < cur.t1 ? 16u : 0u;      // zeros beyond what is seen
-                cp_async16_off_hint<0>(d, a.kv.k_pages + off, n, policy);
-                cp_async16_off_hint<0>(d + Lay::KV, a.kv.v_pages + off, n, policy);
+                for (int u = 0; u < kA8Blk / RPI / WR; ++u) {
+                    constexpr int TILE = 16 * DH;
+                    const int byte = u * WR * 512;               // 32 lanes x 16 bytes for each of the group's warps
+                    // (at dh = 128 every other step of four tokens has the pieces' third bit the other way round)
+                    const uint32_t d = (DH == 128 && (u * WR & 1) ? d0 ^ 64u : d0) + byte;
+                    const size_t at = (byte < TILE ? at0 : at1) + byte % TILE;
+                    cp_async16_full_hint<0>(d, a.kv.k_pages + at, policy);
+                    cp_async16_full_hint<0>(d + Lay::KV, a.kv.v_pages + at, policy);
+                }
+            } else {
+#pragma unroll
+                for (int u = 0; u < kA8Blk / RPI / WR; ++u) {
+                    const int t = (u * WR + wr) * RPI + sub;
+                    const size_t off = (size_t)__shfl_sync(0xffffffffu, row, t) * DH + piece * 16;
+                    const uint32_t d = sb + piece_at<DH>(t, piece), n = cur.tok + t < cur.t1 ? 16u : 0u;      // zeros beyond what is seen
+                    cp_async16_off_hint<0>(d, a.kv.k_pages + off, n, policy);
+                    cp_async16_off_hint<0>(d + Lay::KV, a.kv.v_pages + off, n, policy);
+                }
             }
             if (wr == 0) {
                 const uint32_t n = cur.tok + lane < cur.t1 ? 4u : 0u;
@@ -518,68 +537,61 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
     const float sm_scale = (1.0f / sqrtf((float)DH)) * 1.4426950408889634f;
     // ldmatrix rows: K: tokens 0-7 and 8-15 of one piece, then of the next; V: four groups of eight tokens of one piece
     const int ktok = lane & 15, kpc = lane >> 4;
-    uint32_t qb[RW][2 * KS][2];
-    float fs[RW][2];                                 // a query element times a key code times the K scale -> log2 units
-    int pn[RW][2], prow[RW][2];                      // positions that a pair sees, its row (no such pair: any, the sequence's number of rows)
-    size_t pout[RW][2];                              // where its partial results go
+    uint32_t qb[2 * KS][2];
+    float fs[2];                                     // a query element times a key code times the K scale -> log2 units
+    int pn[2], prow[2];                              // positions that a pair sees, its row (no such pair: any, the sequence's number of rows)
+    size_t pout[2];                                  // where its partial results go
     bool fresh = true;
     int slot = 0, last_slot = 0, nv = 0;
     for (int item = i_begin; item < i_end; ++item) {
         if (fresh) {                                 // the queries stay in registers while the items are chunks of one context
             nv = tval[it.seq];
+            const int pair0 = (it.set * WR + wr) * 8;
+            auto pair_at = [&](int pair, int &m, int &row, int &head) -> bool {
+                const bool there = pair < nv * gq;
+                m = there ? pair / gq : 0;
+                row = it.seq * a.M + m;
+                head = it.kvh * gq + (there ? pair - m * gq : 0);
+                return there;
+            };
+            int m, row, head;
+            pair_at(pair0 + g, m, row, head);
+            const bf16_t *qp = a.q + (long long)row * a.ldq + (long long)head * DH;
+            uint2 x[2 * KS];
+            uint32_t am = 0;
 #pragma unroll
-            for (int r = 0; r < RW; ++r) {
-                const int pair0 = (it.set * TILES + wr * RW + r) * 8;
-                auto pair_at = [&](int pair, int &m, int &row, int &head) -> bool {
-                    const bool there = pair < nv * gq;
-                    m = there ? pair / gq : 0;
-                    row = it.seq * a.M + m;
-                    head = it.kvh * gq + (there ? pair - m * gq : 0);
-                    return there;
-                };
-                int m, row, head;
-                pair_at(pair0 + g, m, row, head);
-                const bf16_t *qp = a.q + (long long)row * a.ldq + (long long)head * DH;
-                uint2 x[2 * KS];
-                uint32_t am = 0;
+            for (int j = 0; j < 2 * KS; ++j) {
+                x[j] = *reinterpret_cast<const uint2 *>(qp + j * 16 + kq * 2);
+                am = finite_max(finite_max(am, x[j].x), x[j].y);
+            }
+            am = max(am & 0xffffu, am >> 16);
+            am = max(am, __shfl_xor_sync(0xffffffffu, am, 1));
+            am = max(am, __shfl_xor_sync(0xffffffffu, am, 2));
+            const float qs = scale_for(am), inv = kQ8 / qs;
 #pragma unroll
-                for (int j = 0; j < 2 * KS; ++j) {
-                    x[j] = *reinterpret_cast<const uint2 *>(qp + j * 16 + kq * 2);
-                    am = finite_max(finite_max(am, x[j].x), x[j].y);
-                }
-                am = max(am & 0xffffu, am >> 16);
-                am = max(am, __shfl_xor_sync(0xffffffffu, am, 1));
-                am = max(am, __shfl_xor_sync(0xffffffffu, am, 2));
-                const float qs = scale_for(am), inv = kQ8 / qs;
+            for (int j = 0; j < 2 * KS; ++j) {       // (a query that is not finite becomes NaN)
+                float y[4] = {bf16lo_f32(x[j].x), bf16hi_f32(x[j].x), bf16lo_f32(x[j].y), bf16hi_f32(x[j].y)};
 #pragma unroll
-                for (int j = 0; j < 2 * KS; ++j) {   // (an infinite query becomes an infinite f16 and its scores NaN or infinite: NaN)
-                    float y[4] = {bf16lo_f32(x[j].x), bf16hi_f32(x[j].x), bf16lo_f32(x[j].y), bf16hi_f32(x[j].y)};
+                for (int i = 0; i < 4; ++i) y[i] = fabsf(y[i]) < INFINITY ? y[i] * inv : __uint_as_float(0x7fffffffu);
+                qb[j][0] = pack_f16x2(y[0], y[1]);
+                qb[j][1] = pack_f16x2(y[2], y[3]);
+            }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) y[i] = fabsf(y[i]) < INFINITY ? y[i] * inv : __uint_as_float(0x7fffffffu);
-                    qb[r][j][0] = pack_f16x2(y[0], y[1]);
-                    qb[r][j][1] = pack_f16x2(y[2], y[3]);
-                }
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    fs[r][e] = __shfl_sync(0xffffffffu, qs, (kq + e) * 4) * (sm_scale / kQ8);
-                    const bool there = pair_at(pair0 + kq + e, m, row, head);
-                    prow[r][e] = there ? m : nv;
-                    pn[r][e] = there ? row_ctx(tpos[it.seq], m) : kMaxLen;
-                    pout[r][e] = ((size_t)row * a.Hq + head) * a.slots * (DH + 2);
-                }
+            for (int e = 0; e < 2; ++e) {
+                fs[e] = __shfl_sync(0xffffffffu, qs, (kq + e) * 4) * (sm_scale / kQ8);
+                const bool there = pair_at(pair0 + kq + e, m, row, head);
+                prow[e] = there ? m : nv;
+                pn[e] = there ? row_ctx(tpos[it.seq], m) : kMaxLen;
+                pout[e] = ((size_t)row * a.Hq + head) * a.slots * (DH + 2);
             }
         }
-        float m_run[RW][2], l_run[RW][2], o[RW][ND][4];      // m: of scores not yet times fs
-        float sv_run = 0.f;                          // largest V scale so far
+        float mo[2] = {kP8Log2, kP8Log2}, l_run[2] = {0.f, 0.f}, o[ND][4];       // a score's exponent: fma(score, fs, mo)
+        float sv_run = 0.f, sv_inv = 0.f;            // largest V scale so far, its inverse
 #pragma unroll
-        for (int r = 0; r < RW; ++r) {
-            m_run[r][0] = m_run[r][1] = -INFINITY;
-            l_run[r][0] = l_run[r][1] = 0.f;
-#pragma unroll
-            for (int i = 0; i < ND; ++i) o[r][i][0] = o[r][i][1] = o[r][i][2] = o[r][i][3] = 0.f;
-        }
+        for (int i = 0; i < ND; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+        const int tb0 = it.t0 + wt * kA8Blk;
 #pragma unroll 1
-        for (int tb = it.t0 + wt * kA8Blk; tb < it.t1; tb += STRIDE) {
+        for (int tb = tb0; tb < it.t1; tb += STRIDE) {
             asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
             group_sync<WR>(wt);
             copy_stage();                            // into the stage that was read last
@@ -587,88 +599,95 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
             last_slot = slot;
             if (++slot == S) slot = 0;
             // ---- scores: tokens 16 h + g, 16 h + 8 + g of pairs kq, kq + 1
-            float sc[RW][2][4];
+            float y[2][4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int h = 0; h < 2; ++h) y[h][0] = y[h][1] = y[h][2] = y[h][3] = 0.f;
 #pragma unroll
-                for (int r = 0; r < RW; ++r) sc[r][h][0] = sc[r][h][1] = sc[r][h][2] = sc[r][h][3] = 0.f;
+            for (int ks = 0; ks < KS; ++ks) {        // 32 dims
+                uint32_t kf[2][4];
 #pragma unroll
-                for (int ks = 0; ks < KS; ++ks) {    // 32 dims
-                    uint32_t kf[4];
-                    ldsm4(sb + piece_at<DH>(h * 16 + ktok, 2 * ks + kpc), kf);
+                for (int h = 0; h < 2; ++h) ldsm4(sb + piece_at<DH>(h * 16 + ktok, 2 * ks + kpc), kf[h]);
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const uint32_t a0 = e4m3lo_f16x2(kf[2 * u]), a2 = e4m3hi_f16x2(kf[2 * u]), a1 = e4m3lo_f16x2(kf[2 * u + 1]), a3 = e4m3hi_f16x2(kf[2 * u + 1]);
+                for (int u = 0; u < 2; ++u)
 #pragma unroll
-                        for (int r = 0; r < RW; ++r) mma_f16(sc[r][h], a0, a1, a2, a3, qb[r][2 * ks + u][0], qb[r][2 * ks + u][1]);
-                    }
-                }
+                    for (int h = 0; h < 2; ++h)
+                        mma_f16(y[h], e4m3lo_f16x2(kf[h][2 * u]), e4m3lo_f16x2(kf[h][2 * u + 1]), e4m3hi_f16x2(kf[h][2 * u]), e4m3hi_f16x2(kf[h][2 * u + 1]),
+                                qb[2 * ks + u][0], qb[2 * ks + u][1]);
             }
-            // ---- scales of the lane's tokens; V's over the largest seen so far
-            float sv[2][2], sv_new = sv_run;
+            // ---- exponents; V scales of the lane's tokens
+            float sv[2][2];
 #pragma unroll
             for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int e = 0; e < 2; ++e) {
-                    const uint32_t at = sb + 2 * Lay::KV + (h * 16 + e * 8 + g) * 4;
+                for (int u = 0; u < 2; ++u) {
+                    const uint32_t at = sb + 2 * Lay::KV + (h * 16 + u * 8 + g) * 4;
                     const float sk = lds32f(at);
-                    sv[h][e] = lds32f(at + kA8Blk * 4);
-                    sv_new = fmaxf(sv_new, sv[h][e]);
-#pragma unroll
-                    for (int r = 0; r < RW; ++r) {
-                        sc[r][h][2 * e] *= sk;
-                        sc[r][h][2 * e + 1] *= sk;
-                    }
+                    sv[h][u] = lds32f(at + kA8Blk * 4);
+                    y[h][2 * u] = fmaf(y[h][2 * u] * sk, fs[0], mo[0]);
+                    y[h][2 * u + 1] = fmaf(y[h][2 * u + 1] * sk, fs[1], mo[1]);
                 }
+            const bool edge = __any_sync(0xffffffffu, min(pn[0], pn[1]) - tb < kA8Blk);
+            if (edge) {
 #pragma unroll
-            for (int x = 4; x < 32; x <<= 1) sv_new = fmaxf(sv_new, __shfl_xor_sync(0xffffffffu, sv_new, x));
-            const float sv_inv = sv_new > 0.f ? __fdividef(1.0f, sv_new) : 0.f, sv_corr = sv_new == sv_run ? 1.0f : sv_run * sv_inv;
-            sv_run = sv_new;
-            // ---- probabilities
-            uint32_t pb[RW][2][2];
-            bool edge = false;
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int r = 0; r < RW; ++r) {
-                if (__any_sync(0xffffffffu, min(pn[r][0], pn[r][1]) - tb < kA8Blk)) {
-                    edge = true;
+                    for (int i = 0; i < 4; ++i)
+                        if (tb + h * 16 + (i >> 1) * 8 + g >= pn[i & 1]) y[h][i] = -INFINITY;
+            }
+            float ym[2];
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i)
-                            if (tb + h * 16 + (i >> 1) * 8 + g >= pn[r][i & 1]) sc[r][h][i] = -INFINITY;
-                }
-                float corr[2], mo[2];
-                bool grown = false;
+            for (int e = 0; e < 2; ++e) ym[e] = fmaxf(fmaxf(y[0][e], y[0][2 + e]), fmaxf(y[1][e], y[1][2 + e]));
+            float svm = fmaxf(fmaxf(sv[0][0], sv[0][1]), fmaxf(sv[1][0], sv[1][1]));
+            if (tb == tb0 || __any_sync(0xffffffffu, fmaxf(ym[0], ym[1]) > kP8Max || svm > sv_run)) {
+                // new references: the stage's maximum where it is the first or far above, the largest V scale
+                float corr[2];
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-                    float mx = fmaxf(fmaxf(sc[r][0][e], sc[r][0][2 + e]), fmaxf(sc[r][1][e], sc[r][1][2 + e]));
 #pragma unroll
-                    for (int x = 4; x < 32; x <<= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, x));
-                    const float m_new = fmaxf(m_run[r][e], mx);
-                    const float m_use = m_new == -INFINITY ? 0.f : m_new;        // nothing seen yet: every probability is 2^-inf
-                    corr[e] = exp2_approx((m_run[r][e] - m_use) * fs[r][e]);
-                    grown |= m_run[r][e] > -INFINITY && corr[e] * sv_corr != 1.0f;
-                    m_run[r][e] = m_new;
-                    mo[e] = kP8Log2 - m_use * fs[r][e];
-                    l_run[r][e] *= corr[e];
+                    for (int x = 4; x < 32; x <<= 1) ym[e] = fmaxf(ym[e], __shfl_xor_sync(0xffffffffu, ym[e], x));
+                    const float d = (tb == tb0 || ym[e] > kP8Max) && ym[e] > -INFINITY ? ym[e] - kP8Log2 : 0.f;
+                    mo[e] -= d;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) { y[h][e] -= d; y[h][2 + e] -= d; }
+                    corr[e] = tb == tb0 ? 1.f : exp2_approx(-d);
+                    l_run[e] *= corr[e];
                 }
+#pragma unroll
+                for (int x = 4; x < 32; x <<= 1) svm = fmaxf(svm, __shfl_xor_sync(0xffffffffu, svm, x));
+                if (svm > sv_run) {
+                    sv_inv = __fdividef(1.0f, svm);
+                    corr[0] *= sv_run * sv_inv;
+                    corr[1] *= sv_run * sv_inv;
+                    sv_run = svm;
+                }
+                if (tb != tb0) {
+#pragma unroll
+                    for (int i = 0; i < ND; ++i) { o[i][0] *= corr[0]; o[i][1] *= corr[1]; o[i][2] *= corr[0]; o[i][3] *= corr[1]; }
+                }
+            }
+            // ---- probabilities
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) y[h][i] = exp2_approx(y[h][i]);
+            l_run[0] += (y[0][0] + y[0][2]) + (y[1][0] + y[1][2]);
+            l_run[1] += (y[0][1] + y[0][3]) + (y[1][1] + y[1][3]);
+            if (!__all_sync(0xffffffffu, sv[0][0] == sv_run && sv[0][1] == sv_run && sv[1][0] == sv_run && sv[1][1] == sv_run)) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
                     for (int u = 0; u < 2; ++u) {
-                        const float p0 = exp2_approx(fmaf(sc[r][h][2 * u], fs[r][0], mo[0])), p1 = exp2_approx(fmaf(sc[r][h][2 * u + 1], fs[r][1], mo[1]));
-                        l_run[r][0] += p0;
-                        l_run[r][1] += p1;
                         const float f = sv[h][u] * sv_inv;
-                        pb[r][h][u] = movmatrix_trans(pack_f16x2(p0 * f, p1 * f));
+                        y[h][2 * u] *= f;
+                        y[h][2 * u + 1] *= f;
                     }
-                if (__any_sync(0xffffffffu, grown)) {
-                    const float c0 = corr[0] * sv_corr, c1 = corr[1] * sv_corr;
-#pragma unroll
-                    for (int i = 0; i < ND; ++i) { o[r][i][0] *= c0; o[r][i][1] *= c1; o[r][i][2] *= c0; o[r][i][3] *= c1; }
-                }
             }
-            // ---- weighted values: dims 16 c + 2 g, 16 c + 2 g + 1 of pairs kq, kq + 1. In a block that some row does not see whole, what
+            uint32_t pb[2][2];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int u = 0; u < 2; ++u) pb[h][u] = movmatrix_trans(pack_f16x2(y[h][2 * u], y[h][2 * u + 1]));
+            // ---- weighted values: dims 16 c + 2 g, 16 c + 2 g + 1 of pairs kq, kq + 1. In a stage that some row does not see whole, what
             // it does not see is a later row's value and need not be a number: there a value that is no number counts as 0 in the
             // products, and is put in afterwards where it is seen
             uint32_t bad = 0;
@@ -687,9 +706,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const uint32_t w0 = __byte_perm(v[2 * h], 0, 0x3120), w1 = __byte_perm(v[2 * h + 1], 0, 0x3120);       // tokens 8 more
-                    const uint32_t a0 = e4m3lo_f16x2(w0), a1 = e4m3hi_f16x2(w0), a2 = e4m3lo_f16x2(w1), a3 = e4m3hi_f16x2(w1);
-#pragma unroll
-                    for (int r = 0; r < RW; ++r) mma_f16(o[r][c], a0, a1, a2, a3, pb[r][h][0], pb[r][h][1]);
+                    mma_f16(o[c], e4m3lo_f16x2(w0), e4m3hi_f16x2(w0), e4m3lo_f16x2(w1), e4m3hi_f16x2(w1), pb[h][0], pb[h][1]);
                 }
             }
             if (edge && __any_sync(0xffffffffu, bad != 0u)) {
@@ -701,82 +718,83 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                         asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(sb + Lay::KV + piece_at<DH>(t, c) + (uint32_t)g * 2) : "memory");
                         const bool n0 = (w & 0x7fu) == 0x7fu, n1 = (w & 0x7f00u) == 0x7f00u;
 #pragma unroll
-                        for (int r = 0; r < RW; ++r)
-#pragma unroll
-                            for (int e = 0; e < 2; ++e) {
-                                const bool seen = tb + t < pn[r][e];
-                                o[r][c][e] += seen && n0 ? NAN : 0.f;
-                                o[r][c][2 + e] += seen && n1 ? NAN : 0.f;
-                            }
+                        for (int e = 0; e < 2; ++e) {
+                            const bool seen = tb + t < pn[e];
+                            o[c][e] += seen && n0 ? NAN : 0.f;
+                            o[c][2 + e] += seen && n1 ? NAN : 0.f;
+                        }
                     }
             }
         }
-        // ---- the chunk's partial result: o and the sum relative to the maximum, the maximum (log2 units)
+        // ---- the chunk's partial result: o and the sum relative to the reference, the reference (log2 units; what a group does not
+        // see of the chunk from its first stage on, it does not see at all)
         const int groups = min(WT, (it.t1 - it.t0 + kA8Blk - 1) / kA8Blk);       // the others had none of the chunk's stages
+        float m_ref[2];
 #pragma unroll
-        for (int r = 0; r < RW; ++r) {
+        for (int e = 0; e < 2; ++e) {
+            m_ref[e] = pn[e] > tb0 ? kP8Log2 - mo[e] : -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
+            for (int x = 4; x < 32; x <<= 1) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], x);
+        }
+        if (WT == 1 || groups == 1) {
+            if (wt == 0) {
 #pragma unroll
-                for (int x = 4; x < 32; x <<= 1) l_run[r][e] += __shfl_xor_sync(0xffffffffu, l_run[r][e], x);
+                for (int e = 0; e < 2; ++e)
+                    if (prow[e] < nv && pn[e] > it.t0) {             // such a pair, and it sees something of the chunk
+                        float *out = a.part + pout[e] + (size_t)it.chunk * (DH + 2);
+#pragma unroll
+                        for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(out + c * 16 + g * 2) = make_float2(o[c][e] * sv_run, o[c][2 + e] * sv_run);
+                        if (g == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(m_ref[e], l_run[e]);
+                    }
             }
-            if (WT == 1 || groups == 1) {
-                if (wt == 0) {
+        } else {
+            // Each warp leaves its result in the stage that its group read last (free until the group's next copy), and the warps of a tile add
+            // them up in the groups' order, 8 / WT pairs each
+            constexpr int LD = DH + 4;               // (rows of pairs start in different banks)
+            static_assert(WT == 1 || 8 * LD * 4 * WR <= Lay::STAGE, "a tile of each warp fits the stage");
+            float2 *ml = reinterpret_cast<float2 *>(smem + Lay::O_ML);
+            int *last = reinterpret_cast<int *>(smem + Lay::O_LAST);
+            group_sync<WR>(wt);                      // all readers of the stage are done
+            if (wt < groups) {
+                float *mine = reinterpret_cast<float *>(ring + (size_t)last_slot * Lay::STAGE) + wr * 8 * LD;
 #pragma unroll
-                    for (int e = 0; e < 2; ++e)
-                        if (prow[r][e] < nv && pn[r][e] > it.t0) {       // such a pair, and it sees something of the chunk
-                            float *out = a.part + pout[r][e] + (size_t)it.chunk * (DH + 2);
+                for (int e = 0; e < 2; ++e) {
 #pragma unroll
-                            for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(out + c * 16 + g * 2) = make_float2(o[r][c][e] * sv_run, o[r][c][2 + e] * sv_run);
-                            if (g == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(m_run[r][e] * fs[r][e], l_run[r][e]);
-                        }
+                    for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(mine + (kq + e) * LD + c * 16 + g * 2) = make_float2(o[c][e] * sv_run, o[c][2 + e] * sv_run);
+                    if (g == 0) ml[warp * 8 + kq + e] = make_float2(m_ref[e], l_run[e]);
                 }
-            } else {
-                // Each warp leaves a tile's result in the stage that its group read last (free until the group's next copy), and the
-                // threads of the tile's WT warps add them up in the groups' order: an eighth of a pair's dims at a time
-                constexpr int LD = DH + 4;           // (rows of pairs start in different banks)
-                static_assert(WT == 1 || 8 * LD * 4 * WR <= Lay::STAGE, "a tile of each warp fits the stage");
-                float2 *ml = reinterpret_cast<float2 *>(smem + Lay::O_ML);
-                int *last = reinterpret_cast<int *>(smem + Lay::O_LAST);
-                if (r == 0) group_sync<WR>(wt);     // all readers of the stage are done
-                if (wt < groups) {
-                    float *mine = reinterpret_cast<float *>(ring + (size_t)last_slot * Lay::STAGE) + wr * 8 * LD;
-#pragma unroll
-                    for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                        for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(mine + (kq + e) * LD + c * 16 + g * 2) = make_float2(o[r][c][e] * sv_run, o[r][c][2 + e] * sv_run);
-                        if (g == 0) ml[warp * 8 + kq + e] = make_float2(m_run[r][e] * fs[r][e], l_run[r][e]);
-                    }
-                    if (lane == 0 && wr == 0) last[wt] = last_slot;
-                }
-                __syncthreads();
-                // this warp's pairs of tile (wr, r): two for WT = 4, four for WT = 2; a pair's lanes take four dims each
-                constexpr int LPP = DH / 4, PPW = 8 / WT;        // lanes per pair, pairs per warp
-#pragma unroll
-                for (int q0 = 0; q0 < PPW; q0 += 32 / LPP) {
-                    const int q = wt * PPW + q0 + lane / LPP, d = lane % LPP * 4, pair = ((it.set * WR + wr) * RW + r) * 8 + q;
-                    float mm = -INFINITY;
-                    for (int x = 0; x < groups; ++x) mm = fmaxf(mm, ml[(x * WR + wr) * 8 + q].x);
-                    const float mu = mm == -INFINITY ? 0.f : mm;
-                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                    float l = 0.f;
-                    for (int x = 0; x < groups; ++x) {
-                        const float2 y = ml[(x * WR + wr) * 8 + q];
-                        const float f = exp2_approx(y.x - mu);
-                        const float4 v = *reinterpret_cast<const float4 *>(smem + (size_t)(x * S + last[x]) * Lay::STAGE + ((wr * 8 + q) * LD + d) * 4);
-                        acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
-                        l += y.y * f;
-                    }
-                    const int m = pair / gq;
-                    if (pair < nv * gq && row_ctx(tpos[it.seq], m) > it.t0) {
-                        float *out = a.part + (((size_t)(it.seq * a.M + m) * a.Hq + it.kvh * gq + (pair - m * gq)) * a.slots + it.chunk) * (DH + 2);
-                        *reinterpret_cast<float2 *>(out + d) = make_float2(acc.x, acc.y);
-                        *reinterpret_cast<float2 *>(out + d + 2) = make_float2(acc.z, acc.w);
-                        if (d == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(mm, l);
-                    }
-                }
-                __syncthreads();
+                if (lane == 0 && wr == 0) last[wt] = last_slot;
             }
+            __syncthreads();
+            constexpr int LPP = DH / 4, PPW = 8 / WT;            // lanes per pair (four dims each), pairs per warp
+#pragma unroll 1
+            for (int q0 = 0; q0 < PPW; q0 += 32 / LPP) {
+                const int q = wt * PPW + q0 + lane / LPP, d = lane % LPP * 4, pair = (it.set * WR + wr) * 8 + q;
+                float mm = -INFINITY;
+#pragma unroll
+                for (int x = 0; x < WT; ++x)
+                    if (x < groups) mm = fmaxf(mm, ml[(x * WR + wr) * 8 + q].x);
+                const float mu = mm == -INFINITY ? 0.f : mm;
+                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                float l = 0.f;
+#pragma unroll
+                for (int x = 0; x < WT; ++x) {
+                    if (x >= groups) continue;
+                    const float2 z = ml[(x * WR + wr) * 8 + q];
+                    const float f = exp2_approx(z.x - mu);
+                    const float4 v = *reinterpret_cast<const float4 *>(smem + (size_t)(x * S + last[x]) * Lay::STAGE + ((wr * 8 + q) * LD + d) * 4);
+                    acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
+                    l += z.y * f;
+                }
+                const int m = pair / gq;
+                if (pair < nv * gq && row_ctx(tpos[it.seq], m) > it.t0) {
+                    float *out = a.part + (((size_t)(it.seq * a.M + m) * a.Hq + it.kvh * gq + (pair - m * gq)) * a.slots + it.chunk) * (DH + 2);
+                    *reinterpret_cast<float2 *>(out + d) = make_float2(acc.x, acc.y);
+                    *reinterpret_cast<float2 *>(out + d + 2) = make_float2(acc.z, acc.w);
+                    if (d == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(mm, l);
+                }
+            }
+            __syncthreads();
         }
         __syncwarp();
         if (item + 1 < i_end) {
@@ -838,11 +856,11 @@ __global__ void __launch_bounds__(DH) kv8_merge_kernel(const Attn8Args a) {
     }
 }
 
-template <int DH, int RW, int WR>
+template <int DH, int WR>
 int attn8_launch(const Attn8Args &a, int rows, int n_sm, cudaStream_t st) {
-    auto kern = kv8_attn_kernel<DH, RW, WR>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Attn8Smem<DH, RW, WR>::TOTAL);
-    if (e == cudaSuccess) e = launch_chained(kern, dim3(Attn8Smem<DH, RW, WR>::CTAS * n_sm), dim3(kA8Threads), (size_t)Attn8Smem<DH, RW, WR>::TOTAL, st, a);
+    auto kern = kv8_attn_kernel<DH, WR>;
+    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Attn8Smem<DH, WR>::TOTAL);
+    if (e == cudaSuccess) e = launch_chained(kern, dim3(Attn8Smem<DH, WR>::CTAS * n_sm), dim3(kA8Threads), (size_t)Attn8Smem<DH, WR>::TOTAL, st, a);
     if (e == cudaSuccess) e = launch_chained(kv8_merge_kernel<DH>, dim3(a.Hq, rows), dim3(DH), 0, st, a);
     return (int)e;
 }
@@ -850,10 +868,8 @@ int attn8_launch(const Attn8Args &a, int rows, int n_sm, cudaStream_t st) {
 template <int DH>
 int attn8_pick(const Attn8Args &a, int rows, int n_sm, cudaStream_t st) {
     const int pairs = a.M * a.gq;
-    if (pairs <= 8) return attn8_launch<DH, 1, 1>(a, rows, n_sm, st);
-    if (DH == 64 || pairs <= 16) return attn8_launch<DH, 1, 2>(a, rows, n_sm, st);
-    if constexpr (DH == 128) return attn8_launch<DH, 1, 4>(a, rows, n_sm, st);
-    return (int)cudaErrorInvalidConfiguration;
+    if (pairs <= 8) return attn8_launch<DH, 1>(a, rows, n_sm, st);
+    return attn8_launch<DH, 2>(a, rows, n_sm, st);
 }
 
 }  // namespace
@@ -894,7 +910,7 @@ int kv8_attention_slots(const Kv8Shape &sh, int M) {
 int kv8_attention(const Kv8AttnCall &c, cudaStream_t st, long long *launches) {
     Attn8Args a{};
     a.Hq = c.sh.Hq; a.Hkv = c.sh.Hkv; a.gq = c.sh.Hq / c.sh.Hkv; a.page = c.sh.page; a.shift = shift_of(c.sh.page); a.max_ctx = c.sh.max_ctx;
-    a.slots = kv8_attention_slots(c.sh, c.M); a.B = c.B; a.M = c.M; a.q = c.q; a.ldq = c.ldq; a.n_new = c.n_new; a.kv = c.kv; a.part = c.part;
+    a.slots = kv8_attention_slots(c.sh, c.M); a.tiles16 = c.sh.page % 16 == 0; a.B = c.B; a.M = c.M; a.q = c.q; a.ldq = c.ldq; a.n_new = c.n_new; a.kv = c.kv; a.part = c.part;
     a.out = c.out; a.xop = c.xop; a.ld_xop = c.ld_xop; a.status = c.status;
     *launches += 2;
     return c.sh.dh == 128 ? attn8_pick<128>(a, c.B * c.M, c.n_sm, st) : attn8_pick<64>(a, c.B * c.M, c.n_sm, st);
