@@ -790,6 +790,7 @@ int fastmtp_kv8_attention(fmtp_ctx *c, const fmtp_bf16 *q, long long ldq, const 
         a.out = out + (size_t)b0 * M * row;
         a.status = dev_status ? dev_status : c->s.status;
         a.n_sm = c->n_sm;
+        a.raised = c->tmaps.attn8_raised;
         int err = kv8_attention(a, static_cast<cudaStream_t>(stream), &c->launches);
         if (err) return cuda_fail(c, (cudaError_t)err);
     }

@@ -8,7 +8,7 @@ namespace fmtp {
 
 namespace {
 
-constexpr uint32_t kDevBadPage = 0x2u, kDevBadPos = 0x4u;
+constexpr uint32_t kDevBadPage = 0x2u, kDevBadPos = 0x4u, kDevTimeout8 = 0x8u;
 constexpr int kMaxLen = 1 << 30;      // a longer committed length is the caller's error: flagged like any position without a slot
 
 __device__ __forceinline__ int kv8_len(const Kv8Ptrs &kv, int b) { return min(max(kv.seq_lens[b], 0), kMaxLen); }
@@ -69,7 +69,7 @@ struct Append8Args {
 constexpr int kAppendWarps = 4;
 
 template <int DH>
-__global__ void __launch_bounds__(kAppendWarps * 32) kv8_append_kernel(const Append8Args a) {
+__global__ void __launch_bounds__(kAppendWarps * 32, 8) kv8_append_kernel(const Append8Args a) {
     chain_release();
     chain_wait();
     constexpr int LPR = DH / 8;                      // lanes per row: eight values each
@@ -95,16 +95,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv8_append_kernel(const App
     }
     const bool is_v = head2 >= a.Hkv;
     const int kvh = is_v ? head2 - a.Hkv : head2;
-    const int page = a.kv.block_table[(size_t)b * a.kv.max_pages + blk];
-    if ((unsigned)page >= (unsigned)a.kv.num_pages) {          // not written either
-        if (lane == 0) atomicOr(a.status, kDevBadPage);
-        return;
-    }
-    const size_t slot = (size_t)page * a.Hkv + kvh;
-    uint8_t *dst = (is_v ? a.kv.v_pages : a.kv.k_pages) + slot * a.page * DH + piece * 8;
-    float *scale = (is_v ? a.kv.v_scales : a.kv.k_scales) + slot;
     const bf16_t *src = (is_v ? a.v : a.k) + ((long long)b * a.M - L) * a.ld + (long long)kvh * DH + piece * 8;      // + position * ld
-    const float s_old = first > at ? *scale : 0.f;
     uint4 x[NT];
     auto load = [&](int p0) {
 #pragma unroll
@@ -114,10 +105,24 @@ __global__ void __launch_bounds__(kAppendWarps * 32) kv8_append_kernel(const App
         }
     };
     uint32_t m = 0;
-    for (int p0 = first; p0 < end; p0 += 16) {       // (more than one turn where a block is longer than 16 tokens)
-        load(p0);
+    auto largest = [&]() {
 #pragma unroll
         for (int u = 0; u < NT; ++u) m = finite_max(finite_max(finite_max(finite_max(m, x[u].x), x[u].y), x[u].z), x[u].w);
+    };
+    load(first);                                     // (on their way while the block is looked up)
+    const int page = a.kv.block_table[(size_t)b * a.kv.max_pages + blk];
+    if ((unsigned)page >= (unsigned)a.kv.num_pages) {          // not written either
+        if (lane == 0) atomicOr(a.status, kDevBadPage);
+        return;
+    }
+    const size_t slot = (size_t)page * a.Hkv + kvh;
+    uint8_t *dst = (is_v ? a.kv.v_pages : a.kv.k_pages) + slot * a.page * DH + piece * 8;
+    float *scale = (is_v ? a.kv.v_scales : a.kv.k_scales) + slot;
+    const float s_old = first > at ? *scale : 0.f;
+    largest();
+    for (int p0 = first + 16; p0 < end; p0 += 16) {  // (blocks longer than 16 tokens)
+        load(p0);
+        largest();
     }
     m = max(m & 0xffffu, m >> 16);
     m = __reduce_max_sync(0xffffffffu, m);
@@ -227,9 +232,9 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv8_read_kernel(const Read8Ar
 }
 
 // ---- attention. The (row, query head) pairs that share a KV head of a sequence are dealt to tiles of eight; a work item is one chunk of
-// a sequence's context for one KV head and a set of WR tiles. A CTA of four warps walks a contiguous range of items. Its
+// a sequence's context for one KV head and a set of RW * WR tiles. A CTA of four warps walks a contiguous range of items. Its
 // WT = 4 / WR groups of WR warps take the chunk's 32-token stages in turn, each with a ring of its own, and meet at the chunk's end,
-// where their results are joined in shared memory; a group's warps take a tile each. (A warp for an item kept the SMs busy
+// where their results are joined in shared memory; a group's warps take RW tiles each, which share the conversions. (A warp for an item kept the SMs busy
 // for three quarters of the time: an item of 256 tokens took it 25 us.)
 //
 // Both products run on mma.sync.m16n8k16 with f16 operands (sm_100a has no mma.sync on e4m3: the assembler emulates it with fifteen
@@ -279,17 +284,19 @@ __host__ __device__ __forceinline__ int chunk8(int n_ctx, int pairs) {
     return c;
 }
 
-template <int DH, int WR>
+constexpr int kList8Words = 6 * kBatchRows + 2;       // see List8
+
+template <int DH, int RW, int WR>
 struct Attn8Smem {
     static constexpr int WT = kA8Warps / WR;                                 // workers of a CTA
-    static constexpr int CTAS = DH == 128 ? 3 : 4;                           // resident per SM
-    static constexpr int S = DH == 128 ? 8 / WT : 12 / WT;                   // stages
+    static constexpr int CTAS = (DH == 128 ? 3 : 4) - (RW - 1);              // resident per SM
+    static constexpr int S = (DH == 128 && RW == 1 ? 8 : 12) / WT;           // stages
     static constexpr int KV = kA8Blk * DH;                                   // bytes of a stage's K (or V) codes
     static constexpr int STAGE = 2 * KV + 2 * kA8Blk * 4;
     static constexpr int O_ML = WT * S * STAGE;                              // [4 warps][8 pairs] maximum, sum
     static constexpr int O_LAST = O_ML + kA8Warps * 8 * 8;                   // [WT] the stage that a group read last
     static constexpr int O_TAB = O_LAST + kA8Warps * 4;
-    static constexpr int TOTAL = O_TAB + (6 * kBatchRows + 2) * 4;
+    static constexpr int TOTAL = O_TAB + kList8Words * 4;
 };
 
 // (Warp-wide instructions are volatile: the compiler may move an asm statement without side effects into a branch that uses its result,
@@ -324,6 +331,9 @@ __device__ __forceinline__ float lds32f(uint32_t addr) {
     asm volatile("ld.shared.f32 %0, [%1];" : "=f"(v) : "r"(addr) : "memory");
     return v;
 }
+__device__ __forceinline__ void sts128(uint32_t addr, uint32_t a, uint32_t b, uint32_t c, uint32_t d) {
+    asm volatile("st.shared.v4.b32 [%0], {%1,%2,%3,%4};" ::"r"(addr), "r"(a), "r"(b), "r"(c), "r"(d) : "memory");
+}
 __device__ __forceinline__ float exp2_approx(float x) {      // 2^x; results below the normal range are zero, as is 2^-inf
     float y;
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
@@ -352,24 +362,26 @@ struct Item8 {
     int t0, t1;                                      // the chunk's tokens [t0, t1): never empty, the sequence's last row sees them all
 };
 
-template <int DH, int WR>
-__global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
-    chain_wait();
-    using Lay = Attn8Smem<DH, WR>;
-    constexpr int WT = Lay::WT, S = Lay::S, KS = DH / 32, ND = DH / 16;
-    extern __shared__ __align__(128) unsigned char smem[];
-    int *prefix = reinterpret_cast<int *>(smem + Lay::O_TAB);              // [B + 1] items before a sequence
-    int *pcost = prefix + kBatchRows + 1;                                  // [B + 1] their cost: a group's stages, and one for each item
-    int *tpos = pcost + kBatchRows + 1;                                    // position of a sequence's row 0
-    int *tval = tpos + kBatchRows;                                         // its rows that count
-    int *tchk = tval + kBatchRows;                                         // tokens of its chunks
-    int *tnum = tchk + kBatchRows;                                         // chunks, sets << 16
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wr = warp % WR, wt = warp / WR;
-    const int max_tokens = min((int)min((long long)a.kv.max_pages * a.page, (long long)kMaxLen), a.max_ctx);
-    const int gq = a.gq;
-    auto row_ctx = [&](int pos0, int m) -> int { return min(pos0 + m, max_tokens - 1) + 1; };     // positions that row m sees
-    constexpr int STRIDE = WT * kA8Blk;              // tokens from one stage of a group to its next
-    if (warp == 0) {                                 // two sequences per lane
+// The list itself. An item has PAIRS pairs; it costs EACH and one for every STRIDE tokens.
+template <int PAIRS, int STRIDE, int EACH>
+struct List8 {
+    int *prefix, *pcost;                             // [B + 1] items before a sequence, and their cost
+    int *tpos, *tval, *tchk, *tnum;                  // position of a sequence's row 0, its rows that count, tokens of its chunks, chunks | sets << 16
+    int B, Hkv, max_tokens;
+
+    __device__ __forceinline__ List8(const Attn8Args &a, void *mem) {
+        prefix = static_cast<int *>(mem);
+        pcost = prefix + kBatchRows + 1;
+        tpos = pcost + kBatchRows + 1;
+        tval = tpos + kBatchRows;
+        tchk = tval + kBatchRows;
+        tnum = tchk + kBatchRows;
+        B = a.B;
+        Hkv = a.Hkv;
+        max_tokens = min((int)min((long long)a.kv.max_pages * a.page, (long long)kMaxLen), a.max_ctx);
+    }
+    __device__ __forceinline__ int row_ctx(int pos0, int m) const { return min(pos0 + m, max_tokens - 1) + 1; }     // positions that row m sees
+    __device__ __forceinline__ void build(const Attn8Args &a, int lane) {      // one warp, two sequences per lane
         int cnt[2], cost[2];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
@@ -377,14 +389,14 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
             cnt[u] = cost[u] = 0;
             if (s < a.B) {
                 const int len = kv8_len(a.kv, s), nv = kv8_rows(a.n_new, s, a.M);
-                const int c = chunk8(row_ctx(len, a.M - 1), a.M * gq);
+                const int c = chunk8(row_ctx(len, a.M - 1), a.M * a.gq);
                 tpos[s] = len; tval[s] = nv; tchk[s] = c;
                 tnum[s] = 0;
                 if (nv > 0) {
-                    const int n = row_ctx(len, nv - 1), chunks = (n + c - 1) / c, sets = (nv * gq + 8 * WR - 1) / (8 * WR);
+                    const int n = row_ctx(len, nv - 1), chunks = (n + c - 1) / c, sets = (nv * a.gq + PAIRS - 1) / PAIRS;
                     tnum[s] = chunks | (sets << 16);
                     cnt[u] = chunks * a.Hkv * sets;
-                    cost[u] = (chunks + (n + STRIDE - 1) / STRIDE) * a.Hkv * sets;
+                    cost[u] = (chunks * EACH + (n + STRIDE - 1) / STRIDE) * a.Hkv * sets;
                     if (len + nv > max_tokens && blockIdx.x == 0) atomicOr(a.status, kDevBadPos);
                 }
             }
@@ -405,47 +417,64 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
         }
         if (lane == 0) prefix[0] = pcost[0] = 0;
     }
-    __syncwarp();
-    __syncthreads();
-    // CTAs' shares of the list have the same cost up to an item: a CTA begins with the first item that starts at or behind its share
-    const int n_items = prefix[a.B], n_cost = pcost[a.B];
-    auto item_at = [&](long long x) -> int {
-        if (x >= n_cost) return n_items;
+    // CTAs' shares of the list have the same cost up to an item: CTA i of n begins with the first item that starts at or behind its share
+    __device__ __forceinline__ int begin_of(int i, int n) const {
+        const int n_cost = pcost[B];
+        const long long x = (long long)i * n_cost / n;
+        if (x >= n_cost) return prefix[B];
         int s = 0;
         while (pcost[s + 1] <= x) ++s;
         const int rem = (int)x - pcost[s], chunks = tnum[s] & 0xffff, contexts = (prefix[s + 1] - prefix[s]) / chunks;
-        const int cost = (pcost[s + 1] - pcost[s]) / contexts, ctx = rem / cost, one = tchk[s] / STRIDE + 1;
+        const int cost = (pcost[s + 1] - pcost[s]) / contexts, ctx = rem / cost, one = tchk[s] / STRIDE + EACH;
         return prefix[s] + ctx * chunks + min((rem - ctx * cost + one - 1) / one, chunks);
-    };
-    const int i_begin = item_at((long long)blockIdx.x * n_cost / gridDim.x), i_end = item_at((long long)(blockIdx.x + 1) * n_cost / gridDim.x);
-    auto chunk_bounds = [&](Item8 &it) {
+    }
+    __device__ __forceinline__ void bounds(Item8 &it) const {
         const int c = tchk[it.seq];
         it.t0 = it.chunk * c;
         it.t1 = min(it.t0 + c, row_ctx(tpos[it.seq], tval[it.seq] - 1));
-    };
-    auto first_item = [&](Item8 &it) {
+    }
+    __device__ __forceinline__ void at(Item8 &it, int i) const {
         int s = 0;
-        while (prefix[s + 1] <= i_begin) ++s;
-        const int rem = i_begin - prefix[s], chunks = tnum[s] & 0xffff, sets = tnum[s] >> 16, t = rem / chunks;
+        while (prefix[s + 1] <= i) ++s;
+        const int rem = i - prefix[s], chunks = tnum[s] & 0xffff, sets = tnum[s] >> 16, t = rem / chunks;
         it.seq = s;
         it.chunk = rem - t * chunks;
         it.kvh = t / sets;
         it.set = t - it.kvh * sets;
-        chunk_bounds(it);
-    };
-    auto next_item = [&](Item8 &it) {
+        bounds(it);
+    }
+    __device__ __forceinline__ bool next(Item8 &it) const {          // whether the queries change (there is another item)
+        bool fresh = false;
         if (++it.chunk == (tnum[it.seq] & 0xffff)) {
             it.chunk = 0;
+            fresh = true;
             if (++it.set == tnum[it.seq] >> 16) {
                 it.set = 0;
-                if (++it.kvh == a.Hkv) {
+                if (++it.kvh == Hkv) {
                     it.kvh = 0;
-                    do ++it.seq; while (prefix[it.seq + 1] == prefix[it.seq]);       // (there is another item)
+                    do ++it.seq; while (prefix[it.seq + 1] == prefix[it.seq]);
                 }
             }
         }
-        chunk_bounds(it);
-    };
+        bounds(it);
+        return fresh;
+    }
+};
+
+template <int DH, int RW, int WR>
+__global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_attn_kernel(const __grid_constant__ Attn8Args a) {
+    chain_wait();
+    using Lay = Attn8Smem<DH, RW, WR>;
+    constexpr int WT = Lay::WT, S = Lay::S, KS = DH / 32, ND = DH / 16, TILES = RW * WR;
+    extern __shared__ __align__(128) unsigned char smem[];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wr = warp % WR, wt = warp / WR;
+    const int gq = a.gq;
+    constexpr int STRIDE = WT * kA8Blk;              // tokens from one stage of a group to its next
+    List8<8 * TILES, STRIDE, 1> list(a, smem + Lay::O_TAB);
+    if (warp == 0) list.build(a, lane);
+    __syncwarp();
+    __syncthreads();
+    const int i_begin = list.begin_of((int)blockIdx.x, (int)gridDim.x), i_end = list.begin_of((int)blockIdx.x + 1, (int)gridDim.x);
     if (i_begin >= i_end) return;                    // (an exit releases the successor as well)
 
     // ---- copying. Block-table entries are read a segment ahead (a read queues behind the copies that are on their way, which takes
@@ -460,7 +489,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
     auto load_segment = [&](Segment &g) {
         while (litem < i_end && ltok >= li.t1) {     // (an item may be too short for this group)
             if (++litem < i_end) {
-                next_item(li);
+                list.next(li);
                 ltok = li.t0 + wt * kA8Blk;
             }
         }
@@ -524,7 +553,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    first_item(li);
+    list.at(li, i_begin);
     Item8 it = li;
     ltok = li.t0 + wt * kA8Blk;
     load_segment(cur);
@@ -537,58 +566,66 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
     const float sm_scale = (1.0f / sqrtf((float)DH)) * 1.4426950408889634f;
     // ldmatrix rows: K: tokens 0-7 and 8-15 of one piece, then of the next; V: four groups of eight tokens of one piece
     const int ktok = lane & 15, kpc = lane >> 4;
-    uint32_t qb[2 * KS][2];
-    float fs[2];                                     // a query element times a key code times the K scale -> log2 units
-    int pn[2], prow[2];                              // positions that a pair sees, its row (no such pair: any, the sequence's number of rows)
-    size_t pout[2];                                  // where its partial results go
+    uint32_t qb[RW][2 * KS][2];
+    float fs[RW][2];                                     // a query element times a key code times the K scale -> log2 units
+    int pn[RW][2], prow[RW][2];                              // positions that a pair sees, its row (no such pair: any, the sequence's number of rows)
+    size_t pout[RW][2];                                  // where its partial results go
     bool fresh = true;
     int slot = 0, last_slot = 0, nv = 0;
     for (int item = i_begin; item < i_end; ++item) {
         if (fresh) {                                 // the queries stay in registers while the items are chunks of one context
-            nv = tval[it.seq];
-            const int pair0 = (it.set * WR + wr) * 8;
-            auto pair_at = [&](int pair, int &m, int &row, int &head) -> bool {
-                const bool there = pair < nv * gq;
-                m = there ? pair / gq : 0;
-                row = it.seq * a.M + m;
-                head = it.kvh * gq + (there ? pair - m * gq : 0);
-                return there;
-            };
-            int m, row, head;
-            pair_at(pair0 + g, m, row, head);
-            const bf16_t *qp = a.q + (long long)row * a.ldq + (long long)head * DH;
-            uint2 x[2 * KS];
-            uint32_t am = 0;
+            nv = list.tval[it.seq];
 #pragma unroll
-            for (int j = 0; j < 2 * KS; ++j) {
-                x[j] = *reinterpret_cast<const uint2 *>(qp + j * 16 + kq * 2);
-                am = finite_max(finite_max(am, x[j].x), x[j].y);
-            }
-            am = max(am & 0xffffu, am >> 16);
-            am = max(am, __shfl_xor_sync(0xffffffffu, am, 1));
-            am = max(am, __shfl_xor_sync(0xffffffffu, am, 2));
-            const float qs = scale_for(am), inv = kQ8 / qs;
+            for (int r = 0; r < RW; ++r) {
+                const int pair0 = ((it.set * WR + wr) * RW + r) * 8;
+                auto pair_at = [&](int pair, int &m, int &row, int &head) -> bool {
+                    const bool there = pair < nv * gq;
+                    m = there ? pair / gq : 0;
+                    row = it.seq * a.M + m;
+                    head = it.kvh * gq + (there ? pair - m * gq : 0);
+                    return there;
+                };
+                int m, row, head;
+                pair_at(pair0 + g, m, row, head);
+                const bf16_t *qp = a.q + (long long)row * a.ldq + (long long)head * DH;
+                uint2 x[2 * KS];
+                uint32_t am = 0;
 #pragma unroll
-            for (int j = 0; j < 2 * KS; ++j) {       // (a query that is not finite becomes NaN)
-                float y[4] = {bf16lo_f32(x[j].x), bf16hi_f32(x[j].x), bf16lo_f32(x[j].y), bf16hi_f32(x[j].y)};
+                for (int j = 0; j < 2 * KS; ++j) {
+                    x[j] = *reinterpret_cast<const uint2 *>(qp + j * 16 + kq * 2);
+                    am = finite_max(finite_max(am, x[j].x), x[j].y);
+                }
+                am = max(am & 0xffffu, am >> 16);
+                am = max(am, __shfl_xor_sync(0xffffffffu, am, 1));
+                am = max(am, __shfl_xor_sync(0xffffffffu, am, 2));
+                const float qs = scale_for(am), inv = kQ8 / qs;
 #pragma unroll
-                for (int i = 0; i < 4; ++i) y[i] = fabsf(y[i]) < INFINITY ? y[i] * inv : __uint_as_float(0x7fffffffu);
-                qb[j][0] = pack_f16x2(y[0], y[1]);
-                qb[j][1] = pack_f16x2(y[2], y[3]);
-            }
+                for (int j = 0; j < 2 * KS; ++j) {       // (a query that is not finite becomes NaN)
+                    float y[4] = {bf16lo_f32(x[j].x), bf16hi_f32(x[j].x), bf16lo_f32(x[j].y), bf16hi_f32(x[j].y)};
 #pragma unroll
-            for (int e = 0; e < 2; ++e) {
-                fs[e] = __shfl_sync(0xffffffffu, qs, (kq + e) * 4) * (sm_scale / kQ8);
-                const bool there = pair_at(pair0 + kq + e, m, row, head);
-                prow[e] = there ? m : nv;
-                pn[e] = there ? row_ctx(tpos[it.seq], m) : kMaxLen;
-                pout[e] = ((size_t)row * a.Hq + head) * a.slots * (DH + 2);
+                    for (int i = 0; i < 4; ++i) y[i] = fabsf(y[i]) < INFINITY ? y[i] * inv : __uint_as_float(0x7fffffffu);
+                    qb[r][j][0] = pack_f16x2(y[0], y[1]);
+                    qb[r][j][1] = pack_f16x2(y[2], y[3]);
+                }
+#pragma unroll
+                for (int e = 0; e < 2; ++e) {
+                    fs[r][e] = __shfl_sync(0xffffffffu, qs, (kq + e) * 4) * (sm_scale / kQ8);
+                    const bool there = pair_at(pair0 + kq + e, m, row, head);
+                    prow[r][e] = there ? m : nv;
+                    pn[r][e] = there ? list.row_ctx(list.tpos[it.seq], m) : kMaxLen;
+                    pout[r][e] = ((size_t)row * a.Hq + head) * a.slots * (DH + 2);
+                }
             }
         }
-        float mo[2] = {kP8Log2, kP8Log2}, l_run[2] = {0.f, 0.f}, o[ND][4];       // a score's exponent: fma(score, fs, mo)
+        float mo[RW][2], l_run[RW][2], o[RW][ND][4];         // a score's exponent: fma(score, fs, mo)
         float sv_run = 0.f, sv_inv = 0.f;            // largest V scale so far, its inverse
 #pragma unroll
-        for (int i = 0; i < ND; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+        for (int r = 0; r < RW; ++r) {
+            mo[r][0] = mo[r][1] = kP8Log2;
+            l_run[r][0] = l_run[r][1] = 0.f;
+#pragma unroll
+            for (int i = 0; i < ND; ++i) o[r][i][0] = o[r][i][1] = o[r][i][2] = o[r][i][3] = 0.f;
+        }
         const int tb0 = it.t0 + wt * kA8Blk;
 #pragma unroll 1
         for (int tb = tb0; tb < it.t1; tb += STRIDE) {
@@ -599,9 +636,11 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
             last_slot = slot;
             if (++slot == S) slot = 0;
             // ---- scores: tokens 16 h + g, 16 h + 8 + g of pairs kq, kq + 1
-            float y[2][4];
+            float y[RW][2][4];
 #pragma unroll
-            for (int h = 0; h < 2; ++h) y[h][0] = y[h][1] = y[h][2] = y[h][3] = 0.f;
+            for (int r = 0; r < RW; ++r)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) y[r][h][0] = y[r][h][1] = y[r][h][2] = y[r][h][3] = 0.f;
 #pragma unroll
             for (int ks = 0; ks < KS; ++ks) {        // 32 dims
                 uint32_t kf[2][4];
@@ -610,9 +649,12 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
 #pragma unroll
                 for (int u = 0; u < 2; ++u)
 #pragma unroll
-                    for (int h = 0; h < 2; ++h)
-                        mma_f16(y[h], e4m3lo_f16x2(kf[h][2 * u]), e4m3lo_f16x2(kf[h][2 * u + 1]), e4m3hi_f16x2(kf[h][2 * u]), e4m3hi_f16x2(kf[h][2 * u + 1]),
-                                qb[2 * ks + u][0], qb[2 * ks + u][1]);
+                    for (int h = 0; h < 2; ++h) {
+                        const uint32_t a0 = e4m3lo_f16x2(kf[h][2 * u]), a1 = e4m3lo_f16x2(kf[h][2 * u + 1]);
+                        const uint32_t a2 = e4m3hi_f16x2(kf[h][2 * u]), a3 = e4m3hi_f16x2(kf[h][2 * u + 1]);
+#pragma unroll
+                        for (int r = 0; r < RW; ++r) mma_f16(y[r][h], a0, a1, a2, a3, qb[r][2 * ks + u][0], qb[r][2 * ks + u][1]);
+                    }
             }
             // ---- exponents; V scales of the lane's tokens
             float sv[2][2];
@@ -623,70 +665,91 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
                     const uint32_t at = sb + 2 * Lay::KV + (h * 16 + u * 8 + g) * 4;
                     const float sk = lds32f(at);
                     sv[h][u] = lds32f(at + kA8Blk * 4);
-                    y[h][2 * u] = fmaf(y[h][2 * u] * sk, fs[0], mo[0]);
-                    y[h][2 * u + 1] = fmaf(y[h][2 * u + 1] * sk, fs[1], mo[1]);
+#pragma unroll
+                    for (int r = 0; r < RW; ++r) {
+                        y[r][h][2 * u] = fmaf(y[r][h][2 * u] * sk, fs[r][0], mo[r][0]);
+                        y[r][h][2 * u + 1] = fmaf(y[r][h][2 * u + 1] * sk, fs[r][1], mo[r][1]);
+                    }
                 }
-            const bool edge = __any_sync(0xffffffffu, min(pn[0], pn[1]) - tb < kA8Blk);
+            int least = kMaxLen;                     // what the pair that sees least sees
+#pragma unroll
+            for (int r = 0; r < RW; ++r) least = min(least, min(pn[r][0], pn[r][1]));
+            const bool edge = __any_sync(0xffffffffu, least - tb < kA8Blk);
             if (edge) {
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+                for (int r = 0; r < RW; ++r)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        if (tb + h * 16 + (i >> 1) * 8 + g >= pn[i & 1]) y[h][i] = -INFINITY;
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i)
+                            if (tb + h * 16 + (i >> 1) * 8 + g >= pn[r][i & 1]) y[r][h][i] = -INFINITY;
             }
-            float ym[2];
+            float ym[RW][2], most = -INFINITY;
 #pragma unroll
-            for (int e = 0; e < 2; ++e) ym[e] = fmaxf(fmaxf(y[0][e], y[0][2 + e]), fmaxf(y[1][e], y[1][2 + e]));
-            float svm = fmaxf(fmaxf(sv[0][0], sv[0][1]), fmaxf(sv[1][0], sv[1][1]));
-            if (tb == tb0 || __any_sync(0xffffffffu, fmaxf(ym[0], ym[1]) > kP8Max || svm > sv_run)) {
-                // new references: the stage's maximum where it is the first or far above, the largest V scale
-                float corr[2];
+            for (int r = 0; r < RW; ++r)
 #pragma unroll
                 for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                    for (int x = 4; x < 32; x <<= 1) ym[e] = fmaxf(ym[e], __shfl_xor_sync(0xffffffffu, ym[e], x));
-                    const float d = (tb == tb0 || ym[e] > kP8Max) && ym[e] > -INFINITY ? ym[e] - kP8Log2 : 0.f;
-                    mo[e] -= d;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) { y[h][e] -= d; y[h][2 + e] -= d; }
-                    corr[e] = tb == tb0 ? 1.f : exp2_approx(-d);
-                    l_run[e] *= corr[e];
+                    ym[r][e] = fmaxf(fmaxf(y[r][0][e], y[r][0][2 + e]), fmaxf(y[r][1][e], y[r][1][2 + e]));
+                    most = fmaxf(most, ym[r][e]);
                 }
+            float svm = fmaxf(fmaxf(sv[0][0], sv[0][1]), fmaxf(sv[1][0], sv[1][1]));
+            if (tb == tb0 || __any_sync(0xffffffffu, most > kP8Max || svm > sv_run)) {
+                // new references: the stage's maximum where it is the first or far above, the largest V scale
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) svm = fmaxf(svm, __shfl_xor_sync(0xffffffffu, svm, x));
+                float vcorr = 1.f;
                 if (svm > sv_run) {
                     sv_inv = __fdividef(1.0f, svm);
-                    corr[0] *= sv_run * sv_inv;
-                    corr[1] *= sv_run * sv_inv;
+                    vcorr = sv_run * sv_inv;
                     sv_run = svm;
                 }
-                if (tb != tb0) {
 #pragma unroll
-                    for (int i = 0; i < ND; ++i) { o[i][0] *= corr[0]; o[i][1] *= corr[1]; o[i][2] *= corr[0]; o[i][3] *= corr[1]; }
+                for (int r = 0; r < RW; ++r) {
+                    float corr[2];
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int x = 4; x < 32; x <<= 1) ym[r][e] = fmaxf(ym[r][e], __shfl_xor_sync(0xffffffffu, ym[r][e], x));
+                        const float d = (tb == tb0 || ym[r][e] > kP8Max) && ym[r][e] > -INFINITY ? ym[r][e] - kP8Log2 : 0.f;
+                        mo[r][e] -= d;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) { y[r][h][e] -= d; y[r][h][2 + e] -= d; }
+                        corr[e] = tb == tb0 ? 1.f : exp2_approx(-d);
+                        l_run[r][e] *= corr[e];
+                        corr[e] *= vcorr;
+                    }
+                    if (tb != tb0) {
+#pragma unroll
+                        for (int i = 0; i < ND; ++i) { o[r][i][0] *= corr[0]; o[r][i][1] *= corr[1]; o[r][i][2] *= corr[0]; o[r][i][3] *= corr[1]; }
+                    }
                 }
             }
             // ---- probabilities
+            const bool scaled = !__all_sync(0xffffffffu, sv[0][0] == sv_run && sv[0][1] == sv_run && sv[1][0] == sv_run && sv[1][1] == sv_run);
+            uint32_t pb[RW][2][2];
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) y[h][i] = exp2_approx(y[h][i]);
-            l_run[0] += (y[0][0] + y[0][2]) + (y[1][0] + y[1][2]);
-            l_run[1] += (y[0][1] + y[0][3]) + (y[1][1] + y[1][3]);
-            if (!__all_sync(0xffffffffu, sv[0][0] == sv_run && sv[0][1] == sv_run && sv[1][0] == sv_run && sv[1][1] == sv_run)) {
+            for (int r = 0; r < RW; ++r) {
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) {
-                        const float f = sv[h][u] * sv_inv;
-                        y[h][2 * u] *= f;
-                        y[h][2 * u + 1] *= f;
-                    }
+                    for (int i = 0; i < 4; ++i) y[r][h][i] = exp2_approx(y[r][h][i]);
+                l_run[r][0] += (y[r][0][0] + y[r][0][2]) + (y[r][1][0] + y[r][1][2]);
+                l_run[r][1] += (y[r][0][1] + y[r][0][3]) + (y[r][1][1] + y[r][1][3]);
+                if (scaled) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) {
+                            const float f = sv[h][u] * sv_inv;
+                            y[r][h][2 * u] *= f;
+                            y[r][h][2 * u + 1] *= f;
+                        }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) pb[r][h][u] = movmatrix_trans(pack_f16x2(y[r][h][2 * u], y[r][h][2 * u + 1]));
             }
-            uint32_t pb[2][2];
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int u = 0; u < 2; ++u) pb[h][u] = movmatrix_trans(pack_f16x2(y[h][2 * u], y[h][2 * u + 1]));
             // ---- weighted values: dims 16 c + 2 g, 16 c + 2 g + 1 of pairs kq, kq + 1. In a stage that some row does not see whole, what
             // it does not see is a later row's value and need not be a number: there a value that is no number counts as 0 in the
             // products, and is put in afterwards where it is seen
@@ -706,7 +769,9 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
                     const uint32_t w0 = __byte_perm(v[2 * h], 0, 0x3120), w1 = __byte_perm(v[2 * h + 1], 0, 0x3120);       // tokens 8 more
-                    mma_f16(o[c], e4m3lo_f16x2(w0), e4m3hi_f16x2(w0), e4m3lo_f16x2(w1), e4m3hi_f16x2(w1), pb[h][0], pb[h][1]);
+                    const uint32_t a0 = e4m3lo_f16x2(w0), a1 = e4m3hi_f16x2(w0), a2 = e4m3lo_f16x2(w1), a3 = e4m3hi_f16x2(w1);
+#pragma unroll
+                    for (int r = 0; r < RW; ++r) mma_f16(o[r][c], a0, a1, a2, a3, pb[r][h][0], pb[r][h][1]);
                 }
             }
             if (edge && __any_sync(0xffffffffu, bad != 0u)) {
@@ -718,92 +783,539 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, WR>::CTAS) kv8_attn_
                         asm volatile("ld.shared.u16 %0, [%1];" : "=h"(w) : "r"(sb + Lay::KV + piece_at<DH>(t, c) + (uint32_t)g * 2) : "memory");
                         const bool n0 = (w & 0x7fu) == 0x7fu, n1 = (w & 0x7f00u) == 0x7f00u;
 #pragma unroll
-                        for (int e = 0; e < 2; ++e) {
-                            const bool seen = tb + t < pn[e];
-                            o[c][e] += seen && n0 ? NAN : 0.f;
-                            o[c][2 + e] += seen && n1 ? NAN : 0.f;
-                        }
+                        for (int r = 0; r < RW; ++r)
+#pragma unroll
+                            for (int e = 0; e < 2; ++e) {
+                                const bool seen = tb + t < pn[r][e];
+                                o[r][c][e] += seen && n0 ? NAN : 0.f;
+                                o[r][c][2 + e] += seen && n1 ? NAN : 0.f;
+                            }
                     }
             }
         }
         // ---- the chunk's partial result: o and the sum relative to the reference, the reference (log2 units; what a group does not
         // see of the chunk from its first stage on, it does not see at all)
         const int groups = min(WT, (it.t1 - it.t0 + kA8Blk - 1) / kA8Blk);       // the others had none of the chunk's stages
-        float m_ref[2];
 #pragma unroll
-        for (int e = 0; e < 2; ++e) {
-            m_ref[e] = pn[e] > tb0 ? kP8Log2 - mo[e] : -INFINITY;
+        for (int r = 0; r < RW; ++r) {
+            float m_ref[2];
 #pragma unroll
-            for (int x = 4; x < 32; x <<= 1) l_run[e] += __shfl_xor_sync(0xffffffffu, l_run[e], x);
-        }
-        if (WT == 1 || groups == 1) {
-            if (wt == 0) {
+            for (int e = 0; e < 2; ++e) {
+                m_ref[e] = pn[r][e] > tb0 ? kP8Log2 - mo[r][e] : -INFINITY;
 #pragma unroll
-                for (int e = 0; e < 2; ++e)
-                    if (prow[e] < nv && pn[e] > it.t0) {             // such a pair, and it sees something of the chunk
-                        float *out = a.part + pout[e] + (size_t)it.chunk * (DH + 2);
+                for (int x = 4; x < 32; x <<= 1) l_run[r][e] += __shfl_xor_sync(0xffffffffu, l_run[r][e], x);
+            }
+            if (WT == 1 || groups == 1) {
+                if (wt == 0) {
 #pragma unroll
-                        for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(out + c * 16 + g * 2) = make_float2(o[c][e] * sv_run, o[c][2 + e] * sv_run);
-                        if (g == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(m_ref[e], l_run[e]);
+                    for (int e = 0; e < 2; ++e)
+                        if (prow[r][e] < nv && pn[r][e] > it.t0) {             // such a pair, and it sees something of the chunk
+                            float *out = a.part + pout[r][e] + (size_t)it.chunk * (DH + 2);
+#pragma unroll
+                            for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(out + c * 16 + g * 2) = make_float2(o[r][c][e] * sv_run, o[r][c][2 + e] * sv_run);
+                            if (g == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(m_ref[e], l_run[r][e]);
+                        }
+                }
+            } else {
+                // Each warp leaves a tile's result in the stage that its group read last (free until the group's next copy), and the tile's warps add
+                // them up in the groups' order, 8 / WT pairs each
+                constexpr int LD = DH + 4;               // (rows of pairs start in different banks)
+                static_assert(WT == 1 || 8 * LD * 4 * WR <= Lay::STAGE, "a tile of each warp fits the stage");
+                float2 *ml = reinterpret_cast<float2 *>(smem + Lay::O_ML);
+                int *last = reinterpret_cast<int *>(smem + Lay::O_LAST);
+                if (r == 0) group_sync<WR>(wt);          // all readers of the stage are done
+                if (wt < groups) {
+                    float *mine = reinterpret_cast<float *>(ring + (size_t)last_slot * Lay::STAGE) + wr * 8 * LD;
+#pragma unroll
+                    for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                        for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(mine + (kq + e) * LD + c * 16 + g * 2) = make_float2(o[r][c][e] * sv_run, o[r][c][2 + e] * sv_run);
+                        if (g == 0) ml[warp * 8 + kq + e] = make_float2(m_ref[e], l_run[r][e]);
                     }
-            }
-        } else {
-            // Each warp leaves its result in the stage that its group read last (free until the group's next copy), and the warps of a tile add
-            // them up in the groups' order, 8 / WT pairs each
-            constexpr int LD = DH + 4;               // (rows of pairs start in different banks)
-            static_assert(WT == 1 || 8 * LD * 4 * WR <= Lay::STAGE, "a tile of each warp fits the stage");
-            float2 *ml = reinterpret_cast<float2 *>(smem + Lay::O_ML);
-            int *last = reinterpret_cast<int *>(smem + Lay::O_LAST);
-            group_sync<WR>(wt);                      // all readers of the stage are done
-            if (wt < groups) {
-                float *mine = reinterpret_cast<float *>(ring + (size_t)last_slot * Lay::STAGE) + wr * 8 * LD;
-#pragma unroll
-                for (int e = 0; e < 2; ++e) {
-#pragma unroll
-                    for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(mine + (kq + e) * LD + c * 16 + g * 2) = make_float2(o[c][e] * sv_run, o[c][2 + e] * sv_run);
-                    if (g == 0) ml[warp * 8 + kq + e] = make_float2(m_ref[e], l_run[e]);
+                    if (lane == 0 && wr == 0) last[wt] = last_slot;
                 }
-                if (lane == 0 && wr == 0) last[wt] = last_slot;
-            }
-            __syncthreads();
-            constexpr int LPP = DH / 4, PPW = 8 / WT;            // lanes per pair (four dims each), pairs per warp
+                __syncthreads();
+                constexpr int LPP = DH / 4, PPW = 8 / WT;            // lanes per pair (four dims each), pairs per warp
 #pragma unroll 1
-            for (int q0 = 0; q0 < PPW; q0 += 32 / LPP) {
-                const int q = wt * PPW + q0 + lane / LPP, d = lane % LPP * 4, pair = (it.set * WR + wr) * 8 + q;
-                float mm = -INFINITY;
+                for (int q0 = 0; q0 < PPW; q0 += 32 / LPP) {
+                    const int q = wt * PPW + q0 + lane / LPP, d = lane % LPP * 4, pair = ((it.set * WR + wr) * RW + r) * 8 + q;
+                    float mm = -INFINITY;
 #pragma unroll
-                for (int x = 0; x < WT; ++x)
-                    if (x < groups) mm = fmaxf(mm, ml[(x * WR + wr) * 8 + q].x);
-                const float mu = mm == -INFINITY ? 0.f : mm;
-                float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-                float l = 0.f;
+                    for (int x = 0; x < WT; ++x)
+                        if (x < groups) mm = fmaxf(mm, ml[(x * WR + wr) * 8 + q].x);
+                    const float mu = mm == -INFINITY ? 0.f : mm;
+                    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+                    float l = 0.f;
 #pragma unroll
-                for (int x = 0; x < WT; ++x) {
-                    if (x >= groups) continue;
-                    const float2 z = ml[(x * WR + wr) * 8 + q];
-                    const float f = exp2_approx(z.x - mu);
-                    const float4 v = *reinterpret_cast<const float4 *>(smem + (size_t)(x * S + last[x]) * Lay::STAGE + ((wr * 8 + q) * LD + d) * 4);
-                    acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
-                    l += z.y * f;
+                    for (int x = 0; x < WT; ++x) {
+                        if (x >= groups) continue;
+                        const float2 z = ml[(x * WR + wr) * 8 + q];
+                        const float f = exp2_approx(z.x - mu);
+                        const float4 v = *reinterpret_cast<const float4 *>(smem + (size_t)(x * S + last[x]) * Lay::STAGE + ((wr * 8 + q) * LD + d) * 4);
+                        acc.x += v.x * f; acc.y += v.y * f; acc.z += v.z * f; acc.w += v.w * f;
+                        l += z.y * f;
+                    }
+                    const int m = pair / gq;
+                    if (pair < nv * gq && list.row_ctx(list.tpos[it.seq], m) > it.t0) {
+                        float *out = a.part + (((size_t)(it.seq * a.M + m) * a.Hq + it.kvh * gq + (pair - m * gq)) * a.slots + it.chunk) * (DH + 2);
+                        *reinterpret_cast<float2 *>(out + d) = make_float2(acc.x, acc.y);
+                        *reinterpret_cast<float2 *>(out + d + 2) = make_float2(acc.z, acc.w);
+                        if (d == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(mm, l);
+                    }
                 }
-                const int m = pair / gq;
-                if (pair < nv * gq && row_ctx(tpos[it.seq], m) > it.t0) {
-                    float *out = a.part + (((size_t)(it.seq * a.M + m) * a.Hq + it.kvh * gq + (pair - m * gq)) * a.slots + it.chunk) * (DH + 2);
-                    *reinterpret_cast<float2 *>(out + d) = make_float2(acc.x, acc.y);
-                    *reinterpret_cast<float2 *>(out + d + 2) = make_float2(acc.z, acc.w);
-                    if (d == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(mm, l);
-                }
+                __syncthreads();
             }
-            __syncthreads();
         }
         __syncwarp();
-        if (item + 1 < i_end) {
-            const int seq = it.seq, kvh = it.kvh, set = it.set;
-            next_item(it);
-            fresh = it.seq != seq || it.kvh != kvh || it.set != set;
-        }
+        if (item + 1 < i_end) fresh = list.next(it);
     }
     asm volatile("cp.async.wait_all;" ::: "memory");
+    chain_release();
+}
+
+// ---- attention of many pairs per KV head (dh = 128): a set is 128 pairs, the rows of a tcgen05 tile, and an item a chunk of a context
+// for one KV head and a set; blocks of 64 tokens. Scores: K's codes are an e4m3 operand as they lie in the cache, a query
+// is two (its nearest e4m3 and the rest's: 8 bits, a bf16's own, down to 2^-10 of the row's largest element; below that it is off by 2^-18 of the
+// largest), both against the same K tile. Values: f16 operands, the codes converted on the way into shared memory, the probabilities
+// rounded to 2^-12 of themselves; V's tile is token-major, which is the product's MN-major operand.
+// Warps 0-3 are the softmax, a thread a row (its scores are 64 columns of the thread's TMEM lane): the row's maximum and sum need no exchange.
+// Warps 4-7 bring K (cp.async, two blocks ahead) and V (through registers, one ahead); one thread of warp 8 issues the products:
+// block n + 1's scores before block n's values, which wait for its probabilities. Two CTAs per SM: one's softmax runs beside the other's
+// products.
+constexpr int kT8Pairs = 128, kT8Blk = 64, kT8Threads = 288, kT8Copiers = 128, kT8KStages = 3;
+constexpr unsigned long long kT8WaitNs = 2000000000ull;
+struct Tile8Block {                                  // per V buffer: a block's scales, written beside its values
+    float sk[kT8Blk], sv[kT8Blk];
+    float sv_most[4], sv_least[4];                   // of each copy warp's 16 tokens
+    uint32_t bad[4];                                 // values that are no number were left out (see kv8_attn_kernel)
+};
+struct Tile8Smem {
+    static constexpr int TILE = 128 * 128, K = kT8Blk * 128, V = kT8Blk * 256;
+    static constexpr int O_K = 2 * TILE, O_V = O_K + kT8KStages * K, O_P = O_V + 2 * V, O_BLK = O_P + TILE;
+    static constexpr int O_BAR = O_BLK + 2 * (int)sizeof(Tile8Block);        // a multiple of eight
+    static constexpr int N_BAR = 2 * kT8KStages + 2 + 2 + 2 + 3;
+    static constexpr int O_WORDS = O_BAR + N_BAR * 8;                        // TMEM address, abort
+    static constexpr int O_LIST = O_WORDS + 8;
+    static constexpr int TOTAL = O_LIST + kList8Words * 4;
+};
+static_assert(sizeof(Tile8Block) % 16 == 0 && 2 * (Tile8Smem::TOTAL + 1024) <= 228 * 1024, "two CTAs per SM");
+
+__device__ __forceinline__ bool tile8_wait(volatile uint32_t *abort_flag, uint64_t *bar, uint32_t parity) {
+    if (mbar_try_wait(bar, parity)) return true;
+    const unsigned long long t0 = global_timer_ns();
+    uint32_t polls = 0;
+    while (!mbar_try_wait(bar, parity)) {
+        if ((++polls & 63u) == 0) {
+            if (*abort_flag) return false;
+            if (global_timer_ns() - t0 > kT8WaitNs) {
+                *abort_flag = 1u;
+                return false;
+            }
+        }
+    }
+    return true;
+}
+
+__global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_constant__ Attn8Args a) {
+    using Lay = Tile8Smem;
+    constexpr int DH = 128;
+    constexpr uint32_t kFull = 0xffffffffu;
+    extern __shared__ __align__(1024) unsigned char smem_t[];
+    unsigned char *const smem = smem_t;
+    uint64_t *kfull = reinterpret_cast<uint64_t *>(smem + Lay::O_BAR), *kempty = kfull + kT8KStages;
+    uint64_t *vfull = kempty + kT8KStages, *vempty = vfull + 2, *sfull = vempty + 2;         // vempty: the block's values are added up
+    uint64_t *pready = sfull + 2, *qready = pready + 1, *drain = qready + 1;
+    volatile uint32_t *words = reinterpret_cast<volatile uint32_t *>(smem + Lay::O_WORDS), *abort_flag = words + 1;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    chain_wait();
+    List8<kT8Pairs, kT8Blk, 2> list(a, smem + Lay::O_LIST);
+    if (warp == 0) list.build(a, lane);
+    if (tid == 32) {
+        for (int i = 0; i < kT8KStages; ++i) { mbar_init(&kfull[i], kT8Copiers); mbar_init(&kempty[i], 1); }
+        for (int i = 0; i < 2; ++i) { mbar_init(&vfull[i], kT8Copiers); mbar_init(&vempty[i], 1); mbar_init(&sfull[i], 1); }
+        mbar_init(pready, 128);
+        mbar_init(qready, 128);
+        mbar_init(drain, 1);
+        words[1] = (smem_u32(smem) & 1023u) != 0u;   // swizzled tiles need the alignment: nothing runs without it
+        mbar_fence_init();
+    }
+    if (warp == 8) {
+        tmem_alloc(const_cast<uint32_t *>(words), 256);
+        tmem_relinquish();
+        tc_fence_before_sync();
+    }
+    __syncwarp();
+    __syncthreads();
+    tc_fence_after_sync();
+    const uint32_t tmem = words[0], tmem_o = tmem + 128;       // two blocks' scores, 64 columns each; 128 columns of weighted values
+    const int gq = a.gq;
+    const int i_begin = list.begin_of((int)blockIdx.x, (int)gridDim.x), i_end = *abort_flag ? i_begin : list.begin_of((int)blockIdx.x + 1, (int)gridDim.x);
+    const uint32_t base = smem_u32(smem);
+
+    if (warp < 4) {
+        // ================= softmax
+        const uint32_t lane_addr = (uint32_t)(warp * 32) << 16, sw = (uint32_t)(tid & 7), p_row = base + Lay::O_P + (uint32_t)tid * 128;
+        const float sm_scale = (1.0f / sqrtf((float)DH)) * 1.4426950408889634f;
+        Item8 it{};
+        if (i_begin < i_end) list.at(it, i_begin);
+        bool fresh = true, ok = true;
+        int n = 0, pn = kMaxLen, seen = 0;
+        uint32_t prow = kFull;                       // the row's place among the partial results, divided by a.slots; kFull: no such pair
+        float fs = 0.f;
+        for (int item = i_begin; item < i_end && ok; ++item) {
+            if (fresh) {                             // (the last block's scores are there, so the products have read the old queries)
+                const int nv = list.tval[it.seq], pair = it.set * kT8Pairs + tid;
+                const bool there = pair < nv * gq;
+                const int m = there ? pair / gq : 0, row = it.seq * a.M + m, head = it.kvh * gq + (there ? pair - m * gq : 0);
+                pn = there ? list.row_ctx(list.tpos[it.seq], m) : kMaxLen;
+                prow = there ? (uint32_t)(row * a.Hq + head) : kFull;
+                seen = list.row_ctx(list.tpos[it.seq], 0);
+                const uint4 *qp = reinterpret_cast<const uint4 *>(a.q + (long long)row * a.ldq + (long long)head * DH);
+                uint4 x[16];
+                uint32_t am = 0;
+#pragma unroll
+                for (int i = 0; i < 16; ++i) {
+                    x[i] = there ? qp[i] : make_uint4(0, 0, 0, 0);
+                    am = finite_max(finite_max(finite_max(finite_max(am, x[i].x), x[i].y), x[i].z), x[i].w);
+                }
+                const float qs = scale_for(max(am & 0xffffu, am >> 16)), inv = 1.0f / qs;
+                fs = qs * sm_scale;
+#pragma unroll
+                for (int c = 0; c < 8; ++c) {        // 16 dims
+                    uint32_t hi[4], lo[4];
+                    const uint32_t w[8] = {x[2 * c].x, x[2 * c].y, x[2 * c].z, x[2 * c].w, x[2 * c + 1].x, x[2 * c + 1].y, x[2 * c + 1].z, x[2 * c + 1].w};
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        float y[4] = {bf16lo_f32(w[2 * i]), bf16hi_f32(w[2 * i]), bf16lo_f32(w[2 * i + 1]), bf16hi_f32(w[2 * i + 1])}, z[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] = fabsf(y[e]) < INFINITY ? y[e] * inv : __uint_as_float(0x7fffffffu);      // (not finite: NaN)
+                        hi[i] = to_e4m3x4(y, 1.f);
+                        e4m3x4_f32(hi[i], z);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) y[e] -= z[e];
+                        lo[i] = to_e4m3x4(y, 1.f);
+                    }
+                    const uint32_t at = base + (uint32_t)tid * 128 + (((uint32_t)c ^ sw) << 4);
+                    sts128(at, hi[0], hi[1], hi[2], hi[3]);
+                    sts128(at + Lay::TILE, lo[0], lo[1], lo[2], lo[3]);
+                }
+                fence_proxy_async();
+                mbar_arrive(qready);
+            }
+            float mo = kP8Log2, l0 = 0.f, l1 = 0.f, sv_run = 0.f, sv_inv = 0.f;
+            uint32_t bad = 0;
+#pragma unroll 1
+            for (int tb = it.t0; tb < it.t1; tb += kT8Blk, ++n) {
+                const int b = n & 1;
+                const uint32_t ph = (uint32_t)(n >> 1) & 1u;
+                ok = tile8_wait(abort_flag, &vfull[b], ph) && tile8_wait(abort_flag, &sfull[b], ph);
+                if (__any_sync(kFull, !ok)) { ok = false; break; }
+                tc_fence_after_sync();
+                uint32_t x0[32], x1[32];
+                tmem_ld32_issue(tmem + lane_addr + (uint32_t)(b * kT8Blk), x0);
+                tmem_ld32_issue(tmem + lane_addr + (uint32_t)(b * kT8Blk + 32), x1);
+                const Tile8Block *blk = reinterpret_cast<const Tile8Block *>(smem + Lay::O_BLK) + b;
+                const float4 sm4 = *reinterpret_cast<const float4 *>(blk->sv_most), sl4 = *reinterpret_cast<const float4 *>(blk->sv_least);
+                const uint4 bd = *reinterpret_cast<const uint4 *>(blk->bad);
+                bad |= bd.x | bd.y | bd.z | bd.w;
+                const float svm = fmaxf(fmaxf(sm4.x, sm4.y), fmaxf(sm4.z, sm4.w)), svl = fminf(fminf(sl4.x, sl4.y), fminf(sl4.z, sl4.w));
+                tmem_ld_wait();
+                // ---- scores times their K scales, the largest
+                float y[kT8Blk];
+#pragma unroll
+                for (int j = 0; j < kT8Blk; j += 4) {
+                    const float4 sk = *reinterpret_cast<const float4 *>(&blk->sk[j]);
+                    const uint32_t *x = j < 32 ? x0 + j : x1 + (j - 32);
+                    y[j] = __uint_as_float(x[0]) * sk.x;
+                    y[j + 1] = __uint_as_float(x[1]) * sk.y;
+                    y[j + 2] = __uint_as_float(x[2]) * sk.z;
+                    y[j + 3] = __uint_as_float(x[3]) * sk.w;
+                }
+                const int vis = pn - tb;
+                if (__any_sync(kFull, vis < kT8Blk)) {
+#pragma unroll
+                    for (int j = 0; j < kT8Blk; ++j) if (j >= vis) y[j] = -INFINITY;
+                }
+                float m4[4] = {y[0], y[1], y[2], y[3]};
+#pragma unroll
+                for (int j = 4; j < kT8Blk; ++j) m4[j & 3] = fmaxf(m4[j & 3], y[j]);
+                const float ym = fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), fs, mo);
+                const bool first = tb == it.t0;
+                const float d = (first || ym > kP8Max) && ym > -INFINITY ? ym - kP8Log2 : 0.f;
+                mo -= d;
+                float corr = first ? 1.f : exp2_approx(-d);
+                l0 *= corr;
+                l1 *= corr;
+                if (svm > sv_run) {
+                    sv_inv = __fdividef(1.0f, svm);
+                    corr *= sv_run * sv_inv;
+                    sv_run = svm;
+                }
+                // ---- probabilities, as f16 words
+                uint32_t pw[kT8Blk / 2];
+                const bool scaled = svl != sv_run;
+#pragma unroll
+                for (int j = 0; j < kT8Blk; j += 4) {
+                    float p[4];
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) p[e] = exp2_approx(fmaf(y[j + e], fs, mo));
+                    l0 += p[0] + p[1];
+                    l1 += p[2] + p[3];
+                    if (scaled) {
+                        const float4 sv = *reinterpret_cast<const float4 *>(&blk->sv[j]);
+                        p[0] *= sv.x * sv_inv; p[1] *= sv.y * sv_inv; p[2] *= sv.z * sv_inv; p[3] *= sv.w * sv_inv;
+                    }
+                    pw[j / 2] = pack_f16x2(p[0], p[1]);
+                    pw[j / 2 + 1] = pack_f16x2(p[2], p[3]);
+                }
+                // ---- the block before has been added up: its probabilities may be overwritten, what it left can be scaled
+                if (n > 0) {
+                    ok = tile8_wait(abort_flag, &vempty[b ^ 1], (uint32_t)((n - 1) >> 1) & 1u);
+                    if (__any_sync(kFull, !ok)) { ok = false; break; }
+                    tc_fence_after_sync();
+                }
+                if (!first && __any_sync(kFull, corr != 1.f)) {
+#pragma unroll 1
+                    for (int c = 0; c < DH; c += 16) {
+                        uint32_t o[16];
+                        tmem_ld16_issue(tmem_o + lane_addr + (uint32_t)c, o);
+                        tmem_ld_wait();
+#pragma unroll
+                        for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
+                        tmem_st16(tmem_o + lane_addr + (uint32_t)c, o);
+                    }
+                    tmem_st_wait();
+                }
+#pragma unroll
+                for (int c = 0; c < 8; ++c) sts128(p_row + (((uint32_t)c ^ sw) << 4), pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3]);
+                fence_proxy_async();
+                tc_fence_before_sync();
+                mbar_arrive(pready);
+            }
+            if (!ok) break;
+            // ---- the chunk's partial result, as kv8_attn_kernel leaves it: rows of 130 words, which a warp writes two at a time
+            ok = tile8_wait(abort_flag, &vempty[(n - 1) & 1], (uint32_t)((n - 1) >> 1) & 1u);
+            if (__any_sync(kFull, !ok)) break;
+            tc_fence_after_sync();
+            const uint32_t out_row = prow != kFull && pn > it.t0 ? prow * (uint32_t)a.slots + (uint32_t)it.chunk : kFull;
+            if (out_row != kFull) *reinterpret_cast<float2 *>(a.part + (size_t)out_row * (DH + 2) + DH) = make_float2(kP8Log2 - mo, l0 + l1);
+#pragma unroll 1
+            for (int c0 = 0; c0 < DH; c0 += 32) {
+                uint32_t o[32];
+                tmem_ld32_issue(tmem_o + lane_addr + (uint32_t)c0, o);
+                tmem_ld_wait();
+#pragma unroll
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * sv_run);
+#pragma unroll
+                for (int c = 0; c < 8; ++c) sts128(p_row + (((uint32_t)c ^ sw) << 4), o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
+                __syncwarp();
+#pragma unroll 1
+                for (int i = 0; i < 16; ++i) {
+                    const int r = 2 * i + (lane >> 4), col = (lane & 15) * 2;
+                    const uint32_t to = __shfl_sync(kFull, out_row, r);
+                    const int sees = __shfl_sync(kFull, pn, r);
+                    float2 v = *reinterpret_cast<const float2 *>(smem + Lay::O_P + (warp * 32 + r) * 128 + (((col >> 2) ^ (r & 7)) << 4) + (col & 3) * 4);
+                    if (to != kFull) {
+                        if (bad) {                   // values that are no number where the row sees them
+                            for (int t = max(it.t0, seen); t < min(it.t1, sees); ++t) {
+                                const int pg = a.kv.block_table[(size_t)it.seq * a.kv.max_pages + page_of(t, a.page, a.shift)];
+                                if ((unsigned)pg >= (unsigned)a.kv.num_pages) continue;
+                                const uint8_t *code = a.kv.v_pages + (((size_t)pg * a.Hkv + it.kvh) * a.page + (t - page_of(t, a.page, a.shift) * a.page)) * DH + c0 + col;
+                                if ((code[0] & 0x7f) == 0x7f) v.x = NAN;
+                                if ((code[1] & 0x7f) == 0x7f) v.y = NAN;
+                            }
+                        }
+                        *reinterpret_cast<float2 *>(a.part + (size_t)to * (DH + 2) + c0 + col) = v;
+                    }
+                }
+                __syncwarp();
+            }
+            tc_fence_before_sync();
+            if (item + 1 < i_end) fresh = list.next(it);
+        }
+    } else if (warp < 8) {
+        // ================= copies: thread = a 16-byte piece of tokens trow + 16 u
+        const int ct = tid - 128, piece = ct & 7, trow = ct >> 3;
+        struct Block { int tok, t1, kvh, seen, pg[4]; };       // first token (-1: none), the chunk's end, what every row sees, pages of the thread's tokens
+        Item8 w{};
+        int witem = i_begin, wtok = 0;
+        if (i_begin < i_end) { list.at(w, i_begin); wtok = w.t0; }
+        auto walk = [&](Block &x) {
+            x.tok = -1;
+            if (witem >= i_end) return;
+            x.tok = wtok; x.t1 = w.t1; x.kvh = w.kvh;
+            x.seen = list.row_ctx(list.tpos[w.seq], 0);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) x.pg[u] = a.kv.block_table[(size_t)w.seq * a.kv.max_pages + page_of(min(wtok + trow + 16 * u, w.t1 - 1), a.page, a.shift)];
+            wtok += kT8Blk;
+            if (wtok >= w.t1 && ++witem < i_end) { list.next(w); wtok = w.t0; }
+        };
+        auto slot_of = [&](const Block &x, int u, int &off) -> uint32_t {
+            const int pos = min(x.tok + trow + 16 * u, x.t1 - 1);
+            int pg = x.pg[u];
+            if ((unsigned)pg >= (unsigned)a.kv.num_pages) { atomicOr(a.status, kDevBadPage); pg = 0; }
+            off = pos - page_of(pos, a.page, a.shift) * a.page;
+            return (uint32_t)pg * (uint32_t)a.Hkv + (uint32_t)x.kvh;
+        };
+        const uint64_t policy = l2_evict_first();
+        int ks = 0, n = 0;
+        uint32_t kph = 0;
+        auto copy_k = [&](const Block &x) -> bool {
+            if (x.tok < 0) return true;
+            if (__any_sync(kFull, !tile8_wait(abort_flag, &kempty[ks], kph ^ 1u))) return false;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                int off;
+                const uint32_t slot = slot_of(x, u, off);
+                const int t = trow + 16 * u;
+                cp_async16_off_hint<0>(base + Lay::O_K + (uint32_t)(ks * Lay::K) + piece_at<DH>(t, piece),
+                                       a.kv.k_pages + ((size_t)slot * a.page + off) * DH + piece * 16, x.tok + t < x.t1 ? 16u : 0u, policy);
+            }
+            cp_async_arrive(&kfull[ks]);
+            if (++ks == kT8KStages) { ks = 0; kph ^= 1u; }
+            return true;
+        };
+        uint4 v[4];
+        float sc[4];                                 // scales of the thread's tokens: pieces 0 K, 1 V
+        auto load_v = [&](const Block &x) {
+            if (x.tok < 0) return;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                int off;
+                const uint32_t slot = slot_of(x, u, off);
+                v[u] = make_uint4(0, 0, 0, 0);
+                if (x.tok + trow + 16 * u < x.t1) v[u] = *reinterpret_cast<const uint4 *>(a.kv.v_pages + ((size_t)slot * a.page + off) * DH + piece * 16);
+                if (piece < 2) sc[u] = (piece ? a.kv.v_scales : a.kv.k_scales)[slot];
+            }
+        };
+        Block b0, b1, b2;
+        walk(b0);
+        walk(b1);
+        walk(b2);
+        bool ok = copy_k(b0) && copy_k(b1);
+        load_v(b0);
+        while (ok && b0.tok >= 0) {
+            ok = copy_k(b2);
+            if (!ok) break;
+            const int b = n & 1;
+            if (__any_sync(kFull, !tile8_wait(abort_flag, &vempty[b], ((uint32_t)(n >> 1) & 1u) ^ 1u))) break;
+            Tile8Block *blk = reinterpret_cast<Tile8Block *>(smem + Lay::O_BLK) + b;
+            const uint32_t dst = base + Lay::O_V + (uint32_t)(b * Lay::V) + (uint32_t)(piece >> 2) * (Lay::V / 2);
+            uint32_t most = 0, least = 0x7f800000u;
+            bool bad = false;
+            const bool edge = b0.tok + kT8Blk > b0.seen;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int t = trow + 16 * u;
+                uint32_t c[4] = {v[u].x, v[u].y, v[u].z, v[u].w}, h[8];
+                if (edge && b0.tok + t >= b0.seen) {
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const uint32_t nan = __vcmpeq4(c[i] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+                        c[i] &= ~nan;
+                        bad = bad || nan != 0u;
+                    }
+                }
+#pragma unroll
+                for (int i = 0; i < 4; ++i) { h[2 * i] = e4m3lo_f16x2(c[i]); h[2 * i + 1] = e4m3hi_f16x2(c[i]); }
+                // dims 16 piece and on: two pieces of a row of 64 dims (the rows' other halves in the other order: all banks at once)
+                const uint32_t q = 2 * (piece & 3), swz = t & 7, at = dst + (uint32_t)t * 128;
+                const bool second = piece >= 4;
+                const uint32_t a0 = at + (((q + (second ? 1 : 0)) ^ swz) << 4), a1 = at + (((q + (second ? 0 : 1)) ^ swz) << 4);
+                sts128(a0, second ? h[4] : h[0], second ? h[5] : h[1], second ? h[6] : h[2], second ? h[7] : h[3]);
+                sts128(a1, second ? h[0] : h[4], second ? h[1] : h[5], second ? h[2] : h[6], second ? h[3] : h[7]);
+                if (piece == 0) blk->sk[t] = sc[u];
+                if (piece == 1) {
+                    blk->sv[t] = sc[u];
+                    most = max(most, __float_as_uint(sc[u]));          // (scales are positive: their bits are in their order)
+                    least = min(least, __float_as_uint(sc[u]));
+                }
+            }
+            most = __reduce_max_sync(kFull, most);
+            least = __reduce_min_sync(kFull, least);
+            bad = __any_sync(kFull, bad);
+            if (lane == 0) {
+                blk->sv_most[warp - 4] = __uint_as_float(most);
+                blk->sv_least[warp - 4] = __uint_as_float(least);
+                blk->bad[warp - 4] = bad ? 1u : 0u;
+            }
+            fence_proxy_async();
+            mbar_arrive(&vfull[b]);
+            b0 = b1;
+            b1 = b2;
+            ++n;
+            load_v(b0);
+            walk(b2);
+        }
+        asm volatile("cp.async.wait_all;" ::: "memory");
+    } else {
+        // ================= products: one thread
+        if (lane == 0 && i_begin < i_end) {
+            constexpr uint32_t kIdS = (1u << 4) | ((uint32_t)(kT8Blk >> 3) << 17) | (8u << 24);                     // e4m3, both K-major
+            constexpr uint32_t kIdO = (1u << 4) | (1u << 16) | ((uint32_t)(DH >> 3) << 17) | (8u << 24);            // f16, B MN-major
+            const uint32_t qd = umma_desc_lo(base), kd = umma_desc_lo(base + Lay::O_K), pd = umma_desc_lo(base + Lay::O_P);
+            // V: two atoms of 64 dims V / 2 apart, groups of eight tokens 1024 bytes apart
+            const uint32_t vd = ((base + Lay::O_V) >> 4) | ((uint32_t)(Lay::V / 2 >> 4) << 16);
+            int ks = 0;
+            uint32_t kph = 0, qph = 0;
+            auto scores = [&](int n, bool fresh) -> bool {
+                if (fresh) {
+                    if (!tile8_wait(abort_flag, qready, qph)) return false;
+                    qph ^= 1u;
+                }
+                if (!tile8_wait(abort_flag, &kfull[ks], kph)) return false;
+                fence_proxy_async();                 // the copies' shared-memory writes, before the tensor core reads them
+                tc_fence_after_sync();
+                const uint32_t d = tmem + (uint32_t)((n & 1) * kT8Blk), k = kd + (uint32_t)(ks * (Lay::K >> 4));
+#pragma unroll
+                for (int j = 0; j < 8; ++j) umma_f8(d, qd + (uint32_t)((j >> 2) * (Lay::TILE >> 4) + (j & 3) * 2), k + (uint32_t)((j & 3) * 2), kIdS, j > 0);
+                umma_commit(&sfull[n & 1]);
+                umma_commit(&kempty[ks]);
+                if (++ks == kT8KStages) { ks = 0; kph ^= 1u; }
+                return true;
+            };
+            Item8 it{};
+            list.at(it, i_begin);
+            int item = i_begin, tok = it.t0, n = 0;
+            bool ok = scores(0, true), first = true;
+            while (ok) {
+                // the block behind this one
+                bool more = true, fresh = false, first_next = false;
+                tok += kT8Blk;
+                if (tok >= it.t1) {
+                    more = ++item < i_end;
+                    if (more) {
+                        fresh = list.next(it);
+                        tok = it.t0;
+                        first_next = true;
+                    }
+                }
+                if (more && !fresh && !(ok = scores(n + 1, false))) break;
+                if (!(ok = tile8_wait(abort_flag, pready, (uint32_t)n & 1u) && tile8_wait(abort_flag, &vfull[n & 1], (uint32_t)(n >> 1) & 1u))) break;
+                tc_fence_after_sync();
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    umma_bf16(tmem_o, pd + (uint32_t)(j * 2), vd + (uint32_t)((n & 1) * (Lay::V >> 4) + j * (2048 >> 4)), kIdO, !(first && j == 0));
+                umma_commit(&vempty[n & 1]);
+                if (!more) break;
+                if (fresh) ok = scores(n + 1, true);         // (the new queries wait for this block's values)
+                first = first_next;
+                ++n;
+            }
+            // every product issued above is done once this arrival lands
+            umma_commit(drain);
+            tile8_wait(abort_flag, drain, 0);
+        }
+        __syncwarp();
+    }
+    __syncwarp();
+    tc_fence_before_sync();
+    __syncthreads();
+    if (warp == 8) {
+        tc_fence_after_sync();
+        tmem_dealloc(tmem, 256);
+    }
+    if (tid == 0 && *abort_flag) atomicOr(a.status, kDevTimeout8);
     chain_release();
 }
 
@@ -856,20 +1368,31 @@ __global__ void __launch_bounds__(DH) kv8_merge_kernel(const Attn8Args a) {
     }
 }
 
-template <int DH, int WR>
-int attn8_launch(const Attn8Args &a, int rows, int n_sm, cudaStream_t st) {
-    auto kern = kv8_attn_kernel<DH, WR>;
-    cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, Attn8Smem<DH, WR>::TOTAL);
-    if (e == cudaSuccess) e = launch_chained(kern, dim3(Attn8Smem<DH, WR>::CTAS * n_sm), dim3(kA8Threads), (size_t)Attn8Smem<DH, WR>::TOTAL, st, a);
+template <int DH>
+int attn8_launch(void (*kern)(const Attn8Args), int ctas, int threads, int smem, const Attn8Args &a, int rows, bool *raised, cudaStream_t st) {
+    cudaError_t e = cudaSuccess;
+    if (!*raised) {                                  // once per context (every context sets the same limit)
+        e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+        *raised = e == cudaSuccess;
+    }
+    if (e == cudaSuccess) e = launch_chained(kern, dim3(ctas), dim3(threads), (size_t)smem, st, a);
     if (e == cudaSuccess) e = launch_chained(kv8_merge_kernel<DH>, dim3(a.Hq, rows), dim3(DH), 0, st, a);
     return (int)e;
 }
+template <int DH, int RW, int WR>
+int attn8_warps(const Attn8Args &a, int rows, int n_sm, bool *raised, cudaStream_t st) {
+    using Lay = Attn8Smem<DH, RW, WR>;
+    return attn8_launch<DH>(kv8_attn_kernel<DH, RW, WR>, Lay::CTAS * n_sm, kA8Threads, Lay::TOTAL, a, rows, raised, st);
+}
 
+// One tile of pairs: four groups of one warp; two tiles: two groups of two; more: two groups of two warps with two tiles each.
 template <int DH>
-int attn8_pick(const Attn8Args &a, int rows, int n_sm, cudaStream_t st) {
+int attn8_pick(const Attn8Args &a, int rows, int n_sm, bool *raised, cudaStream_t st) {
     const int pairs = a.M * a.gq;
-    if (pairs <= 8) return attn8_launch<DH, 1>(a, rows, n_sm, st);
-    return attn8_launch<DH, 2>(a, rows, n_sm, st);
+    if (pairs <= 8) return attn8_warps<DH, 1, 1>(a, rows, n_sm, raised, st);
+    if (pairs <= 32) return attn8_warps<DH, 1, 2>(a, rows, n_sm, raised + 1, st);
+    if constexpr (DH == 128) return attn8_launch<DH>(kv8_tile_kernel, 2 * n_sm, kT8Threads, Tile8Smem::TOTAL, a, rows, raised + 2, st);
+    else return attn8_warps<DH, 2, 2>(a, rows, n_sm, raised + 2, st);
 }
 
 }  // namespace
@@ -913,7 +1436,7 @@ int kv8_attention(const Kv8AttnCall &c, cudaStream_t st, long long *launches) {
     a.slots = kv8_attention_slots(c.sh, c.M); a.tiles16 = c.sh.page % 16 == 0; a.B = c.B; a.M = c.M; a.q = c.q; a.ldq = c.ldq; a.n_new = c.n_new; a.kv = c.kv; a.part = c.part;
     a.out = c.out; a.xop = c.xop; a.ld_xop = c.ld_xop; a.status = c.status;
     *launches += 2;
-    return c.sh.dh == 128 ? attn8_pick<128>(a, c.B * c.M, c.n_sm, st) : attn8_pick<64>(a, c.B * c.M, c.n_sm, st);
+    return c.sh.dh == 128 ? attn8_pick<128>(a, c.B * c.M, c.n_sm, c.raised, st) : attn8_pick<64>(a, c.B * c.M, c.n_sm, c.raised, st);
 }
 
 }  // namespace fmtp
