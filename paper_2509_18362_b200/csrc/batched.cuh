@@ -27,7 +27,7 @@ struct TmapCache {
     int n, next;
     bool gemm_raised[2];                     // skinny_gemm_kernel<2>, <4>: shared-memory limit raised
     bool attn_raised[2];                     // attn_kernel for one row / several rows per sequence
-    bool attn8_raised[3];                    // see Kv8AttnCall
+    bool attn8_raised[4];                    // see Kv8AttnCall
 };
 
 struct BatchedWs {

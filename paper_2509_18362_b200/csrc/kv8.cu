@@ -884,10 +884,9 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
 // products.
 constexpr int kT8Pairs = 128, kT8Blk = 64, kT8Threads = 288, kT8Copiers = 128, kT8KStages = 3;
 constexpr unsigned long long kT8WaitNs = 2000000000ull;
-struct Tile8Block {                                  // per V buffer: a block's scales, written beside its values
-    float sk[kT8Blk], sv[kT8Blk];
-    float sv_most[4], sv_least[4];                   // of each copy warp's 16 tokens
-    uint32_t bad[4];                                 // values that are no number were left out (see kv8_attn_kernel)
+struct Tile8Block {                                  // per V buffer: scales of the block's 16-token tiles, written beside its values
+    float sk[4], sv[4];
+    uint32_t bad[4];                                 // values that are no number were left out (see kv8_attn_kernel); of each copy warp
 };
 struct Tile8Smem {
     static constexpr int TILE = 128 * 128, K = kT8Blk * 128, V = kT8Blk * 256;
@@ -959,46 +958,63 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
         Item8 it{};
         if (i_begin < i_end) list.at(it, i_begin);
         bool fresh = true, ok = true;
-        int n = 0, pn = kMaxLen, seen = 0;
+        int n = 0, pn = kMaxLen;
         uint32_t prow = kFull;                       // the row's place among the partial results, divided by a.slots; kFull: no such pair
         float fs = 0.f;
         for (int item = i_begin; item < i_end && ok; ++item) {
-            if (fresh) {                             // (the last block's scores are there, so the products have read the old queries)
-                const int nv = list.tval[it.seq], pair = it.set * kT8Pairs + tid;
-                const bool there = pair < nv * gq;
-                const int m = there ? pair / gq : 0, row = it.seq * a.M + m, head = it.kvh * gq + (there ? pair - m * gq : 0);
-                pn = there ? list.row_ctx(list.tpos[it.seq], m) : kMaxLen;
-                prow = there ? (uint32_t)(row * a.Hq + head) : kFull;
-                seen = list.row_ctx(list.tpos[it.seq], 0);
-                const uint4 *qp = reinterpret_cast<const uint4 *>(a.q + (long long)row * a.ldq + (long long)head * DH);
-                uint4 x[16];
-                uint32_t am = 0;
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    x[i] = there ? qp[i] : make_uint4(0, 0, 0, 0);
-                    am = finite_max(finite_max(finite_max(finite_max(am, x[i].x), x[i].y), x[i].z), x[i].w);
-                }
-                const float qs = scale_for(max(am & 0xffffu, am >> 16)), inv = 1.0f / qs;
-                fs = qs * sm_scale;
-#pragma unroll
-                for (int c = 0; c < 8; ++c) {        // 16 dims
-                    uint32_t hi[4], lo[4];
-                    const uint32_t w[8] = {x[2 * c].x, x[2 * c].y, x[2 * c].z, x[2 * c].w, x[2 * c + 1].x, x[2 * c + 1].y, x[2 * c + 1].z, x[2 * c + 1].w};
+            if (fresh) {
+                // queries, two rows at a time, eight dims per lane (the last block's scores are there, so the old ones have been read)
+                const int nv = list.tval[it.seq], pair0 = it.set * kT8Pairs + warp * 32;
+                auto pair_at = [&](int pair, int &m, int &row, int &head) -> bool {
+                    const bool there = pair < nv * gq;
+                    m = there ? pair / gq : 0;
+                    row = it.seq * a.M + m;
+                    head = it.kvh * gq + (there ? pair - m * gq : 0);
+                    return there;
+                };
+                int m, row, head;
+                float qs = 1.f;
+                const int piece = lane & 15;
+#pragma unroll 1
+                for (int r0 = 0; r0 < 32; r0 += 8) {
+                    uint4 x[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        float y[4] = {bf16lo_f32(w[2 * i]), bf16hi_f32(w[2 * i]), bf16lo_f32(w[2 * i + 1]), bf16hi_f32(w[2 * i + 1])}, z[4];
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) y[e] = fabsf(y[e]) < INFINITY ? y[e] * inv : __uint_as_float(0x7fffffffu);      // (not finite: NaN)
-                        hi[i] = to_e4m3x4(y, 1.f);
-                        e4m3x4_f32(hi[i], z);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) y[e] -= z[e];
-                        lo[i] = to_e4m3x4(y, 1.f);
+                        const bool there = pair_at(pair0 + r0 + 2 * i + (lane >> 4), m, row, head);
+                        x[i] = make_uint4(0, 0, 0, 0);
+                        if (there) x[i] = *reinterpret_cast<const uint4 *>(a.q + (long long)row * a.ldq + (long long)head * DH + piece * 8);
                     }
-                    const uint32_t at = base + (uint32_t)tid * 128 + (((uint32_t)c ^ sw) << 4);
-                    sts128(at, hi[0], hi[1], hi[2], hi[3]);
-                    sts128(at + Lay::TILE, lo[0], lo[1], lo[2], lo[3]);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) {
+                        const int r = warp * 32 + r0 + 2 * i + (lane >> 4);
+                        uint32_t am = finite_max(finite_max(finite_max(finite_max(0, x[i].x), x[i].y), x[i].z), x[i].w);
+                        am = max(am & 0xffffu, am >> 16);
+#pragma unroll
+                        for (int o = 1; o < 16; o <<= 1) am = max(am, __shfl_xor_sync(kFull, am, o));
+                        const float rs = scale_for(am), inv = 1.0f / rs, other = __shfl_sync(kFull, rs, (lane & 1) * 16);
+                        if ((lane >> 1) == (r0 >> 1) + i) qs = other;
+                        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                        uint32_t hi[2], lo[2];
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            float y[4] = {bf16lo_f32(w[2 * h]), bf16hi_f32(w[2 * h]), bf16lo_f32(w[2 * h + 1]), bf16hi_f32(w[2 * h + 1])}, z[4];
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) y[e] = fabsf(y[e]) < INFINITY ? y[e] * inv : __uint_as_float(0x7fffffffu);      // (not finite: NaN)
+                            hi[h] = to_e4m3x4(y, 1.f);
+                            e4m3x4_f32(hi[h], z);
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) y[e] -= z[e];
+                            lo[h] = to_e4m3x4(y, 1.f);
+                        }
+                        unsigned char *at = smem + r * 128 + (((piece >> 1) ^ (r & 7)) << 4) + (piece & 1) * 8;
+                        *reinterpret_cast<uint2 *>(at) = make_uint2(hi[0], hi[1]);
+                        *reinterpret_cast<uint2 *>(at + Lay::TILE) = make_uint2(lo[0], lo[1]);
+                    }
                 }
+                fs = qs * sm_scale;
+                const bool there = pair_at(pair0 + lane, m, row, head);
+                pn = there ? list.row_ctx(list.tpos[it.seq], m) : kMaxLen;
+                prow = there ? (uint32_t)(row * a.Hq + head) : kFull;
                 fence_proxy_async();
                 mbar_arrive(qready);
             }
@@ -1007,66 +1023,56 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
 #pragma unroll 1
             for (int tb = it.t0; tb < it.t1; tb += kT8Blk, ++n) {
                 const int b = n & 1;
-                const uint32_t ph = (uint32_t)(n >> 1) & 1u;
+                const uint32_t ph = (uint32_t)(n >> 1) & 1u, tmem_s = tmem + lane_addr + (uint32_t)(b * kT8Blk);
                 ok = tile8_wait(abort_flag, &vfull[b], ph) && tile8_wait(abort_flag, &sfull[b], ph);
                 if (__any_sync(kFull, !ok)) { ok = false; break; }
                 tc_fence_after_sync();
-                uint32_t x0[32], x1[32];
-                tmem_ld32_issue(tmem + lane_addr + (uint32_t)(b * kT8Blk), x0);
-                tmem_ld32_issue(tmem + lane_addr + (uint32_t)(b * kT8Blk + 32), x1);
                 const Tile8Block *blk = reinterpret_cast<const Tile8Block *>(smem + Lay::O_BLK) + b;
-                const float4 sm4 = *reinterpret_cast<const float4 *>(blk->sv_most), sl4 = *reinterpret_cast<const float4 *>(blk->sv_least);
+                const float4 sk4 = *reinterpret_cast<const float4 *>(blk->sk), sv4 = *reinterpret_cast<const float4 *>(blk->sv);
                 const uint4 bd = *reinterpret_cast<const uint4 *>(blk->bad);
                 bad |= bd.x | bd.y | bd.z | bd.w;
-                const float svm = fmaxf(fmaxf(sm4.x, sm4.y), fmaxf(sm4.z, sm4.w)), svl = fminf(fminf(sl4.x, sl4.y), fminf(sl4.z, sl4.w));
-                tmem_ld_wait();
-                // ---- scores times their K scales, the largest
-                float y[kT8Blk];
-#pragma unroll
-                for (int j = 0; j < kT8Blk; j += 4) {
-                    const float4 sk = *reinterpret_cast<const float4 *>(&blk->sk[j]);
-                    const uint32_t *x = j < 32 ? x0 + j : x1 + (j - 32);
-                    y[j] = __uint_as_float(x[0]) * sk.x;
-                    y[j + 1] = __uint_as_float(x[1]) * sk.y;
-                    y[j + 2] = __uint_as_float(x[2]) * sk.z;
-                    y[j + 3] = __uint_as_float(x[3]) * sk.w;
-                }
+                // a code product times c is a score in log2 units (c > 0: nothing seen, -inf, stays that)
+                const float c[4] = {fmaxf(sk4.x * fs, 1e-37f), fmaxf(sk4.y * fs, 1e-37f), fmaxf(sk4.z * fs, 1e-37f), fmaxf(sk4.w * fs, 1e-37f)};
                 const int vis = pn - tb;
                 if (__any_sync(kFull, vis < kT8Blk)) {
+#pragma unroll 1
+                    for (int j0 = 0; j0 < kT8Blk; j0 += 16) {
+                        uint32_t x[16];
+                        tmem_ld16_issue(tmem_s + (uint32_t)j0, x);
+                        tmem_ld_wait();
 #pragma unroll
-                    for (int j = 0; j < kT8Blk; ++j) if (j >= vis) y[j] = -INFINITY;
+                        for (int j = 0; j < 16; ++j) if (j0 + j >= vis) x[j] = 0xff800000u;
+                        tmem_st16(tmem_s + (uint32_t)j0, x);
+                    }
+                    tmem_st_wait();
                 }
-                float m4[4] = {y[0], y[1], y[2], y[3]};
+                // ---- the largest score (the scores are read from tensor memory twice: 64 of them would not fit the registers)
+                float ym = -INFINITY;
 #pragma unroll
-                for (int j = 4; j < kT8Blk; ++j) m4[j & 3] = fmaxf(m4[j & 3], y[j]);
-                const float ym = fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), fs, mo);
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t x[32];
+                    tmem_ld32_issue(tmem_s + (uint32_t)(h * 32), x);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int g = 0; g < 2; ++g) {
+                        float m4[4];
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) m4[j] = fmaxf(fmaxf(__uint_as_float(x[g * 16 + j]), __uint_as_float(x[g * 16 + 4 + j])),
+                                                                  fmaxf(__uint_as_float(x[g * 16 + 8 + j]), __uint_as_float(x[g * 16 + 12 + j])));
+                        ym = fmaxf(ym, fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), c[2 * h + g], mo));
+                    }
+                }
                 const bool first = tb == it.t0;
                 const float d = (first || ym > kP8Max) && ym > -INFINITY ? ym - kP8Log2 : 0.f;
                 mo -= d;
                 float corr = first ? 1.f : exp2_approx(-d);
                 l0 *= corr;
                 l1 *= corr;
+                const float svm = fmaxf(fmaxf(sv4.x, sv4.y), fmaxf(sv4.z, sv4.w));
                 if (svm > sv_run) {
                     sv_inv = __fdividef(1.0f, svm);
                     corr *= sv_run * sv_inv;
                     sv_run = svm;
-                }
-                // ---- probabilities, as f16 words
-                uint32_t pw[kT8Blk / 2];
-                const bool scaled = svl != sv_run;
-#pragma unroll
-                for (int j = 0; j < kT8Blk; j += 4) {
-                    float p[4];
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) p[e] = exp2_approx(fmaf(y[j + e], fs, mo));
-                    l0 += p[0] + p[1];
-                    l1 += p[2] + p[3];
-                    if (scaled) {
-                        const float4 sv = *reinterpret_cast<const float4 *>(&blk->sv[j]);
-                        p[0] *= sv.x * sv_inv; p[1] *= sv.y * sv_inv; p[2] *= sv.z * sv_inv; p[3] *= sv.w * sv_inv;
-                    }
-                    pw[j / 2] = pack_f16x2(p[0], p[1]);
-                    pw[j / 2 + 1] = pack_f16x2(p[2], p[3]);
                 }
                 // ---- the block before has been added up: its probabilities may be overwritten, what it left can be scaled
                 if (n > 0) {
@@ -1076,18 +1082,39 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 }
                 if (!first && __any_sync(kFull, corr != 1.f)) {
 #pragma unroll 1
-                    for (int c = 0; c < DH; c += 16) {
+                    for (int o0 = 0; o0 < DH; o0 += 16) {
                         uint32_t o[16];
-                        tmem_ld16_issue(tmem_o + lane_addr + (uint32_t)c, o);
+                        tmem_ld16_issue(tmem_o + lane_addr + (uint32_t)o0, o);
                         tmem_ld_wait();
 #pragma unroll
                         for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * corr);
-                        tmem_st16(tmem_o + lane_addr + (uint32_t)c, o);
+                        tmem_st16(tmem_o + lane_addr + (uint32_t)o0, o);
                     }
                     tmem_st_wait();
                 }
+                // ---- probabilities, as f16
+                const float f[4] = {sv4.x * sv_inv, sv4.y * sv_inv, sv4.z * sv_inv, sv4.w * sv_inv};
+                const bool scaled = fminf(fminf(sv4.x, sv4.y), fminf(sv4.z, sv4.w)) != sv_run;
 #pragma unroll
-                for (int c = 0; c < 8; ++c) sts128(p_row + (((uint32_t)c ^ sw) << 4), pw[4 * c], pw[4 * c + 1], pw[4 * c + 2], pw[4 * c + 3]);
+                for (int h = 0; h < 2; ++h) {
+                    uint32_t x[32];
+                    tmem_ld32_issue(tmem_s + (uint32_t)(h * 32), x);
+                    tmem_ld_wait();
+#pragma unroll
+                    for (int q = 0; q < 4; ++q) {
+                        const float cc = c[2 * h + (q >> 1)];
+                        float p[8];
+#pragma unroll
+                        for (int e = 0; e < 8; ++e) p[e] = exp2_approx(fmaf(__uint_as_float(x[q * 8 + e]), cc, mo));
+                        l0 += (p[0] + p[1]) + (p[2] + p[3]);
+                        l1 += (p[4] + p[5]) + (p[6] + p[7]);
+                        if (scaled) {
+#pragma unroll
+                            for (int e = 0; e < 8; ++e) p[e] *= f[2 * h + (q >> 1)];
+                        }
+                        sts128(p_row + (((uint32_t)(h * 4 + q) ^ sw) << 4), pack_f16x2(p[0], p[1]), pack_f16x2(p[2], p[3]), pack_f16x2(p[4], p[5]), pack_f16x2(p[6], p[7]));
+                    }
+                }
                 fence_proxy_async();
                 tc_fence_before_sync();
                 mbar_arrive(pready);
@@ -1098,7 +1125,8 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             if (__any_sync(kFull, !ok)) break;
             tc_fence_after_sync();
             const uint32_t out_row = prow != kFull && pn > it.t0 ? prow * (uint32_t)a.slots + (uint32_t)it.chunk : kFull;
-            if (out_row != kFull) *reinterpret_cast<float2 *>(a.part + (size_t)out_row * (DH + 2) + DH) = make_float2(kP8Log2 - mo, l0 + l1);
+            float *mine = a.part + (size_t)out_row * (DH + 2);
+            if (out_row != kFull) *reinterpret_cast<float2 *>(mine + DH) = make_float2(kP8Log2 - mo, l0 + l1);
 #pragma unroll 1
             for (int c0 = 0; c0 < DH; c0 += 32) {
                 uint32_t o[32];
@@ -1109,24 +1137,23 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
 #pragma unroll
                 for (int c = 0; c < 8; ++c) sts128(p_row + (((uint32_t)c ^ sw) << 4), o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
                 __syncwarp();
-#pragma unroll 1
+                const int half = lane >> 4, col = (lane & 15) * 2;
+#pragma unroll 8
                 for (int i = 0; i < 16; ++i) {
-                    const int r = 2 * i + (lane >> 4), col = (lane & 15) * 2;
+                    const int r = 2 * i + half;
                     const uint32_t to = __shfl_sync(kFull, out_row, r);
-                    const int sees = __shfl_sync(kFull, pn, r);
-                    float2 v = *reinterpret_cast<const float2 *>(smem + Lay::O_P + (warp * 32 + r) * 128 + (((col >> 2) ^ (r & 7)) << 4) + (col & 3) * 4);
-                    if (to != kFull) {
-                        if (bad) {                   // values that are no number where the row sees them
-                            for (int t = max(it.t0, seen); t < min(it.t1, sees); ++t) {
-                                const int pg = a.kv.block_table[(size_t)it.seq * a.kv.max_pages + page_of(t, a.page, a.shift)];
-                                if ((unsigned)pg >= (unsigned)a.kv.num_pages) continue;
-                                const uint8_t *code = a.kv.v_pages + (((size_t)pg * a.Hkv + it.kvh) * a.page + (t - page_of(t, a.page, a.shift) * a.page)) * DH + c0 + col;
-                                if ((code[0] & 0x7f) == 0x7f) v.x = NAN;
-                                if ((code[1] & 0x7f) == 0x7f) v.y = NAN;
-                            }
-                        }
-                        *reinterpret_cast<float2 *>(a.part + (size_t)to * (DH + 2) + c0 + col) = v;
-                    }
+                    const float2 v = *reinterpret_cast<const float2 *>(smem + Lay::O_P + (warp * 32 + r) * 128 + (((col >> 2) ^ (r & 7)) << 4) + (col & 3) * 4);
+                    if (to != kFull) *reinterpret_cast<float2 *>(a.part + (size_t)to * (DH + 2) + c0 + col) = v;
+                }
+                __syncwarp();
+            }
+            if (bad) {                               // values that are no number, where the row sees them
+                __syncwarp();
+                for (int t = max(it.t0, list.row_ctx(list.tpos[it.seq], 0)); out_row != kFull && t < min(it.t1, pn); ++t) {
+                    const int blk = page_of(t, a.page, a.shift), pg = a.kv.block_table[(size_t)it.seq * a.kv.max_pages + blk];
+                    if ((unsigned)pg >= (unsigned)a.kv.num_pages) continue;
+                    const uint8_t *code = a.kv.v_pages + (((size_t)pg * a.Hkv + it.kvh) * a.page + (t - blk * a.page)) * DH;
+                    for (int i = 0; i < DH; ++i) if ((code[i] & 0x7f) == 0x7f) mine[i] = NAN;
                 }
                 __syncwarp();
             }
@@ -1176,7 +1203,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             return true;
         };
         uint4 v[4];
-        float sc[4];                                 // scales of the thread's tokens: pieces 0 K, 1 V
+        float sc[4] = {};                            // threads 0 and 1: K and V scales of the block's 16-token tiles
         auto load_v = [&](const Block &x) {
             if (x.tok < 0) return;
 #pragma unroll
@@ -1185,7 +1212,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 const uint32_t slot = slot_of(x, u, off);
                 v[u] = make_uint4(0, 0, 0, 0);
                 if (x.tok + trow + 16 * u < x.t1) v[u] = *reinterpret_cast<const uint4 *>(a.kv.v_pages + ((size_t)slot * a.page + off) * DH + piece * 16);
-                if (piece < 2) sc[u] = (piece ? a.kv.v_scales : a.kv.k_scales)[slot];
+                if (trow == 0 && piece < 2) sc[u] = (piece ? a.kv.v_scales : a.kv.k_scales)[slot];
             }
         };
         Block b0, b1, b2;
@@ -1201,7 +1228,6 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             if (__any_sync(kFull, !tile8_wait(abort_flag, &vempty[b], ((uint32_t)(n >> 1) & 1u) ^ 1u))) break;
             Tile8Block *blk = reinterpret_cast<Tile8Block *>(smem + Lay::O_BLK) + b;
             const uint32_t dst = base + Lay::O_V + (uint32_t)(b * Lay::V) + (uint32_t)(piece >> 2) * (Lay::V / 2);
-            uint32_t most = 0, least = 0x7f800000u;
             bool bad = false;
             const bool edge = b0.tok + kT8Blk > b0.seen;
 #pragma unroll
@@ -1224,21 +1250,10 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 const uint32_t a0 = at + (((q + (second ? 1 : 0)) ^ swz) << 4), a1 = at + (((q + (second ? 0 : 1)) ^ swz) << 4);
                 sts128(a0, second ? h[4] : h[0], second ? h[5] : h[1], second ? h[6] : h[2], second ? h[7] : h[3]);
                 sts128(a1, second ? h[0] : h[4], second ? h[1] : h[5], second ? h[2] : h[6], second ? h[3] : h[7]);
-                if (piece == 0) blk->sk[t] = sc[u];
-                if (piece == 1) {
-                    blk->sv[t] = sc[u];
-                    most = max(most, __float_as_uint(sc[u]));          // (scales are positive: their bits are in their order)
-                    least = min(least, __float_as_uint(sc[u]));
-                }
             }
-            most = __reduce_max_sync(kFull, most);
-            least = __reduce_min_sync(kFull, least);
+            if (ct < 2) *reinterpret_cast<float4 *>(ct ? blk->sv : blk->sk) = make_float4(sc[0], sc[1], sc[2], sc[3]);
             bad = __any_sync(kFull, bad);
-            if (lane == 0) {
-                blk->sv_most[warp - 4] = __uint_as_float(most);
-                blk->sv_least[warp - 4] = __uint_as_float(least);
-                blk->bad[warp - 4] = bad ? 1u : 0u;
-            }
+            if (lane == 0) blk->bad[warp - 4] = bad ? 1u : 0u;
             fence_proxy_async();
             mbar_arrive(&vfull[b]);
             b0 = b1;
@@ -1391,8 +1406,8 @@ int attn8_pick(const Attn8Args &a, int rows, int n_sm, bool *raised, cudaStream_
     const int pairs = a.M * a.gq;
     if (pairs <= 8) return attn8_warps<DH, 1, 1>(a, rows, n_sm, raised, st);
     if (pairs <= 32) return attn8_warps<DH, 1, 2>(a, rows, n_sm, raised + 1, st);
-    if constexpr (DH == 128) return attn8_launch<DH>(kv8_tile_kernel, 2 * n_sm, kT8Threads, Tile8Smem::TOTAL, a, rows, raised + 2, st);
-    else return attn8_warps<DH, 2, 2>(a, rows, n_sm, raised + 2, st);
+    if (DH == 128 && a.tiles16) return attn8_launch<DH>(kv8_tile_kernel, 2 * n_sm, kT8Threads, Tile8Smem::TOTAL, a, rows, raised + 3, st);
+    return attn8_warps<DH, 2, 2>(a, rows, n_sm, raised + 2, st);
 }
 
 }  // namespace

@@ -38,7 +38,7 @@ struct Kv8AttnCall {
     int ld_xop;
     uint32_t *status;
     int n_sm;
-    bool *raised;                         // [3] the context's: kernels whose shared-memory limit has been raised
+    bool *raised;                         // [4] the context's: kernels whose shared-memory limit has been raised
 };
 int kv8_attention_slots(const Kv8Shape &sh, int M);
 int kv8_attention(const Kv8AttnCall &c, cudaStream_t st, long long *launches);
