@@ -1210,7 +1210,7 @@ size_t batched_layout(BatchedWs &ws, unsigned char *base, const BatchedShape &sh
         const size_t need = (size_t)r * kv8_attention_slots(s8, m);
         if (need > ws.part_rows) ws.part_rows = need;
     }
-    ws.att_part = reinterpret_cast<float *>(take(ws.part_rows * sh.Hq * (sh.dh + 2) * 4));
+    ws.att_part = reinterpret_cast<float *>(take(ws.part_rows * sh.Hq * (sh.dh + 4) * 4));
     ws.qkv = reinterpret_cast<bf16_t *>(take((size_t)rows * (qdim + 2 * kvdim) * 2));
     ws.keys_bytes = (size_t)(sh.max_K > 1 ? sh.max_K : 1) * kBatchRows * 8 + 256;
     ws.keys = reinterpret_cast<unsigned long long *>(take(ws.keys_bytes));

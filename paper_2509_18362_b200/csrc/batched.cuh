@@ -39,7 +39,7 @@ struct BatchedWs {
     float *hout;                  // [rows][d]   final-normed hidden state (recursed in fp32)
     bf16_t *q;                    // rotated, scaled queries as high and low bf16 parts
     float *att_part;              // [rows][Hq][max_chunks][dh + 2]  (o, m, l) per context chunk
-    size_t part_rows;             // room of att_part in [Hq][dh + 2] results
+    size_t part_rows;             // room of att_part in [Hq] results (kv8.cu lays them dh + 4 words apart)
     bf16_t *qkv;                  // [rows][qdim + 2 kvdim] rotated queries and keys, values (target steps over 8-bit caches)
     unsigned long long *keys;     // [max_K][kBatchRows] argmax keys
     uint32_t *id_bitmap;          // [ceil(V/32)] membership bits of the subset

@@ -31,6 +31,16 @@ __device__ __forceinline__ uint32_t e4m3x2_f16x2(uint16_t v) {               // 
     asm("cvt.rn.f16x2.e4m3x2 %0, %1;" : "=r"(r) : "h"(v));
     return r;
 }
+__device__ __forceinline__ uint32_t f16x2_e4m3x2(uint32_t v) {               // as to_e4m3x2
+    uint16_t r;
+    asm("cvt.rn.satfinite.e4m3x2.f16x2 %0, %1;" : "=h"(r) : "r"(v));
+    return r;
+}
+__device__ __forceinline__ uint32_t sub_f16x2(uint32_t x, uint32_t y) {
+    uint32_t r;
+    asm("sub.rn.f16x2 %0, %1, %2;" : "=r"(r) : "r"(x), "r"(y));
+    return r;
+}
 __device__ __forceinline__ void f16x2_f32(uint32_t h, float &a, float &b) {
     asm("{.reg .b16 l, h;\n\tmov.b32 {l, h}, %2;\n\tcvt.f32.f16 %0, l;\n\tcvt.f32.f16 %1, h;\n\t}" : "=f"(a), "=f"(b) : "r"(h));
 }
@@ -284,6 +294,8 @@ __host__ __device__ __forceinline__ int chunk8(int n_ctx, int pairs) {
     return c;
 }
 
+// Words from one partial result to the next: dh weighted values, their reference and sum, and two that keep 16 bytes' alignment.
+__host__ __device__ constexpr int part8_ld(int dh) { return dh + 4; }
 constexpr int kList8Words = 6 * kBatchRows + 2;       // see List8
 
 template <int DH, int RW, int WR>
@@ -419,12 +431,11 @@ struct List8 {
     }
     // CTAs' shares of the list have the same cost up to an item: CTA i of n begins with the first item that starts at or behind its share
     __device__ __forceinline__ int begin_of(int i, int n) const {
-        const int n_cost = pcost[B];
-        const long long x = (long long)i * n_cost / n;
+        const int n_cost = pcost[B], each = n_cost / n, x = i * each + i * (n_cost - each * n) / n;      // i * n_cost / n
         if (x >= n_cost) return prefix[B];
         int s = 0;
         while (pcost[s + 1] <= x) ++s;
-        const int rem = (int)x - pcost[s], chunks = tnum[s] & 0xffff, contexts = (prefix[s + 1] - prefix[s]) / chunks;
+        const int rem = x - pcost[s], chunks = tnum[s] & 0xffff, contexts = (prefix[s + 1] - prefix[s]) / chunks;
         const int cost = (pcost[s + 1] - pcost[s]) / contexts, ctx = rem / cost, one = tchk[s] / STRIDE + EACH;
         return prefix[s] + ctx * chunks + min((rem - ctx * cost + one - 1) / one, chunks);
     }
@@ -613,7 +624,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                     const bool there = pair_at(pair0 + kq + e, m, row, head);
                     prow[r][e] = there ? m : nv;
                     pn[r][e] = there ? list.row_ctx(list.tpos[it.seq], m) : kMaxLen;
-                    pout[r][e] = ((size_t)row * a.Hq + head) * a.slots * (DH + 2);
+                    pout[r][e] = ((size_t)row * a.Hq + head) * a.slots * part8_ld(DH);
                 }
             }
         }
@@ -810,7 +821,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
                         if (prow[r][e] < nv && pn[r][e] > it.t0) {             // such a pair, and it sees something of the chunk
-                            float *out = a.part + pout[r][e] + (size_t)it.chunk * (DH + 2);
+                            float *out = a.part + pout[r][e] + (size_t)it.chunk * part8_ld(DH);
 #pragma unroll
                             for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(out + c * 16 + g * 2) = make_float2(o[r][c][e] * sv_run, o[r][c][2 + e] * sv_run);
                             if (g == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(m_ref[e], l_run[r][e]);
@@ -857,7 +868,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                     }
                     const int m = pair / gq;
                     if (pair < nv * gq && list.row_ctx(list.tpos[it.seq], m) > it.t0) {
-                        float *out = a.part + (((size_t)(it.seq * a.M + m) * a.Hq + it.kvh * gq + (pair - m * gq)) * a.slots + it.chunk) * (DH + 2);
+                        float *out = a.part + (((size_t)(it.seq * a.M + m) * a.Hq + it.kvh * gq + (pair - m * gq)) * a.slots + it.chunk) * part8_ld(DH);
                         *reinterpret_cast<float2 *>(out + d) = make_float2(acc.x, acc.y);
                         *reinterpret_cast<float2 *>(out + d + 2) = make_float2(acc.z, acc.w);
                         if (d == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(mm, l);
@@ -964,47 +975,41 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
         for (int item = i_begin; item < i_end && ok; ++item) {
             if (fresh) {
                 // queries, two rows at a time, eight dims per lane (the last block's scores are there, so the old ones have been read)
-                const int nv = list.tval[it.seq], pair0 = it.set * kT8Pairs + warp * 32;
-                auto pair_at = [&](int pair, int &m, int &row, int &head) -> bool {
-                    const bool there = pair < nv * gq;
-                    m = there ? pair / gq : 0;
-                    row = it.seq * a.M + m;
-                    head = it.kvh * gq + (there ? pair - m * gq : 0);
-                    return there;
-                };
-                int m, row, head;
+                const int nv = list.tval[it.seq], pair = it.set * kT8Pairs + tid;
+                const bool there = pair < nv * gq;
+                const int m = there ? pair / gq : 0, row = it.seq * a.M + m, head = it.kvh * gq + (there ? pair - m * gq : 0);
+                pn = there ? list.row_ctx(list.tpos[it.seq], m) : kMaxLen;
+                prow = there ? (uint32_t)(row * a.Hq + head) : kFull;
+                const int piece = lane & 15, half = lane >> 4;
                 float qs = 1.f;
-                const int piece = lane & 15;
 #pragma unroll 1
                 for (int r0 = 0; r0 < 32; r0 += 8) {
                     uint4 x[4];
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const bool there = pair_at(pair0 + r0 + 2 * i + (lane >> 4), m, row, head);
-                        x[i] = make_uint4(0, 0, 0, 0);
-                        if (there) x[i] = *reinterpret_cast<const uint4 *>(a.q + (long long)row * a.ldq + (long long)head * DH + piece * 8);
+                        const int from = r0 + 2 * i + half, qrow = __shfl_sync(kFull, row, from), qhead = __shfl_sync(kFull, head, from);
+                        x[i] = *reinterpret_cast<const uint4 *>(a.q + (long long)qrow * a.ldq + qhead * DH + piece * 8);      // (no such pair: the first one's)
                     }
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const int r = warp * 32 + r0 + 2 * i + (lane >> 4);
-                        uint32_t am = finite_max(finite_max(finite_max(finite_max(0, x[i].x), x[i].y), x[i].z), x[i].w);
+                        const int r = warp * 32 + r0 + 2 * i + half;
+                        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                        uint32_t am = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
                         am = max(am & 0xffffu, am >> 16);
 #pragma unroll
                         for (int o = 1; o < 16; o <<= 1) am = max(am, __shfl_xor_sync(kFull, am, o));
-                        const float rs = scale_for(am), inv = 1.0f / rs, other = __shfl_sync(kFull, rs, (lane & 1) * 16);
+                        const float rs = scale_for(am), other = __shfl_sync(kFull, rs, (lane & 1) * 16);
                         if ((lane >> 1) == (r0 >> 1) + i) qs = other;
-                        const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+                        // the power of two's inverse; a row that is not finite is NaN
+                        const float inv = am < 0x7f80u ? __uint_as_float(0x7f000000u - __float_as_uint(rs)) : __uint_as_float(0x7fffffffu);
                         uint32_t hi[2], lo[2];
 #pragma unroll
                         for (int h = 0; h < 2; ++h) {
-                            float y[4] = {bf16lo_f32(w[2 * h]), bf16hi_f32(w[2 * h]), bf16lo_f32(w[2 * h + 1]), bf16hi_f32(w[2 * h + 1])}, z[4];
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) y[e] = fabsf(y[e]) < INFINITY ? y[e] * inv : __uint_as_float(0x7fffffffu);      // (not finite: NaN)
-                            hi[h] = to_e4m3x4(y, 1.f);
-                            e4m3x4_f32(hi[h], z);
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) y[e] -= z[e];
-                            lo[h] = to_e4m3x4(y, 1.f);
+                            const uint32_t y0 = pack_f16x2(bf16lo_f32(w[2 * h]) * inv, bf16hi_f32(w[2 * h]) * inv);       // (below 448: exact, but for what is below 2^-14)
+                            const uint32_t y1 = pack_f16x2(bf16lo_f32(w[2 * h + 1]) * inv, bf16hi_f32(w[2 * h + 1]) * inv);
+                            const uint32_t h0 = f16x2_e4m3x2(y0), h1 = f16x2_e4m3x2(y1);
+                            hi[h] = h0 | (h1 << 16);
+                            lo[h] = f16x2_e4m3x2(sub_f16x2(y0, e4m3x2_f16x2((uint16_t)h0))) | (f16x2_e4m3x2(sub_f16x2(y1, e4m3x2_f16x2((uint16_t)h1))) << 16);
                         }
                         unsigned char *at = smem + r * 128 + (((piece >> 1) ^ (r & 7)) << 4) + (piece & 1) * 8;
                         *reinterpret_cast<uint2 *>(at) = make_uint2(hi[0], hi[1]);
@@ -1012,9 +1017,6 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                     }
                 }
                 fs = qs * sm_scale;
-                const bool there = pair_at(pair0 + lane, m, row, head);
-                pn = there ? list.row_ctx(list.tpos[it.seq], m) : kMaxLen;
-                prow = there ? (uint32_t)(row * a.Hq + head) : kFull;
                 fence_proxy_async();
                 mbar_arrive(qready);
             }
@@ -1120,13 +1122,16 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 mbar_arrive(pready);
             }
             if (!ok) break;
-            // ---- the chunk's partial result, as kv8_attn_kernel leaves it: rows of 130 words, which a warp writes two at a time
+            // ---- the chunk's partial result, as kv8_attn_kernel leaves it; a warp writes four rows at a time
             ok = tile8_wait(abort_flag, &vempty[(n - 1) & 1], (uint32_t)((n - 1) >> 1) & 1u);
             if (__any_sync(kFull, !ok)) break;
             tc_fence_after_sync();
             const uint32_t out_row = prow != kFull && pn > it.t0 ? prow * (uint32_t)a.slots + (uint32_t)it.chunk : kFull;
-            float *mine = a.part + (size_t)out_row * (DH + 2);
+            float *mine = a.part + (size_t)out_row * part8_ld(DH);
             if (out_row != kFull) *reinterpret_cast<float2 *>(mine + DH) = make_float2(kP8Log2 - mo, l0 + l1);
+            uint32_t to[8];                          // rows of the four that a warp writes at a time
+#pragma unroll
+            for (int i = 0; i < 8; ++i) to[i] = __shfl_sync(kFull, out_row, 4 * i + (lane >> 3));
 #pragma unroll 1
             for (int c0 = 0; c0 < DH; c0 += 32) {
                 uint32_t o[32];
@@ -1137,13 +1142,11 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
 #pragma unroll
                 for (int c = 0; c < 8; ++c) sts128(p_row + (((uint32_t)c ^ sw) << 4), o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
                 __syncwarp();
-                const int half = lane >> 4, col = (lane & 15) * 2;
-#pragma unroll 8
-                for (int i = 0; i < 16; ++i) {
-                    const int r = 2 * i + half;
-                    const uint32_t to = __shfl_sync(kFull, out_row, r);
-                    const float2 v = *reinterpret_cast<const float2 *>(smem + Lay::O_P + (warp * 32 + r) * 128 + (((col >> 2) ^ (r & 7)) << 4) + (col & 3) * 4);
-                    if (to != kFull) *reinterpret_cast<float2 *>(a.part + (size_t)to * (DH + 2) + c0 + col) = v;
+#pragma unroll
+                for (int i = 0; i < 8; ++i) {
+                    const int r = 4 * i + (lane >> 3), c = lane & 7;
+                    const float4 v = *reinterpret_cast<const float4 *>(smem + Lay::O_P + (warp * 32 + r) * 128 + ((c ^ (r & 7)) << 4));
+                    if (to[i] != kFull) *reinterpret_cast<float4 *>(a.part + (size_t)to[i] * part8_ld(DH) + c0 + c * 4) = v;
                 }
                 __syncwarp();
             }
@@ -1163,7 +1166,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
     } else if (warp < 8) {
         // ================= copies: thread = a 16-byte piece of tokens trow + 16 u
         const int ct = tid - 128, piece = ct & 7, trow = ct >> 3;
-        struct Block { int tok, t1, kvh, seen, pg[4]; };       // first token (-1: none), the chunk's end, what every row sees, pages of the thread's tokens
+        struct Block { int tok, t1, kvh, edge, pg[4]; };       // first token (-1: none), the chunk's end, tokens that every row sees, pages of the thread's tokens
         Item8 w{};
         int witem = i_begin, wtok = 0;
         if (i_begin < i_end) { list.at(w, i_begin); wtok = w.t0; }
@@ -1171,70 +1174,50 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             x.tok = -1;
             if (witem >= i_end) return;
             x.tok = wtok; x.t1 = w.t1; x.kvh = w.kvh;
-            x.seen = list.row_ctx(list.tpos[w.seq], 0);
+            x.edge = list.row_ctx(list.tpos[w.seq], 0) - wtok;
 #pragma unroll
             for (int u = 0; u < 4; ++u) x.pg[u] = a.kv.block_table[(size_t)w.seq * a.kv.max_pages + page_of(min(wtok + trow + 16 * u, w.t1 - 1), a.page, a.shift)];
             wtok += kT8Blk;
             if (wtok >= w.t1 && ++witem < i_end) { list.next(w); wtok = w.t0; }
         };
-        auto slot_of = [&](const Block &x, int u, int &off) -> uint32_t {
-            const int pos = min(x.tok + trow + 16 * u, x.t1 - 1);
-            int pg = x.pg[u];
-            if ((unsigned)pg >= (unsigned)a.kv.num_pages) { atomicOr(a.status, kDevBadPage); pg = 0; }
-            off = pos - page_of(pos, a.page, a.shift) * a.page;
-            return (uint32_t)pg * (uint32_t)a.Hkv + (uint32_t)x.kvh;
-        };
         const uint64_t policy = l2_evict_first();
-        int ks = 0, n = 0;
+        struct Values { uint4 v[4]; float sc[4]; int edge; bool there; };       // sc: threads 0 and 1: K and V scales of the block's 16-token tiles
+        int ks = 0;
         uint32_t kph = 0;
-        auto copy_k = [&](const Block &x) -> bool {
-            if (x.tok < 0) return true;
+        auto fetch = [&](const Block &x, Values &y) -> bool {          // K into the ring, V into registers
+            y.there = x.tok >= 0;
+            y.edge = x.edge;
+            if (!y.there) return true;
             if (__any_sync(kFull, !tile8_wait(abort_flag, &kempty[ks], kph ^ 1u))) return false;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                int off;
-                const uint32_t slot = slot_of(x, u, off);
-                const int t = trow + 16 * u;
-                cp_async16_off_hint<0>(base + Lay::O_K + (uint32_t)(ks * Lay::K) + piece_at<DH>(t, piece),
-                                       a.kv.k_pages + ((size_t)slot * a.page + off) * DH + piece * 16, x.tok + t < x.t1 ? 16u : 0u, policy);
+                const int t = trow + 16 * u, pos = min(x.tok + t, x.t1 - 1);
+                int pg = x.pg[u];
+                if ((unsigned)pg >= (unsigned)a.kv.num_pages) { atomicOr(a.status, kDevBadPage); pg = 0; }
+                const uint32_t slot = (uint32_t)pg * (uint32_t)a.Hkv + (uint32_t)x.kvh;
+                const size_t at = ((size_t)slot * a.page + (pos - page_of(pos, a.page, a.shift) * a.page)) * DH + piece * 16;
+                const bool seen = x.tok + t < x.t1;
+                cp_async16_off_hint<0>(base + Lay::O_K + (uint32_t)(ks * Lay::K) + piece_at<DH>(t, piece), a.kv.k_pages + at, seen ? 16u : 0u, policy);
+                y.v[u] = make_uint4(0, 0, 0, 0);
+                if (seen) y.v[u] = *reinterpret_cast<const uint4 *>(a.kv.v_pages + at);
+                if (ct < 2) y.sc[u] = (ct ? a.kv.v_scales : a.kv.k_scales)[slot];
             }
             cp_async_arrive(&kfull[ks]);
             if (++ks == kT8KStages) { ks = 0; kph ^= 1u; }
             return true;
         };
-        uint4 v[4];
-        float sc[4] = {};                            // threads 0 and 1: K and V scales of the block's 16-token tiles
-        auto load_v = [&](const Block &x) {
-            if (x.tok < 0) return;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                int off;
-                const uint32_t slot = slot_of(x, u, off);
-                v[u] = make_uint4(0, 0, 0, 0);
-                if (x.tok + trow + 16 * u < x.t1) v[u] = *reinterpret_cast<const uint4 *>(a.kv.v_pages + ((size_t)slot * a.page + off) * DH + piece * 16);
-                if (trow == 0 && piece < 2) sc[u] = (piece ? a.kv.v_scales : a.kv.k_scales)[slot];
-            }
-        };
-        Block b0, b1, b2;
-        walk(b0);
-        walk(b1);
-        walk(b2);
-        bool ok = copy_k(b0) && copy_k(b1);
-        load_v(b0);
-        while (ok && b0.tok >= 0) {
-            ok = copy_k(b2);
-            if (!ok) break;
+        int n = 0;
+        auto convert = [&](const Values &y) -> bool {
             const int b = n & 1;
-            if (__any_sync(kFull, !tile8_wait(abort_flag, &vempty[b], ((uint32_t)(n >> 1) & 1u) ^ 1u))) break;
+            if (__any_sync(kFull, !tile8_wait(abort_flag, &vempty[b], ((uint32_t)(n >> 1) & 1u) ^ 1u))) return false;
             Tile8Block *blk = reinterpret_cast<Tile8Block *>(smem + Lay::O_BLK) + b;
             const uint32_t dst = base + Lay::O_V + (uint32_t)(b * Lay::V) + (uint32_t)(piece >> 2) * (Lay::V / 2);
             bool bad = false;
-            const bool edge = b0.tok + kT8Blk > b0.seen;
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
                 const int t = trow + 16 * u;
-                uint32_t c[4] = {v[u].x, v[u].y, v[u].z, v[u].w}, h[8];
-                if (edge && b0.tok + t >= b0.seen) {
+                uint32_t c[4] = {y.v[u].x, y.v[u].y, y.v[u].z, y.v[u].w}, h[8];
+                if (t >= y.edge) {
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const uint32_t nan = __vcmpeq4(c[i] & 0x7f7f7f7fu, 0x7f7f7f7fu);
@@ -1251,16 +1234,28 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 sts128(a0, second ? h[4] : h[0], second ? h[5] : h[1], second ? h[6] : h[2], second ? h[7] : h[3]);
                 sts128(a1, second ? h[0] : h[4], second ? h[1] : h[5], second ? h[2] : h[6], second ? h[3] : h[7]);
             }
-            if (ct < 2) *reinterpret_cast<float4 *>(ct ? blk->sv : blk->sk) = make_float4(sc[0], sc[1], sc[2], sc[3]);
+            if (ct < 2) *reinterpret_cast<float4 *>(ct ? blk->sv : blk->sk) = make_float4(y.sc[0], y.sc[1], y.sc[2], y.sc[3]);
             bad = __any_sync(kFull, bad);
             if (lane == 0) blk->bad[warp - 4] = bad ? 1u : 0u;
             fence_proxy_async();
             mbar_arrive(&vfull[b]);
-            b0 = b1;
-            b1 = b2;
             ++n;
-            load_v(b0);
-            walk(b2);
+            return true;
+        };
+        // two blocks are on their way, and the pages of a third
+        Block next;
+        Values y0, y1;
+        walk(next);
+        bool ok = fetch(next, y0);
+        walk(next);
+        ok = ok && fetch(next, y1);
+        walk(next);
+        while (ok && y0.there) {
+            if (!(ok = convert(y0) && fetch(next, y0))) break;
+            walk(next);
+            if (!y1.there) break;
+            if (!(ok = convert(y1) && fetch(next, y1))) break;
+            walk(next);
         }
         asm volatile("cp.async.wait_all;" ::: "memory");
     } else {
@@ -1347,7 +1342,7 @@ __global__ void __launch_bounds__(DH) kv8_merge_kernel(const Attn8Args a) {
     const int len = kv8_len(a.kv, seq);
     const int n = min(len + m, max_tokens - 1) + 1, c = chunk8(min(len + a.M - 1, max_tokens - 1) + 1, a.M * a.gq);
     const int chunks = (n + c - 1) / c;
-    constexpr int stride = DH + 2, G = 16;
+    constexpr int stride = part8_ld(DH), G = 16;
     const float *base = a.part + ((size_t)r * a.Hq + head) * a.slots * stride;
     float mx = -INFINITY;
     for (int i = lane; i < chunks; i += 32) mx = fmaxf(mx, base[(size_t)i * stride + DH]);

@@ -32,7 +32,7 @@ struct Kv8AttnCall {
     long long ldq;
     int B, M;                             // B <= 64 sequences, M <= 64 rows of each
     const int32_t *n_new;                 // as above
-    float *part;                          // [rows][Hq][kv8_attention_slots][dh + 2] partial results of a context's chunks
+    float *part;                          // [rows][Hq][kv8_attention_slots][dh + 4] partial results of a context's chunks
     bf16_t *out;                          // [rows][Hq][dh], or
     bf16_t *xop;                          // the next GEMM's operand: rows 2r (high parts) and 2r + 1 (low parts), ld_xop apart
     int ld_xop;
