@@ -281,16 +281,16 @@ constexpr float kQ8 = 32.f;                          // queries below 448 * 32
 // Tokens of a chunk: a function of the sequence's committed length and of the call's rows per sequence, never of the batch. Short
 // enough for a context to keep many CTAs busy, long enough for the partial results (dh + 2 fp32 values for each pair and chunk,
 // 512 bytes against 256 bytes of K/V per token at dh = 128) to stay a small part of the traffic: up to `few` chunks until a chunk is
-// `base` long, up to `most` chunks of that and more tokens beyond.
-struct Chunk8 { int first, few, base, most; };
+// 2^base long, up to `most` chunks of that and more tokens beyond.
+struct Chunk8 { int first, few, base, most; };       // first and base: powers of two
 __host__ __device__ __forceinline__ Chunk8 chunk8_rule(int pairs) {
-    return pairs <= 8 ? Chunk8{128, 16, 512, 128} : pairs <= 32 ? Chunk8{128, 16, 512, 64} : Chunk8{256, 8, 512, 32};
+    return pairs <= 8 ? Chunk8{7, 16, 9, 128} : pairs <= 32 ? Chunk8{7, 16, 9, 64} : Chunk8{8, 8, 9, 32};
 }
-__host__ __device__ __forceinline__ int chunk8(int n_ctx, int pairs) {
+__host__ __device__ __forceinline__ int chunk8(int n_ctx, int pairs) {      // log2
     const Chunk8 r = chunk8_rule(pairs);
     int c = r.first;
-    while (c < r.base && n_ctx > c * r.few) c *= 2;
-    while ((n_ctx + c - 1) / c > r.most) c *= 2;
+    while (c < r.base && n_ctx > r.few << c) ++c;
+    while (((n_ctx - 1) >> c) >= r.most) ++c;
     return c;
 }
 
@@ -378,7 +378,7 @@ struct Item8 {
 template <int PAIRS, int STRIDE, int EACH>
 struct List8 {
     int *prefix, *pcost;                             // [B + 1] items before a sequence, and their cost
-    int *tpos, *tval, *tchk, *tnum;                  // position of a sequence's row 0, its rows that count, tokens of its chunks, chunks | sets << 16
+    int *tpos, *tval, *tchk, *tnum;                  // position of a sequence's row 0, its rows that count, tokens of its chunks (log2), chunks | sets << 16
     int B, Hkv, max_tokens;
 
     __device__ __forceinline__ List8(const Attn8Args &a, void *mem) {
@@ -405,7 +405,7 @@ struct List8 {
                 tpos[s] = len; tval[s] = nv; tchk[s] = c;
                 tnum[s] = 0;
                 if (nv > 0) {
-                    const int n = row_ctx(len, nv - 1), chunks = (n + c - 1) / c, sets = (nv * a.gq + PAIRS - 1) / PAIRS;
+                    const int n = row_ctx(len, nv - 1), chunks = ((n - 1) >> c) + 1, sets = (nv * a.gq + PAIRS - 1) / PAIRS;
                     tnum[s] = chunks | (sets << 16);
                     cnt[u] = chunks * a.Hkv * sets;
                     cost[u] = (chunks * EACH + (n + STRIDE - 1) / STRIDE) * a.Hkv * sets;
@@ -435,14 +435,14 @@ struct List8 {
         if (x >= n_cost) return prefix[B];
         int s = 0;
         while (pcost[s + 1] <= x) ++s;
-        const int rem = x - pcost[s], chunks = tnum[s] & 0xffff, contexts = (prefix[s + 1] - prefix[s]) / chunks;
-        const int cost = (pcost[s + 1] - pcost[s]) / contexts, ctx = rem / cost, one = tchk[s] / STRIDE + EACH;
+        const int rem = x - pcost[s], chunks = tnum[s] & 0xffff;
+        const int cost = (pcost[s + 1] - pcost[s]) / (Hkv * (tnum[s] >> 16)), ctx = rem / cost, one = (1 << tchk[s]) / STRIDE + EACH;
         return prefix[s] + ctx * chunks + min((rem - ctx * cost + one - 1) / one, chunks);
     }
     __device__ __forceinline__ void bounds(Item8 &it) const {
         const int c = tchk[it.seq];
-        it.t0 = it.chunk * c;
-        it.t1 = min(it.t0 + c, row_ctx(tpos[it.seq], tval[it.seq] - 1));
+        it.t0 = it.chunk << c;
+        it.t1 = min(it.t0 + (1 << c), row_ctx(tpos[it.seq], tval[it.seq] - 1));
     }
     __device__ __forceinline__ void at(Item8 &it, int i) const {
         int s = 0;
@@ -895,8 +895,8 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
 // products.
 constexpr int kT8Pairs = 128, kT8Blk = 64, kT8Threads = 288, kT8Copiers = 128, kT8KStages = 3;
 constexpr unsigned long long kT8WaitNs = 2000000000ull;
-struct Tile8Block {                                  // per V buffer: scales of the block's 16-token tiles, written beside its values
-    float sk[4], sv[4];
+struct Tile8Block {                                  // per V buffer, written beside its values
+    float sk[4], sv[4], sv_log2[4], sv_inv[4];       // of the block's 16-token tiles
     uint32_t bad[4];                                 // values that are no number were left out (see kv8_attn_kernel); of each copy warp
 };
 struct Tile8Smem {
@@ -908,7 +908,7 @@ struct Tile8Smem {
     static constexpr int O_LIST = O_WORDS + 8;
     static constexpr int TOTAL = O_LIST + kList8Words * 4;
 };
-static_assert(sizeof(Tile8Block) % 16 == 0 && 2 * (Tile8Smem::TOTAL + 1024) <= 228 * 1024, "two CTAs per SM");
+static_assert(sizeof(Tile8Block) % 16 == 0 && offsetof(Tile8Block, sv) == 16 && 2 * (Tile8Smem::TOTAL + 1024) <= 228 * 1024, "two CTAs per SM");
 
 __device__ __forceinline__ bool tile8_wait(volatile uint32_t *abort_flag, uint64_t *bar, uint32_t parity) {
     if (mbar_try_wait(bar, parity)) return true;
@@ -937,9 +937,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
     uint64_t *pready = sfull + 2, *qready = pready + 1, *drain = qready + 1;
     volatile uint32_t *words = reinterpret_cast<volatile uint32_t *>(smem + Lay::O_WORDS), *abort_flag = words + 1;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    chain_wait();
     List8<kT8Pairs, kT8Blk, 2> list(a, smem + Lay::O_LIST);
-    if (warp == 0) list.build(a, lane);
     if (tid == 32) {
         for (int i = 0; i < kT8KStages; ++i) { mbar_init(&kfull[i], kT8Copiers); mbar_init(&kempty[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&vfull[i], kT8Copiers); mbar_init(&vempty[i], 1); mbar_init(&sfull[i], 1); }
@@ -954,6 +952,8 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
         tmem_relinquish();
         tc_fence_before_sync();
     }
+    chain_wait();
+    if (warp == 0) list.build(a, lane);
     __syncwarp();
     __syncthreads();
     tc_fence_after_sync();
@@ -982,16 +982,17 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 prow = there ? (uint32_t)(row * a.Hq + head) : kFull;
                 const int piece = lane & 15, half = lane >> 4;
                 float qs = 1.f;
+                uint4 x[2], ahead[2];
 #pragma unroll 1
-                for (int r0 = 0; r0 < 32; r0 += 8) {
-                    uint4 x[4];
+                for (int r0 = -4; r0 < 32; r0 += 4) {          // the next four rows are on their way
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int from = r0 + 2 * i + half, qrow = __shfl_sync(kFull, row, from), qhead = __shfl_sync(kFull, head, from);
-                        x[i] = *reinterpret_cast<const uint4 *>(a.q + (long long)qrow * a.ldq + qhead * DH + piece * 8);      // (no such pair: the first one's)
+                    for (int i = 0; i < 2; ++i) {
+                        const int from = min(r0 + 4 + 2 * i + half, 31), qrow = __shfl_sync(kFull, row, from), qhead = __shfl_sync(kFull, head, from);
+                        ahead[i] = *reinterpret_cast<const uint4 *>(a.q + (long long)qrow * a.ldq + qhead * DH + piece * 8);      // (no such pair: the first one's)
                     }
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
+                    for (int i = 0; i < 2; ++i) {
+                        if (r0 < 0) break;
                         const int r = warp * 32 + r0 + 2 * i + half;
                         const uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
                         uint32_t am = __vmaxu2(__vmaxu2(w[0] & 0x7fff7fffu, w[1] & 0x7fff7fffu), __vmaxu2(w[2] & 0x7fff7fffu, w[3] & 0x7fff7fffu));
@@ -1015,12 +1016,14 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                         *reinterpret_cast<uint2 *>(at) = make_uint2(hi[0], hi[1]);
                         *reinterpret_cast<uint2 *>(at + Lay::TILE) = make_uint2(lo[0], lo[1]);
                     }
+                    x[0] = ahead[0];
+                    x[1] = ahead[1];
                 }
                 fs = qs * sm_scale;
                 fence_proxy_async();
                 mbar_arrive(qready);
             }
-            float mo = kP8Log2, l0 = 0.f, l1 = 0.f, sv_run = 0.f, sv_inv = 0.f;
+            float mo = kP8Log2, l_run = 0.f, sv_run = 0.f, sv_log2 = 0.f;
             uint32_t bad = 0;
 #pragma unroll 1
             for (int tb = it.t0; tb < it.t1; tb += kT8Blk, ++n) {
@@ -1050,10 +1053,11 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 }
                 // ---- the largest score (the scores are read from tensor memory twice: 64 of them would not fit the registers)
                 float ym = -INFINITY;
-#pragma unroll
+#pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     uint32_t x[32];
                     tmem_ld32_issue(tmem_s + (uint32_t)(h * 32), x);
+                    const float ch[2] = {h ? c[2] : c[0], h ? c[3] : c[1]};
                     tmem_ld_wait();
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {
@@ -1061,20 +1065,19 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
 #pragma unroll
                         for (int j = 0; j < 4; ++j) m4[j] = fmaxf(fmaxf(__uint_as_float(x[g * 16 + j]), __uint_as_float(x[g * 16 + 4 + j])),
                                                                   fmaxf(__uint_as_float(x[g * 16 + 8 + j]), __uint_as_float(x[g * 16 + 12 + j])));
-                        ym = fmaxf(ym, fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), c[2 * h + g], mo));
+                        ym = fmaxf(ym, fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), ch[g], mo));
                     }
                 }
                 const bool first = tb == it.t0;
                 const float d = (first || ym > kP8Max) && ym > -INFINITY ? ym - kP8Log2 : 0.f;
                 mo -= d;
                 float corr = first ? 1.f : exp2_approx(-d);
-                l0 *= corr;
-                l1 *= corr;
+                l_run *= corr;
                 const float svm = fmaxf(fmaxf(sv4.x, sv4.y), fmaxf(sv4.z, sv4.w));
                 if (svm > sv_run) {
-                    sv_inv = __fdividef(1.0f, svm);
-                    corr *= sv_run * sv_inv;
+                    corr *= __fdividef(sv_run, svm);
                     sv_run = svm;
+                    sv_log2 = __log2f(svm);
                 }
                 // ---- the block before has been added up: its probabilities may be overwritten, what it left can be scaled
                 if (n > 0) {
@@ -1094,27 +1097,29 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                     }
                     tmem_st_wait();
                 }
-                // ---- probabilities, as f16
-                const float f[4] = {sv4.x * sv_inv, sv4.y * sv_inv, sv4.z * sv_inv, sv4.w * sv_inv};
-                const bool scaled = fminf(fminf(sv4.x, sv4.y), fminf(sv4.z, sv4.w)) != sv_run;
-#pragma unroll
+                // ---- probabilities, as f16, times their V scales over the largest (2^-60 of it counts as much as nothing): in the exponent,
+                // and taken out of a tile's sum again
+                const float4 sl4 = *reinterpret_cast<const float4 *>(blk->sv_log2), si4 = *reinterpret_cast<const float4 *>(blk->sv_inv);
+                const float e[4] = {mo + fmaxf(sl4.x - sv_log2, -60.f), mo + fmaxf(sl4.y - sv_log2, -60.f), mo + fmaxf(sl4.z - sv_log2, -60.f), mo + fmaxf(sl4.w - sv_log2, -60.f)};
+                const float f[4] = {fminf(si4.x * sv_run, 0x1p60f), fminf(si4.y * sv_run, 0x1p60f), fminf(si4.z * sv_run, 0x1p60f), fminf(si4.w * sv_run, 0x1p60f)};
+#pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     uint32_t x[32];
                     tmem_ld32_issue(tmem_s + (uint32_t)(h * 32), x);
+                    const float ch[2] = {h ? c[2] : c[0], h ? c[3] : c[1]}, eh[2] = {h ? e[2] : e[0], h ? e[3] : e[1]}, fh[2] = {h ? f[2] : f[0], h ? f[3] : f[1]};
                     tmem_ld_wait();
 #pragma unroll
-                    for (int q = 0; q < 4; ++q) {
-                        const float cc = c[2 * h + (q >> 1)];
-                        float p[8];
+                    for (int g = 0; g < 2; ++g) {
+                        float sum = 0.f;
 #pragma unroll
-                        for (int e = 0; e < 8; ++e) p[e] = exp2_approx(fmaf(__uint_as_float(x[q * 8 + e]), cc, mo));
-                        l0 += (p[0] + p[1]) + (p[2] + p[3]);
-                        l1 += (p[4] + p[5]) + (p[6] + p[7]);
-                        if (scaled) {
+                        for (int q = 2 * g; q < 2 * g + 2; ++q) {
+                            float p[8];
 #pragma unroll
-                            for (int e = 0; e < 8; ++e) p[e] *= f[2 * h + (q >> 1)];
+                            for (int i = 0; i < 8; ++i) p[i] = exp2_approx(fmaf(__uint_as_float(x[q * 8 + i]), ch[g], eh[g]));
+                            sum += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+                            sts128(p_row + (((uint32_t)(h * 4 + q) ^ sw) << 4), pack_f16x2(p[0], p[1]), pack_f16x2(p[2], p[3]), pack_f16x2(p[4], p[5]), pack_f16x2(p[6], p[7]));
                         }
-                        sts128(p_row + (((uint32_t)(h * 4 + q) ^ sw) << 4), pack_f16x2(p[0], p[1]), pack_f16x2(p[2], p[3]), pack_f16x2(p[4], p[5]), pack_f16x2(p[6], p[7]));
+                        l_run = fmaf(sum, fh[g], l_run);
                     }
                 }
                 fence_proxy_async();
@@ -1128,7 +1133,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             tc_fence_after_sync();
             const uint32_t out_row = prow != kFull && pn > it.t0 ? prow * (uint32_t)a.slots + (uint32_t)it.chunk : kFull;
             float *mine = a.part + (size_t)out_row * part8_ld(DH);
-            if (out_row != kFull) *reinterpret_cast<float2 *>(mine + DH) = make_float2(kP8Log2 - mo, l0 + l1);
+            if (out_row != kFull) *reinterpret_cast<float2 *>(mine + DH) = make_float2(kP8Log2 - mo, l_run);
             uint32_t to[8];                          // rows of the four that a warp writes at a time
 #pragma unroll
             for (int i = 0; i < 8; ++i) to[i] = __shfl_sync(kFull, out_row, 4 * i + (lane >> 3));
@@ -1164,9 +1169,10 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             if (item + 1 < i_end) fresh = list.next(it);
         }
     } else if (warp < 8) {
-        // ================= copies: thread = a 16-byte piece of tokens trow + 16 u
-        const int ct = tid - 128, piece = ct & 7, trow = ct >> 3;
-        struct Block { int tok, t1, kvh, edge, pg[4]; };       // first token (-1: none), the chunk's end, tokens that every row sees, pages of the thread's tokens
+        // ================= copies: thread = a 16-byte piece of tokens trow + 16 u. (Eight lanes hold four pieces of two tokens: their f16 values,
+        // two pieces of a row of 64 dims, lie in all banks.)
+        const int piece = (lane & 3) | (lane >> 1 & 4), trow = (warp - 4) * 4 + (lane >> 2 & 1) + (lane >> 3 & 2);
+        struct Block { int tok, t1, kvh, edge, pg, off; };     // first token (-1: none), the chunk's end, tokens that every row sees; 16-token tile `lane & 3`: page, place in it
         Item8 w{};
         int witem = i_begin, wtok = 0;
         if (i_begin < i_end) { list.at(w, i_begin); wtok = w.t0; }
@@ -1175,67 +1181,75 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             if (witem >= i_end) return;
             x.tok = wtok; x.t1 = w.t1; x.kvh = w.kvh;
             x.edge = list.row_ctx(list.tpos[w.seq], 0) - wtok;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) x.pg[u] = a.kv.block_table[(size_t)w.seq * a.kv.max_pages + page_of(min(wtok + trow + 16 * u, w.t1 - 1), a.page, a.shift)];
+            const int tile = min(wtok + (lane & 3) * 16, (w.t1 - 1) & ~15), blk = page_of(tile, a.page, a.shift);
+            x.off = tile - blk * a.page;
+            x.pg = a.kv.block_table[(size_t)w.seq * a.kv.max_pages + blk];
             wtok += kT8Blk;
             if (wtok >= w.t1 && ++witem < i_end) { list.next(w); wtok = w.t0; }
         };
         const uint64_t policy = l2_evict_first();
-        struct Values { uint4 v[4]; float sc[4]; int edge; bool there; };       // sc: threads 0 and 1: K and V scales of the block's 16-token tiles
+        struct Values { uint4 v[4]; float scale; int edge; bool there; };       // scale: lanes 0-3 of warp 4: K's of a tile, 4-7: V's
         int ks = 0;
         uint32_t kph = 0;
+        const uint32_t k_at = base + Lay::O_K + piece_at<DH>(trow, piece);
+        const size_t from = (size_t)trow * DH + piece * 16;
         auto fetch = [&](const Block &x, Values &y) -> bool {          // K into the ring, V into registers
             y.there = x.tok >= 0;
             y.edge = x.edge;
             if (!y.there) return true;
             if (__any_sync(kFull, !tile8_wait(abort_flag, &kempty[ks], kph ^ 1u))) return false;
+            int pg = x.pg;
+            if ((unsigned)pg >= (unsigned)a.kv.num_pages) { atomicOr(a.status, kDevBadPage); pg = 0; }
+            const uint32_t slot = (uint32_t)pg * (uint32_t)a.Hkv + (uint32_t)x.kvh, row = slot * (uint32_t)a.page + (uint32_t)x.off;
+            if (warp == 4 && lane < 8) y.scale = (lane < 4 ? a.kv.k_scales : a.kv.v_scales)[slot];
+            const uint32_t dst = k_at + (uint32_t)(ks * Lay::K);
+            const int left = x.t1 - x.tok - trow;                      // (zeros beyond the chunk's end)
 #pragma unroll
             for (int u = 0; u < 4; ++u) {
-                const int t = trow + 16 * u, pos = min(x.tok + t, x.t1 - 1);
-                int pg = x.pg[u];
-                if ((unsigned)pg >= (unsigned)a.kv.num_pages) { atomicOr(a.status, kDevBadPage); pg = 0; }
-                const uint32_t slot = (uint32_t)pg * (uint32_t)a.Hkv + (uint32_t)x.kvh;
-                const size_t at = ((size_t)slot * a.page + (pos - page_of(pos, a.page, a.shift) * a.page)) * DH + piece * 16;
-                const bool seen = x.tok + t < x.t1;
-                cp_async16_off_hint<0>(base + Lay::O_K + (uint32_t)(ks * Lay::K) + piece_at<DH>(t, piece), a.kv.k_pages + at, seen ? 16u : 0u, policy);
+                const size_t at = (size_t)__shfl_sync(kFull, row, u) * DH + from;
+                cp_async16_off_hint<0>(dst + (uint32_t)(u * 16 * DH), a.kv.k_pages + at, u * 16 < left ? 16u : 0u, policy);
                 y.v[u] = make_uint4(0, 0, 0, 0);
-                if (seen) y.v[u] = *reinterpret_cast<const uint4 *>(a.kv.v_pages + at);
-                if (ct < 2) y.sc[u] = (ct ? a.kv.v_scales : a.kv.k_scales)[slot];
+                if (u * 16 < left) y.v[u] = *reinterpret_cast<const uint4 *>(a.kv.v_pages + at);
             }
             cp_async_arrive(&kfull[ks]);
             if (++ks == kT8KStages) { ks = 0; kph ^= 1u; }
             return true;
         };
         int n = 0;
-        auto convert = [&](const Values &y) -> bool {
+        const uint32_t v_at = base + Lay::O_V + (uint32_t)(piece >> 2) * (Lay::V / 2) + (uint32_t)trow * 128;
+        const uint32_t v0 = v_at + ((uint32_t)((2 * (piece & 3)) ^ (trow & 7)) << 4), v1 = v_at + ((uint32_t)((2 * (piece & 3) + 1) ^ (trow & 7)) << 4);
+        auto convert = [&](Values &y) -> bool {
             const int b = n & 1;
             if (__any_sync(kFull, !tile8_wait(abort_flag, &vempty[b], ((uint32_t)(n >> 1) & 1u) ^ 1u))) return false;
             Tile8Block *blk = reinterpret_cast<Tile8Block *>(smem + Lay::O_BLK) + b;
-            const uint32_t dst = base + Lay::O_V + (uint32_t)(b * Lay::V) + (uint32_t)(piece >> 2) * (Lay::V / 2);
             bool bad = false;
+            if (y.edge < kT8Blk) {
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const int t = trow + 16 * u;
-                uint32_t c[4] = {y.v[u].x, y.v[u].y, y.v[u].z, y.v[u].w}, h[8];
-                if (t >= y.edge) {
+                for (int u = 0; u < 4; ++u) {
+                    uint32_t c[4] = {y.v[u].x, y.v[u].y, y.v[u].z, y.v[u].w};
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
-                        const uint32_t nan = __vcmpeq4(c[i] & 0x7f7f7f7fu, 0x7f7f7f7fu);
+                        const uint32_t nan = trow + 16 * u >= y.edge ? __vcmpeq4(c[i] & 0x7f7f7f7fu, 0x7f7f7f7fu) : 0u;
                         c[i] &= ~nan;
                         bad = bad || nan != 0u;
                     }
+                    y.v[u] = make_uint4(c[0], c[1], c[2], c[3]);
                 }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) { h[2 * i] = e4m3lo_f16x2(c[i]); h[2 * i + 1] = e4m3hi_f16x2(c[i]); }
-                // dims 16 piece and on: two pieces of a row of 64 dims (the rows' other halves in the other order: all banks at once)
-                const uint32_t q = 2 * (piece & 3), swz = t & 7, at = dst + (uint32_t)t * 128;
-                const bool second = piece >= 4;
-                const uint32_t a0 = at + (((q + (second ? 1 : 0)) ^ swz) << 4), a1 = at + (((q + (second ? 0 : 1)) ^ swz) << 4);
-                sts128(a0, second ? h[4] : h[0], second ? h[5] : h[1], second ? h[6] : h[2], second ? h[7] : h[3]);
-                sts128(a1, second ? h[0] : h[4], second ? h[1] : h[5], second ? h[2] : h[6], second ? h[3] : h[7]);
+                bad = __any_sync(kFull, bad);
             }
-            if (ct < 2) *reinterpret_cast<float4 *>(ct ? blk->sv : blk->sk) = make_float4(y.sc[0], y.sc[1], y.sc[2], y.sc[3]);
-            bad = __any_sync(kFull, bad);
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const uint32_t o = (uint32_t)(b * Lay::V + u * 16 * 128);
+                sts128(v0 + o, e4m3lo_f16x2(y.v[u].x), e4m3hi_f16x2(y.v[u].x), e4m3lo_f16x2(y.v[u].y), e4m3hi_f16x2(y.v[u].y));
+                sts128(v1 + o, e4m3lo_f16x2(y.v[u].z), e4m3hi_f16x2(y.v[u].z), e4m3lo_f16x2(y.v[u].w), e4m3hi_f16x2(y.v[u].w));
+            }
+            if (warp == 4 && lane < 8) {
+                reinterpret_cast<float *>(blk)[lane] = y.scale;        // sk, sv
+                if (lane >= 4) {
+                    blk->sv_log2[lane - 4] = __log2f(y.scale);
+                    blk->sv_inv[lane - 4] = 1.0f / y.scale;
+                }
+            }
             if (lane == 0) blk->bad[warp - 4] = bad ? 1u : 0u;
             fence_proxy_async();
             mbar_arrive(&vfull[b]);
@@ -1341,7 +1355,7 @@ __global__ void __launch_bounds__(DH) kv8_merge_kernel(const Attn8Args a) {
     const int max_tokens = min((int)min((long long)a.kv.max_pages * a.page, (long long)kMaxLen), a.max_ctx);
     const int len = kv8_len(a.kv, seq);
     const int n = min(len + m, max_tokens - 1) + 1, c = chunk8(min(len + a.M - 1, max_tokens - 1) + 1, a.M * a.gq);
-    const int chunks = (n + c - 1) / c;
+    const int chunks = ((n - 1) >> c) + 1;
     constexpr int stride = part8_ld(DH), G = 16;
     const float *base = a.part + ((size_t)r * a.Hq + head) * a.slots * stride;
     float mx = -INFINITY;
@@ -1435,7 +1449,7 @@ int kv8_read(const Kv8Shape &sh, const Kv8Ptrs &kv, int B, int max_n, const int3
 int kv8_attention_slots(const Kv8Shape &sh, int M) {
     // the largest number of chunks of any context up to max_ctx
     const Chunk8 r = chunk8_rule(M * (sh.Hq / sh.Hkv));
-    auto up = [](int n, int c) { return (n + c - 1) / c; };
+    auto up = [](int n, int c) { return ((n - 1) >> c) + 1; };
     const int few = up(sh.max_ctx, r.first) < r.few ? up(sh.max_ctx, r.first) : r.few, most = up(sh.max_ctx, r.base) < r.most ? up(sh.max_ctx, r.base) : r.most;
     return few > most ? few : most;
 }
