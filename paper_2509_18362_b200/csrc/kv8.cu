@@ -1343,52 +1343,94 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
     chain_release();
 }
 
-// ---- a row's chunks joined in ascending order. Block = (query head, row), a thread per element; a warp's lanes hold the weights of
-// 32 chunks, and a batch of the chunks' values is requested before they are known.
-template <int DH>
-__global__ void __launch_bounds__(DH) kv8_merge_kernel(const Attn8Args a) {
+// ---- a row's chunks joined in ascending order. A warp for a (query head, row), DH / 32 dims per lane; its lanes hold the weights of
+// 32 chunks, and a batch of the chunks' values is requested before they are known. WARPS > 1: the warps of a block take the 32s in turn and are joined in
+// their order (few rows of many chunks).
+template <int DH, int WARPS>
+__global__ void __launch_bounds__(128) kv8_merge_kernel(const Attn8Args a) {
     chain_release();
     chain_wait();
-    const int head = blockIdx.x, r = blockIdx.y, j = threadIdx.x, lane = j & 31;
+    constexpr int stride = part8_ld(DH), D = DH / 32, G = 16, RESULTS = 4 / WARPS;
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, share = warp % WARPS;
+    const int at = (int)blockIdx.x * RESULTS + warp / WARPS, r = at / a.Hq, head = at - r * a.Hq;
     const int seq = r / a.M, m = r - seq * a.M;
-    if (m >= kv8_rows(a.n_new, seq, a.M)) return;    // padding: left as it was
+    if (seq >= a.B || m >= kv8_rows(a.n_new, seq, a.M)) return;      // padding: left as it was (a block's warps agree where they meet)
     const int max_tokens = min((int)min((long long)a.kv.max_pages * a.page, (long long)kMaxLen), a.max_ctx);
     const int len = kv8_len(a.kv, seq);
     const int n = min(len + m, max_tokens - 1) + 1, c = chunk8(min(len + a.M - 1, max_tokens - 1) + 1, a.M * a.gq);
     const int chunks = ((n - 1) >> c) + 1;
-    constexpr int stride = part8_ld(DH), G = 16;
-    const float *base = a.part + ((size_t)r * a.Hq + head) * a.slots * stride;
-    float mx = -INFINITY;
-    for (int i = lane; i < chunks; i += 32) mx = fmaxf(mx, base[(size_t)i * stride + DH]);
-#pragma unroll
-    for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
-    const float mu = mx == -INFINITY ? 0.f : mx;
-    float acc = 0.f, l = 0.f;
-    for (int c0 = 0; c0 < chunks; c0 += 32) {
+    const float *base = a.part + (size_t)at * a.slots * stride;
+    float mu = -INFINITY, l = 0.f, acc[D] = {};
+    for (int c0 = share * 32; c0 < chunks; c0 += 32 * WARPS) {
         const int i = c0 + lane;
-        const float w = i < chunks ? exp2f(base[(size_t)i * stride + DH] - mu) : 0.f;
-        float lw = i < chunks ? base[(size_t)i * stride + DH + 1] * w : 0.f;
+        const float2 ml = i < chunks ? *reinterpret_cast<const float2 *>(base + (size_t)i * stride + DH) : make_float2(-INFINITY, 0.f);
+        float v[G][D];
+        auto load = [&](int g0) {
+#pragma unroll
+            for (int u = 0; u < G; ++u) {
+                const float *p = base + (size_t)min(c0 + g0 + u, chunks - 1) * stride + lane * D;
+                if constexpr (D == 4) { const float4 x = *reinterpret_cast<const float4 *>(p); v[u][0] = x.x; v[u][1] = x.y; v[u][2] = x.z; v[u][3] = x.w; }
+                else { const float2 x = *reinterpret_cast<const float2 *>(p); v[u][0] = x.x; v[u][1] = x.y; }
+            }
+        };
+        load(0);
+        float mx = fmaxf(mu, ml.x);
+#pragma unroll
+        for (int o = 16; o > 0; o >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, o));
+        const float ref = mx == -INFINITY ? 0.f : mx, old = exp2f(mu - ref), w = i < chunks ? exp2f(ml.x - ref) : 0.f;
+        mu = mx;
+        float lw = ml.y * w;
 #pragma unroll
         for (int o = 16; o > 0; o >>= 1) lw += __shfl_xor_sync(0xffffffffu, lw, o);
-        l += lw;
+        l = l * old + lw;
 #pragma unroll
-        for (int g0 = 0; g0 < 32; g0 += G) {
-            if (c0 + g0 >= chunks) break;
-            float v[G];
+        for (int d = 0; d < D; ++d) acc[d] *= old;
+#pragma unroll 1
+        for (int g0 = 0; g0 < 32 && c0 + g0 < chunks; g0 += G) {
+            if (g0) load(g0);
 #pragma unroll
-            for (int u = 0; u < G; ++u) v[u] = c0 + g0 + u < chunks ? base[(size_t)(c0 + g0 + u) * stride + j] : 0.f;
+            for (int u = 0; u < G; ++u) {
+                const float wu = __shfl_sync(0xffffffffu, w, g0 + u);
+                if (c0 + g0 + u < chunks) {
 #pragma unroll
-            for (int u = 0; u < G; ++u) acc += v[u] * __shfl_sync(0xffffffffu, w, g0 + u);
+                    for (int d = 0; d < D; ++d) acc[d] += v[u][d] * wu;
+                }
+            }
         }
     }
-    const float o = acc / l;
-    if (a.xop) {
-        uint16_t hi, lo;
-        split_bf16(o, hi, lo);
-        a.xop[(size_t)(2 * r) * a.ld_xop + head * DH + j] = hi;
-        a.xop[(size_t)(2 * r + 1) * a.ld_xop + head * DH + j] = lo;
-    } else {
-        a.out[((size_t)r * a.Hq + head) * DH + j] = f32_bf16bits(o);
+    if constexpr (WARPS > 1) {
+        __shared__ float sm[WARPS][DH + 2];
+        const int used = min(WARPS, (chunks + 31) / 32);
+        if (used > 1) {
+#pragma unroll
+            for (int d = 0; d < D; ++d) sm[share][lane * D + d] = acc[d];
+            if (lane == 0) { sm[share][DH] = mu; sm[share][DH + 1] = l; }
+            __syncthreads();
+            if (share) return;
+            for (int x = 1; x < used; ++x) mu = fmaxf(mu, sm[x][DH]);
+            const float ref = mu == -INFINITY ? 0.f : mu;
+            l = 0.f;
+#pragma unroll
+            for (int d = 0; d < D; ++d) acc[d] = 0.f;
+            for (int x = 0; x < used; ++x) {
+                const float w = exp2f(sm[x][DH] - ref);
+                l += sm[x][DH + 1] * w;
+#pragma unroll
+                for (int d = 0; d < D; ++d) acc[d] += sm[x][lane * D + d] * w;
+            }
+        } else if (share) return;
+    }
+#pragma unroll
+    for (int d = 0; d < D; ++d) {
+        const float o = acc[d] / l;
+        if (a.xop) {
+            uint16_t hi, lo;
+            split_bf16(o, hi, lo);
+            a.xop[(size_t)(2 * r) * a.ld_xop + head * DH + lane * D + d] = hi;
+            a.xop[(size_t)(2 * r + 1) * a.ld_xop + head * DH + lane * D + d] = lo;
+        } else {
+            a.out[((size_t)r * a.Hq + head) * DH + lane * D + d] = f32_bf16bits(o);
+        }
     }
 }
 
@@ -1400,7 +1442,9 @@ int attn8_launch(void (*kern)(const Attn8Args), int ctas, int threads, int smem,
         *raised = e == cudaSuccess;
     }
     if (e == cudaSuccess) e = launch_chained(kern, dim3(ctas), dim3(threads), (size_t)smem, st, a);
-    if (e == cudaSuccess) e = launch_chained(kv8_merge_kernel<DH>, dim3(a.Hq, rows), dim3(DH), 0, st, a);
+    // (more than 32 chunks: long contexts of a few rows)
+    if (e == cudaSuccess) e = a.slots > 32 ? launch_chained(kv8_merge_kernel<DH, 4>, dim3(a.Hq * rows), dim3(128), 0, st, a)
+                                           : launch_chained(kv8_merge_kernel<DH, 1>, dim3((a.Hq * rows + 3) / 4), dim3(128), 0, st, a);
     return (int)e;
 }
 template <int DH, int RW, int WR>
