@@ -374,8 +374,9 @@ struct Item8 {
     int t0, t1;                                      // the chunk's tokens [t0, t1): never empty, the sequence's last row sees them all
 };
 
-// The list itself. An item has PAIRS pairs; it costs EACH and one for every STRIDE tokens.
-template <int PAIRS, int STRIDE, int EACH>
+// The list itself. An item has PAIRS pairs; it costs EACH and one for every STRIDE tokens, the
+// first of a context FRESH more.
+template <int PAIRS, int STRIDE, int EACH, int FRESH>
 struct List8 {
     int *prefix, *pcost;                             // [B + 1] items before a sequence, and their cost
     int *tpos, *tval, *tchk, *tnum;                  // position of a sequence's row 0, its rows that count, tokens of its chunks (log2), chunks | sets << 16
@@ -408,7 +409,7 @@ struct List8 {
                     const int n = row_ctx(len, nv - 1), chunks = ((n - 1) >> c) + 1, sets = (nv * a.gq + PAIRS - 1) / PAIRS;
                     tnum[s] = chunks | (sets << 16);
                     cnt[u] = chunks * a.Hkv * sets;
-                    cost[u] = (chunks * EACH + (n + STRIDE - 1) / STRIDE) * a.Hkv * sets;
+                    cost[u] = (FRESH + chunks * EACH + (n + STRIDE - 1) / STRIDE) * a.Hkv * sets;
                     if (len + nv > max_tokens && blockIdx.x == 0) atomicOr(a.status, kDevBadPos);
                 }
             }
@@ -437,7 +438,8 @@ struct List8 {
         while (pcost[s + 1] <= x) ++s;
         const int rem = x - pcost[s], chunks = tnum[s] & 0xffff;
         const int cost = (pcost[s + 1] - pcost[s]) / (Hkv * (tnum[s] >> 16)), ctx = rem / cost, one = (1 << tchk[s]) / STRIDE + EACH;
-        return prefix[s] + ctx * chunks + min((rem - ctx * cost + one - 1) / one, chunks);
+        const int in = rem - ctx * cost;             // (item k > 0 starts at FRESH + k * one)
+        return prefix[s] + ctx * chunks + (in == 0 ? 0 : min(max((in - FRESH + one - 1) / one, 1), chunks));
     }
     __device__ __forceinline__ void bounds(Item8 &it) const {
         const int c = tchk[it.seq];
@@ -481,7 +483,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, wr = warp % WR, wt = warp / WR;
     const int gq = a.gq;
     constexpr int STRIDE = WT * kA8Blk;              // tokens from one stage of a group to its next
-    List8<8 * TILES, STRIDE, 1> list(a, smem + Lay::O_TAB);
+    List8<8 * TILES, STRIDE, 1, 0> list(a, smem + Lay::O_TAB);
     if (warp == 0) list.build(a, lane);
     __syncwarp();
     __syncthreads();
@@ -937,7 +939,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
     uint64_t *pready = sfull + 2, *qready = pready + 1, *drain = qready + 1;
     volatile uint32_t *words = reinterpret_cast<volatile uint32_t *>(smem + Lay::O_WORDS), *abort_flag = words + 1;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    List8<kT8Pairs, kT8Blk, 2> list(a, smem + Lay::O_LIST);
+    List8<kT8Pairs, kT8Blk, 2, 3> list(a, smem + Lay::O_LIST);
     if (tid == 32) {
         for (int i = 0; i < kT8KStages; ++i) { mbar_init(&kfull[i], kT8Copiers); mbar_init(&kempty[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&vfull[i], kT8Copiers); mbar_init(&vempty[i], 1); mbar_init(&sfull[i], 1); }
