@@ -490,3 +490,58 @@ def test_refusals():
     at(x, ok, 1, 1, o)
     assert ctx.launch_count > launches
     ctx.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,page,M", [(16, 2, 128, 16, 5), (64, 8, 128, 48, 16), (8, 8, 128, 16, 64), (28, 4, 128, 32, 64),
+                                              (8, 1, 128, 5, 9), (8, 2, 64, 16, 17)])
+def test_attention_of_many_pairs_against_64_bits(Hq, Hkv, dh, page, M):
+    """40, 128, 64 and 448 pairs per KV head in tiles of 128; blocks that are no whole 16 tokens and head dimension 64, which have none."""
+    test_attention_against_64_bits(Hq, Hkv, dh, page, M)
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,M", [(8, 1, 128, 1), (8, 1, 128, 4), (8, 1, 128, 8), (8, 1, 64, 8)])
+def test_attention_with_scores_and_scales_that_climb(Hq, Hkv, dh, M):
+    """Every block's scores lie far above the ones before and its V scale is larger or far smaller: the reference and the largest
+    V scale move many times within a chunk, down to a scale that counts as nothing."""
+    Bd, rng = _bd(), np.random.default_rng(31 + M + dh)
+    page, L = 16, 700
+    ctx = Bd.Context(_shape(Hq, Hkv, dh, page), max_rows=8, max_K=1, max_ctx=1024)
+    kv = _cache(rng, Hkv, dh, page, [L + M], M, garbage=False)
+    kv["seq_lens"] = np.asarray([L], dtype=np.int32)
+    q = torch.ones((1, M, Hq, dh), dtype=torch.bfloat16, device="cuda") * 2.0 ** -6
+    for i, pg in enumerate(kv["block_table"][0][:(L + M + page - 1) // page]):
+        kv["k_pages"][pg] = R.encode(np.full((Hkv, page, dh), 1.0) + 0.25 * rng.integers(0, 2, (Hkv, page, dh)))
+        kv["k_scales"][pg] = 0.5 + 0.75 * i
+        kv["v_scales"][pg] = (2.0 ** (i / 2 - 10), 1.5, 2.0 ** -90)[i % 3]
+    dev = _to_gpu(kv)
+    out, st = _attend(Bd, ctx, dev, q, 1, M, None)
+    for w in "kv":
+        kv[w + "_scales"] = dev[w + "_scales"].cpu().numpy()
+    ref, tol = R.attention(kv, q.double().cpu().numpy(), [M], page)
+    err = np.abs(out.double().cpu().numpy() - ref)
+    assert np.all(err <= tol), float((err / tol).max())
+    assert int(st.item()) == 0
+    ctx.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,M", [(28, 4, 128, 1), (28, 4, 128, 4), (64, 8, 128, 8), (28, 4, 128, 64), (16, 2, 64, 20)])
+def test_attention_puts_a_value_that_is_no_number_where_it_is_seen(Hq, Hkv, dh, M):
+    """One dimension of one token's value, committed or new: that dimension of the rows that see it, and no other bit."""
+    Bd, rng = _bd(), np.random.default_rng(41 + M)
+    page, lens = 16, [0, 70, 600]
+    ctx = Bd.Context(_shape(Hq, Hkv, dh, page), max_rows=3 * M, max_K=1, max_ctx=1024)
+    kv = _cache(rng, Hkv, dh, page, [L + M for L in lens], M)
+    kv["seq_lens"] = np.asarray(lens, dtype=np.int32)
+    dev = _to_gpu(kv)
+    q, _ = _bf16(rng, (3, M, Hq, dh))
+    good, _ = _attend(Bd, ctx, dev, q, 3, M, None)
+    want = good.clone()
+    g = Hq // Hkv
+    for b, L in enumerate(lens):
+        for p, kvh, d in ((L + M // 2, 0, 3), (L + M - 1, Hkv - 1, dh - 2)) + (((L - 30, 1, 17),) if L else ()):
+            dev["v_pages"][int(kv["block_table"][b, p // page]), kvh, p % page, d] = R.NAN_CODE | (0x80 if d == 3 else 0)
+            want[b, max(0, p - L):, kvh * g:(kvh + 1) * g, d] = float("nan")
+    out, _ = _attend(Bd, ctx, dev, q, 3, M, None)
+    assert torch.equal(torch.isnan(want), torch.isnan(out))
+    assert torch.equal(want.nan_to_num(7.0), out.nan_to_num(7.0))
+    ctx.close()
