@@ -364,7 +364,9 @@ int fastmtp_kv8_read(fmtp_ctx *ctx, const fmtp_kv8 *kv, int B, int max_n, const 
  *
  * M = 1 is a decoding step, M = K+1 scores drafts, up to M = 64 a chunk of a prompt. A query that is not finite gives NaN. Queries
  * beyond the last slot see all slots and are flagged. Requires B*M <= max_rows, M <= 64. Results do not depend on the batch
- * a sequence is in; rows scored with another M agree within rounding (the context is cut at other places). */
+ * a sequence is in; rows scored with another M agree within rounding (the context is cut at other places). Rounding: a probability
+ * is off by 2^-12 of itself, the output is bf16; with more than 32 pairs of a row and a query head per KV head (dh = 128, page_size a
+ * multiple of 16) a query element below 2^-10 of its row's and head's largest is off by up to 2^-18 of that one. */
 int fastmtp_kv8_attention(fmtp_ctx *ctx, const fmtp_bf16 *q, long long ldq, const fmtp_kv8 *kv, int B, int M, const int32_t *n_new,
                           fmtp_bf16 *out, uint32_t *dev_status, void *stream);
 

@@ -68,6 +68,10 @@ __device__ __forceinline__ float scale_for(uint32_t amax_bits) {
 // [first, end) of the block are new, those before `first` committed. The new scale covers the new tokens and is never below the
 // committed tokens' one; where it grows, these are rounded once more (a shift of the exponent, exact but for subnormal codes).
 // What lies behind `end` (rejected drafts, nothing) is left and does not count.
+// A block's new rows have to be seen before its scale is known: up to 16 of them are read once, into registers (eight times 16 bytes per
+// lane at dh = 128), the largest value is found by shuffles and the codes leave as 8-byte stores. Bound by the copy rate where there is much to do (16
+// prompts of up to 4096 tokens, 4 x 128: 23.4 us, 4.3 TB/s; rows requested before the block table's entry: 25.4 us before), by the
+// launch where there is little.
 struct Append8Args {
     int Hkv, page, shift, max_ctx, B, M, nb;         // nb: blocks that M rows can touch
     const bf16_t *k, *v;
@@ -168,7 +172,8 @@ __global__ void __launch_bounds__(kAppendWarps * 32, 8) kv8_append_kernel(const 
     }
 }
 
-// ---- reading back: a warp takes 16 tokens of one sequence and KV head, 16 codes per lane and step.
+// ---- reading back: a warp takes 16 tokens of one sequence and KV head, 16 codes per lane and step, all requested before the first is
+// converted. Bound by the copy rate: 32 ragged caches of 8 x 128 (286 MB of codes, twice that written) 155 us, 85% of it.
 struct Read8Args {
     int Hkv, page, shift, max_ctx, B, max_n, tiles;
     const int32_t *start, *count;
@@ -241,11 +246,16 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv8_read_kernel(const Read8Ar
     }
 }
 
-// ---- attention. The (row, query head) pairs that share a KV head of a sequence are dealt to tiles of eight; a work item is one chunk of
-// a sequence's context for one KV head and a set of RW * WR tiles. A CTA of four warps walks a contiguous range of items. Its
-// WT = 4 / WR groups of WR warps take the chunk's 32-token stages in turn, each with a ring of its own, and meet at the chunk's end,
-// where their results are joined in shared memory; a group's warps take RW tiles each, which share the conversions. (A warp for an item kept the SMs busy
-// for three quarters of the time: an item of 256 tokens took it 25 us.)
+// ---- attention. Two kernels and a join. kv8_attn_kernel, here: the (row, query head) pairs that share a KV head of a sequence are dealt to tiles of
+// eight; a work item is one chunk of a sequence's context for one KV head and a set of RW * WR tiles. A CTA of four warps walks a
+// contiguous range of items. Its WT = 4 / WR groups of WR warps take the chunk's 32-token stages in turn, each with a ring of its own, and meet at
+// the chunk's end, where their results are joined in shared memory; a group's warps take RW tiles each, which share the
+// conversions. (A warp for an item kept the SMs busy for three quarters of the time: an item of 256 tokens took it 25 us.)
+//
+// What bounds it (B200): instructions. A stage of one tile is about 700 of them, 128 conversions and 32 products among them, at 1.3 to 1.9 per cycle and
+// SM with 12 warps; the bytes alone would take two thirds of the time. 64 contexts of 512 to 8192 tokens, 28/4 heads of 128, one row each: 68 us, 4.4
+// TB/s of codes and scales (66% of the measured copy rate); two contexts of 50 000 to 60 000 tokens, 32/8 heads: 50 us, 4.5 TB/s. Short calls are latency: 2048
+// tokens of one sequence 11 us in two launches.
 //
 // Both products run on mma.sync.m16n8k16 with f16 operands (sm_100a has no mma.sync on e4m3: the assembler emulates it with fifteen
 // instructions each). K and V are the A operand, 16 tokens or 16 dims, so that eight pairs fill the n side: S^T = K Q^T, O^T = V^T
@@ -279,7 +289,7 @@ constexpr float kP8Max = 15.f;                       // and the reference is mov
 constexpr float kQ8 = 32.f;                          // queries below 448 * 32
 
 // Tokens of a chunk: a function of the sequence's committed length and of the call's rows per sequence, never of the batch. Short
-// enough for a context to keep many CTAs busy, long enough for the partial results (dh + 2 fp32 values for each pair and chunk,
+// enough for a context to keep many CTAs busy, long enough for the partial results (dh + 4 fp32 words for each pair and chunk,
 // 512 bytes against 256 bytes of K/V per token at dh = 128) to stay a small part of the traffic: up to `few` chunks until a chunk is
 // 2^base long, up to `most` chunks of that and more tokens beyond.
 struct Chunk8 { int first, few, base, most; };       // first and base: powers of two
@@ -892,9 +902,13 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
 // largest), both against the same K tile. Values: f16 operands, the codes converted on the way into shared memory, the probabilities
 // rounded to 2^-12 of themselves; V's tile is token-major, which is the product's MN-major operand.
 // Warps 0-3 are the softmax, a thread a row (its scores are 64 columns of the thread's TMEM lane): the row's maximum and sum need no exchange.
-// Warps 4-7 bring K (cp.async, two blocks ahead) and V (through registers, one ahead); one thread of warp 8 issues the products:
+// Warps 4-7 bring K (cp.async) and V (through registers), both two blocks ahead; one thread of warp 8 issues the products:
 // block n + 1's scores before block n's values, which wait for its probabilities. Two CTAs per SM: one's softmax runs beside the other's
-// products.
+// products. What bounds it (B200): issue and latency of softmax and conversions, 5 200 warp instructions per block at 1.8 per cycle and SM (a
+// block's exponentials alone are 512 cycles of an SM, its products 256), and the ends: 4 us of set-up and first loads, 5 us of
+// queries, 3 us for each chunk's result. Four contexts of 3500 to 4200 tokens, 64 rows each, 28/4 heads: 61 us with the join (7 us); held scores
+// (64 registers, spilt) 109 us, page look-ups one block ahead 84 us. Without the search for a maximum (block's exponentials first, again where one
+// does not fit f16) wide scores took 70 instead of 66 us.
 constexpr int kT8Pairs = 128, kT8Blk = 64, kT8Threads = 288, kT8Copiers = 128, kT8KStages = 3;
 constexpr unsigned long long kT8WaitNs = 2000000000ull;
 struct Tile8Block {                                  // per V buffer, written beside its values
@@ -1455,7 +1469,12 @@ int attn8_warps(const Attn8Args &a, int rows, int n_sm, bool *raised, cudaStream
     return attn8_launch<DH>(kv8_attn_kernel<DH, RW, WR>, Lay::CTAS * n_sm, kA8Threads, Lay::TOTAL, a, rows, raised, st);
 }
 
-// One tile of pairs: four groups of one warp; two tiles: two groups of two; more: two groups of two warps with two tiles each.
+// One tile of pairs: four groups of one warp; up to four: two groups of two, a set for every two tiles. More: tiles of 128 pairs on tcgen05 where
+// a 16-token tile has one scale (dh = 128), else two groups of two warps with two tiles each. Measured, us, 28/4 heads of 128 (tcgen05 / two tiles per warp): 35
+// pairs of 1 x 4000 tokens 25.1 / 23.4, of 16 x 1000 22.2 / 32.5, 84 pairs of 4 x 4000 28.0 / 43.0, 448 pairs of 1 x 4000 29.3 / 44.2, of 4
+// x 4000 57.8 / 131.9. At 28 pairs tcgen05 loses on few sequences (1 x 4000: 24.6 against 15.1 with groups of two; 17 ragged ones 42.9
+// against 34.1) and wins on many (48 x 2000: 79 against 97). At 28 pairs two tiles per warp: 44 us against 36 (the 17 ragged ones); at 448 pairs one
+// tile per warp: 146 us against 133.
 template <int DH>
 int attn8_pick(const Attn8Args &a, int rows, int n_sm, bool *raised, cudaStream_t st) {
     const int pairs = a.M * a.gq;

@@ -13,6 +13,11 @@
 //
 // A row is cut into equal parts, as many as give every resident CTA one; the CTA that completes a row joins the row's parts and
 // writes its outputs.
+//
+// What bounds it (B200): the pass is bound by instructions, 13 for an element (its power of two, two sums, the strips' maxima) at 1.5 per cycle and SM, not by
+// bytes: 256 rows of 152 064 bf16 with 20 alternatives 35.6 us, 2.2 TB/s (a third of the measured copy rate). Few rows are bound by
+// latency, the pass's and the completing CTA's: four such rows 10.0 us, 75 rows of 32 001 fp32 10.8 us. The 256 rows took 48 us with lists
+// of candidates kept along the way and parts of whole slices, 88 with one element at a time.
 #include "logprobs.cuh"
 #include "ptx.cuh"
 #include "umma.cuh"
