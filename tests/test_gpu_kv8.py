@@ -545,3 +545,43 @@ def test_attention_puts_a_value_that_is_no_number_where_it_is_seen(Hq, Hkv, dh, 
     assert torch.equal(torch.isnan(want), torch.isnan(out))
     assert torch.equal(want.nan_to_num(7.0), out.nan_to_num(7.0))
     ctx.close()
+
+
+def test_tiles_of_pairs_in_graphs_beside_other_streams_and_with_bad_pages():
+    """140 pairs per KV head: a captured call replayed at other lengths, two contexts on two streams at once, a page that does not
+    exist."""
+    Bd, rng = _bd(), np.random.default_rng(51)
+    Hq, Hkv, dh, page, B, M = 28, 4, 128, 16, 5, 20
+    lens = [0, 33, 700, 1500, 64]
+    ctxs = [Bd.Context(_shape(Hq, Hkv, dh, page), max_rows=B * M, max_K=1, max_ctx=2048) for _ in range(2)]
+    kv = _cache(rng, Hkv, dh, page, [L + M + 70 for L in lens], 0, garbage=False)
+    kv["seq_lens"] = np.asarray(lens, dtype=np.int32)
+    dev = _to_gpu(kv)
+    q, _ = _bf16(rng, (B, M, Hq, dh))
+    want, st = _attend(Bd, ctxs[0], dev, q, B, M, None)
+    assert int(st.item()) == 0
+    outs = [torch.zeros_like(want) for _ in ctxs]
+    streams = [torch.cuda.Stream() for _ in ctxs]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for c, s, o in zip(ctxs, streams, outs):
+            c.fastmtp_kv8_attention(q, Bd.kv8(dev), B, M, o, stream=s)
+    torch.cuda.synchronize()
+    assert all(torch.equal(o, want) for o in outs)
+    out = torch.zeros_like(want)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        ctxs[0].fastmtp_kv8_attention(q, Bd.kv8(dev), B, M, out)
+    for step in (3, 64):
+        dev["seq_lens"] += step
+        graph.replay()
+        eager, _ = _attend(Bd, ctxs[1], dev, q, B, M, None)
+        torch.cuda.synchronize()
+        assert torch.equal(out, eager) and torch.isfinite(out.float()).all()
+    dev["block_table"][2, 7] = -5
+    bad, st = _attend(Bd, ctxs[0], dev, q, B, M, None)
+    assert int(st.item()) == Bd.DEV_BAD_PAGE
+    keep = [0, 1, 3, 4]
+    assert torch.equal(bad[keep], out[keep])
+    for c in ctxs:
+        c.close()
