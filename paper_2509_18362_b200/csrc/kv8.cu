@@ -292,9 +292,11 @@ constexpr float kQ8 = 32.f;                          // queries below 448 * 32
 // enough for a context to keep many CTAs busy, long enough for the partial results (dh + 4 fp32 words for each pair and chunk,
 // 512 bytes against 256 bytes of K/V per token at dh = 128) to stay a small part of the traffic: up to `few` chunks until a chunk is
 // 2^base long, up to `most` chunks of that and more tokens beyond.
+// (few = 8 / 16 for 33 to 128 pairs, one set of tiles: 112 pairs of 1 x 4000 tokens 26.2 / 20.4 us, of 4 x 4000 28.9 / 23.2; for 448: 29.4 / 23.2 and
+// 57.6 / 65.7, the sets fill the SMs and each chunk's result costs.)
 struct Chunk8 { int first, few, base, most; };       // first and base: powers of two
 __host__ __device__ __forceinline__ Chunk8 chunk8_rule(int pairs) {
-    return pairs <= 8 ? Chunk8{7, 16, 9, 128} : pairs <= 32 ? Chunk8{7, 16, 9, 64} : Chunk8{8, 8, 9, 32};
+    return pairs <= 8 ? Chunk8{7, 16, 9, 128} : pairs <= 32 ? Chunk8{7, 16, 9, 64} : pairs <= 128 ? Chunk8{8, 16, 9, 32} : Chunk8{8, 8, 9, 32};
 }
 __host__ __device__ __forceinline__ int chunk8(int n_ctx, int pairs) {      // log2
     const Chunk8 r = chunk8_rule(pairs);
@@ -310,7 +312,7 @@ constexpr int kList8Words = 6 * kBatchRows + 2;       // see List8
 
 template <int DH, int RW, int WR>
 struct Attn8Smem {
-    static constexpr int WT = kA8Warps / WR;                                 // workers of a CTA
+    static constexpr int WT = kA8Warps / WR;                                 // groups of a CTA
     static constexpr int CTAS = (DH == 128 ? 3 : 4) - (RW - 1);              // resident per SM
     static constexpr int S = (DH == 128 && RW == 1 ? 8 : 12) / WT;           // stages
     static constexpr int KV = kA8Blk * DH;                                   // bytes of a stage's K (or V) codes
@@ -1470,7 +1472,7 @@ int attn8_warps(const Attn8Args &a, int rows, int n_sm, bool *raised, cudaStream
 }
 
 // One tile of pairs: four groups of one warp; up to four: two groups of two, a set for every two tiles. More: tiles of 128 pairs on tcgen05 where
-// a 16-token tile has one scale (dh = 128), else two groups of two warps with two tiles each. Measured, us, 28/4 heads of 128 (tcgen05 / two tiles per warp): 35
+// a 16-token tile has one scale (dh = 128), else two groups of two warps with two tiles each. Measured, us, 28/4 heads of 128, chunks of 512 (tcgen05 / two tiles per warp): 35
 // pairs of 1 x 4000 tokens 25.1 / 23.4, of 16 x 1000 22.2 / 32.5, 84 pairs of 4 x 4000 28.0 / 43.0, 448 pairs of 1 x 4000 29.3 / 44.2, of 4
 // x 4000 57.8 / 131.9. At 28 pairs tcgen05 loses on few sequences (1 x 4000: 24.6 against 15.1 with groups of two; 17 ragged ones 42.9
 // against 34.1) and wins on many (48 x 2000: 79 against 97). At 28 pairs two tiles per warp: 44 us against 36 (the 17 ragged ones); at 448 pairs one
