@@ -96,6 +96,7 @@ __global__ void __launch_bounds__(kAppendWarps * 32, 8) kv8_append_kernel(const 
     const int i = (int)(t % a.nb), b = (int)(t / a.nb);
     if (b >= a.B) return;
     const int L = kv8_len(a.kv, b), n = kv8_rows(a.n_new, b, a.M);
+    if (n == 0) return;                              // sits out: neither its table nor the scale of its last block is touched
     const int max_tokens = min((int)min((long long)a.kv.max_pages * a.page, (long long)kMaxLen), a.max_ctx);
     const int blk = page_of(L, a.page, a.shift) + i;
     const int at = blk * a.page;                     // position of the block's first token
