@@ -313,6 +313,7 @@ constexpr int kList8Words = 6 * kBatchRows + 2;       // see List8
 
 template <int DH, int RW, int WR>
 struct Attn8Smem {
+    static_assert(WR == 1 || WR == 2, "a CTA has four groups or two");
     static constexpr int WT = kA8Warps / WR;                                 // groups of a CTA
     static constexpr int CTAS = (DH == 128 ? 3 : 4) - (RW - 1);              // resident per SM
     static constexpr int S = (DH == 128 && RW == 1 ? 8 : 12) / WT;           // stages
@@ -325,7 +326,8 @@ struct Attn8Smem {
 };
 
 // (Warp-wide instructions are volatile: the compiler may move an asm statement without side effects into a branch that uses its result,
-// and all lanes have to execute them.)
+// and all lanes have to execute them at once, which the .aligned forms do not see to. So a __syncwarp() stands between them and whatever
+// the lanes could have come through apart: a wait, a copy's conditions, a branch that is the same for all lanes but does not look it.)
 __device__ __forceinline__ void mma_f16(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
     asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
@@ -658,6 +660,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
             asm volatile("cp.async.wait_group %0;" ::"n"(S - 2) : "memory");
             group_sync<WR>(wt);
             copy_stage();                            // into the stage that was read last
+            __syncwarp();
             const uint32_t sb = smem_u32(ring + (size_t)slot * Lay::STAGE);
             last_slot = slot;
             if (++slot == S) slot = 0;
@@ -710,6 +713,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                         for (int i = 0; i < 4; ++i)
                             if (tb + h * 16 + (i >> 1) * 8 + g >= pn[r][i & 1]) y[r][h][i] = -INFINITY;
             }
+            __syncwarp();
             float ym[RW][2], most = -INFINITY;
 #pragma unroll
             for (int r = 0; r < RW; ++r)
@@ -750,6 +754,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                     }
                 }
             }
+            __syncwarp();
             // ---- probabilities
             const bool scaled = !__all_sync(0xffffffffu, sv[0][0] == sv_run && sv[0][1] == sv_run && sv[1][0] == sv_run && sv[1][1] == sv_run);
             uint32_t pb[RW][2][2];
@@ -771,6 +776,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                             y[r][h][2 * u + 1] *= f;
                         }
                 }
+                __syncwarp();
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
@@ -791,6 +797,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                         v[i] &= ~nan;
                         bad |= nan;
                     }
+                    __syncwarp();
                 }
 #pragma unroll
                 for (int h = 0; h < 2; ++h) {
@@ -818,6 +825,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                             }
                     }
             }
+            __syncwarp();
         }
         // ---- the chunk's partial result: o and the sum relative to the reference, the reference (log2 units; what a group does not
         // see of the chunk from its first stage on, it does not see at all)
@@ -831,7 +839,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) l_run[r][e] += __shfl_xor_sync(0xffffffffu, l_run[r][e], x);
             }
-            if (WT == 1 || groups == 1) {
+            if (groups == 1) {
                 if (wt == 0) {
 #pragma unroll
                     for (int e = 0; e < 2; ++e)
@@ -846,7 +854,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                 // Each warp leaves a tile's result in the stage that its group read last (free until the group's next copy), and the tile's warps add
                 // them up in the groups' order, 8 / WT pairs each
                 constexpr int LD = DH + 4;               // (rows of pairs start in different banks)
-                static_assert(WT == 1 || 8 * LD * 4 * WR <= Lay::STAGE, "a tile of each warp fits the stage");
+                static_assert(8 * LD * 4 * WR <= Lay::STAGE, "a tile of each warp fits the stage");
                 float2 *ml = reinterpret_cast<float2 *>(smem + Lay::O_ML);
                 int *last = reinterpret_cast<int *>(smem + Lay::O_LAST);
                 if (r == 0) group_sync<WR>(wt);          // all readers of the stage are done
@@ -1050,6 +1058,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 const uint32_t ph = (uint32_t)(n >> 1) & 1u, tmem_s = tmem + lane_addr + (uint32_t)(b * kT8Blk);
                 ok = tile8_wait(abort_flag, &vfull[b], ph) && tile8_wait(abort_flag, &sfull[b], ph);
                 if (__any_sync(kFull, !ok)) { ok = false; break; }
+                __syncwarp();
                 tc_fence_after_sync();
                 const Tile8Block *blk = reinterpret_cast<const Tile8Block *>(smem + Lay::O_BLK) + b;
                 const float4 sk4 = *reinterpret_cast<const float4 *>(blk->sk), sv4 = *reinterpret_cast<const float4 *>(blk->sv);
@@ -1070,6 +1079,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                     }
                     tmem_st_wait();
                 }
+                __syncwarp();
                 // ---- the largest score (the scores are read from tensor memory twice: 64 of them would not fit the registers)
                 float ym = -INFINITY;
 #pragma unroll 1
@@ -1104,6 +1114,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                     if (__any_sync(kFull, !ok)) { ok = false; break; }
                     tc_fence_after_sync();
                 }
+                __syncwarp();
                 if (!first && __any_sync(kFull, corr != 1.f)) {
 #pragma unroll 1
                     for (int o0 = 0; o0 < DH; o0 += 16) {
@@ -1116,6 +1127,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                     }
                     tmem_st_wait();
                 }
+                __syncwarp();
                 // ---- probabilities, as f16, times their V scales over the largest (2^-60 of it counts as much as nothing): in the exponent,
                 // and taken out of a tile's sum again
                 const float4 sl4 = *reinterpret_cast<const float4 *>(blk->sv_log2), si4 = *reinterpret_cast<const float4 *>(blk->sv_inv);
@@ -1156,6 +1168,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             uint32_t to[8];                          // rows of the four that a warp writes at a time
 #pragma unroll
             for (int i = 0; i < 8; ++i) to[i] = __shfl_sync(kFull, out_row, 4 * i + (lane >> 3));
+            __syncwarp();
 #pragma unroll 1
             for (int c0 = 0; c0 < DH; c0 += 32) {
                 uint32_t o[32];
