@@ -122,7 +122,7 @@ typedef struct {
 /* The same cache held in 8 bits. k_pages / v_pages: dev [num_pages, Hkv, page_size, dh] e4m3 codes (OCP 8-bit floating
  * point: 4 exponent and 3 mantissa bits, largest number 448, no infinity); k_scales / v_scales: dev [num_pages, Hkv], one
  * fp32 scale for each block of tokens (a page) and KV head; a value is code * scale. Half the bytes of fmtp_kv plus 4 bytes in
- * page_size * dh. num_pages * Hkv * page_size < 2^32. Pages are 16-byte aligned. */
+ * page_size * dh. num_pages * Hkv * page_size < 2^32. Pages are 16-byte aligned; scales are positive (or zero, for a block of zeros). */
 typedef struct {
     uint8_t *k_pages, *v_pages;
     float *k_scales, *v_scales;
@@ -364,9 +364,10 @@ int fastmtp_kv8_read(fmtp_ctx *ctx, const fmtp_kv8 *kv, int B, int max_n, const 
  *
  * M = 1 is a decoding step, M = K+1 scores drafts, up to M = 64 a chunk of a prompt. A query that is not finite gives NaN. Queries
  * beyond the last slot see all slots and are flagged. Requires B*M <= max_rows, M <= 64. Results do not depend on the batch
- * a sequence is in; rows scored with another M agree within rounding (the context is cut at other places). Rounding: a probability
- * is off by 2^-12 of itself, the output is bf16; with more than 32 pairs of a row and a query head per KV head (dh = 128, page_size a
- * multiple of 16) a query element below 2^-10 of its row's and head's largest is off by up to 2^-18 of that one. */
+ * a sequence is in, nor a row's on later rows of the call; rows scored with another M agree within rounding (the context is cut at other
+ * places). Rounding: the output is bf16; a token's weight (its probability times its V scale) is held in f16, off by up to 2^-11 of itself
+ * or, where that is more, 2^-27 of its row's and head's largest weight; with more than 32 pairs of a row and a query head per KV head
+ * (dh = 128, page_size a multiple of 16) a query element below 2^-9 of its row's and head's largest is off by up to 2^-17 of that one. */
 int fastmtp_kv8_attention(fmtp_ctx *ctx, const fmtp_bf16 *q, long long ldq, const fmtp_kv8 *kv, int B, int M, const int32_t *n_new,
                           fmtp_bf16 *out, uint32_t *dev_status, void *stream);
 

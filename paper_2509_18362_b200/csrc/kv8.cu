@@ -260,14 +260,16 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv8_read_kernel(const Read8Ar
 //
 // Both products run on mma.sync.m16n8k16 with f16 operands (sm_100a has no mma.sync on e4m3: the assembler emulates it with fifteen
 // instructions each). K and V are the A operand, 16 tokens or 16 dims, so that eight pairs fill the n side: S^T = K Q^T, O^T = V^T
-// P^T. An e4m3 code is exact in f16, a bf16 query (over a power of two, eight bits) as well; a probability is rounded to 2^-12 of
-// itself or 2^-31 of the chunk's largest at least. A word of K is four dims of a token, and the contraction takes them in the order in which a
+// P^T. An e4m3 code is exact in f16, a bf16 query (over a power of two, eight bits) as well. A word of K is four dims of a token, and the contraction takes them in the order in which a
 // lane holds them. V's transposed 16-bit ldmatrix gives dims 2u, 2u + 1 of two tokens in a word, which a byte permutation sorts;
 // movmatrix turns a tile of probabilities from the first product's layout into the second one's.
 //
-// Scores are scaled by the token's K scale, probabilities by its V scale over the largest seen so far (O carries the factor). The
-// reference of the exponentials is the maximum of a group's first stage and is moved only when a score lies 2^9 above it, so most
-// stages need neither the maximum over all lanes nor a rescaling (partial results carry their reference).
+// Scores are scaled by the token's K scale. What is multiplied with V's codes is a weight, a probability times the token's V scale, and weights have a reference of
+// their own for every pair: f16 holds them right over 2^31 only, and where the scales differ, the largest weight need not be the largest
+// probability's. A weight is rounded to 2^-11 of itself or 2^-27 of the pair's largest so far at least; a pair's references depend on what it sees alone.
+// The reference of the exponentials is the maximum of a group's first stage and is moved only when a score lies 2^5 above it, so most
+// stages need neither the maximum over all lanes nor a rescaling (partial results carry their reference). As long as all scales are within 2^3 of the first
+// token's, the weights' reference is the probabilities' times that scale, and a weight costs a product.
 // A stage of the ring is 32 tokens of K and V with their scales, copied by the warps that read them (16-byte cp.async, any page
 // size).
 struct Attn8Args {
@@ -286,7 +288,9 @@ struct Attn8Args {
 constexpr int kA8Warps = 4, kA8Threads = kA8Warps * 32;
 constexpr int kA8Blk = 32;                           // tokens of a stage
 constexpr float kP8Log2 = 6.f;                       // probabilities relative to the reference are held times 2^6: f16 reaches down to 2^-24,
-constexpr float kP8Max = 15.f;                       // and the reference is moved when one comes out above 2^15
+constexpr float kW8Max = 15.f, kW8Min = 2.f;          // the largest weight so far is kept between 2^2 and 2^15
+constexpr float kNear8 = 8.f;                        // V scales within this factor of the reference leave weights and probabilities one reference,
+constexpr float kP8Max = 11.f;                       // which is moved when a probability comes out above 2^11 (times eight: below 2^15)
 constexpr float kQ8 = 32.f;                          // queries below 448 * 32
 
 // Tokens of a chunk: a function of the sequence's committed length and of the call's rows per sequence, never of the batch. Short
@@ -366,8 +370,24 @@ __device__ __forceinline__ float exp2_approx(float x) {      // 2^x; results bel
     asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
     return y;
 }
+__device__ __forceinline__ float min_nan(float a, float b) {         // NaN if one is
+    float r;
+    asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+    return r;
+}
 __device__ __forceinline__ void cp_async4(uint32_t dst, const void *src, uint32_t bytes) {
     asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+}
+// How far (log2) the references of a pair's probabilities and weights move in a stage whose largest exponents are ym and zm: a reference above which
+// something lies too far, or which is not there yet, to 2^6 below the largest. The weights' moves along with the probabilities' (so that
+// equal scales keep both the same) unless the largest weight would leave its range; then it stays or goes its own way.
+struct Moved8 { float p, w; };
+__device__ __forceinline__ Moved8 move8(float ym, float zm, bool first, float most) {
+    Moved8 mv;
+    mv.p = (first || ym > most) && ym > -INFINITY ? ym - kP8Log2 : 0.f;
+    const float z = zm - mv.p;
+    mv.w = z <= kW8Max && (z >= kW8Min || (mv.p == 0.f && !first)) ? mv.p : (first || zm > kW8Max) && zm > -INFINITY ? zm - kP8Log2 : 0.f;
+    return mv;
 }
 // Byte position of 16-byte piece c of token row t: the eight rows an ldmatrix phase reads lie in different banks.
 template <int DH>
@@ -646,11 +666,12 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
             }
         }
         float mo[RW][2], l_run[RW][2], o[RW][ND][4];         // a score's exponent: fma(score, fs, mo)
-        float sv_run = 0.f, sv_inv = 0.f;            // largest V scale so far, its inverse
+        float sv_ref = 1.f, sv_inv = 1.f, vo[RW][2];        // weights (see above) are held times 2^vo / sv_ref
+        bool level = true;                           // all vo are zero
 #pragma unroll
         for (int r = 0; r < RW; ++r) {
             mo[r][0] = mo[r][1] = kP8Log2;
-            l_run[r][0] = l_run[r][1] = 0.f;
+            l_run[r][0] = l_run[r][1] = vo[r][0] = vo[r][1] = 0.f;
 #pragma unroll
             for (int i = 0; i < ND; ++i) o[r][i][0] = o[r][i][1] = o[r][i][2] = o[r][i][3] = 0.f;
         }
@@ -714,6 +735,12 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                             if (tb + h * 16 + (i >> 1) * 8 + g >= pn[r][i & 1]) y[r][h][i] = -INFINITY;
             }
             __syncwarp();
+            const bool first = tb == tb0;
+            if (first) {                             // the group's first token: whoever sees any of its tokens sees this one
+                sv_ref = __shfl_sync(0xffffffffu, sv[0][0], 0);
+                if (!(sv_ref > 0.f && sv_ref < INFINITY)) sv_ref = 1.f;
+                sv_inv = __fdividef(1.0f, sv_ref);
+            }
             float ym[RW][2], most = -INFINITY;
 #pragma unroll
             for (int r = 0; r < RW; ++r)
@@ -722,66 +749,117 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                     ym[r][e] = fmaxf(fmaxf(y[r][0][e], y[r][0][2 + e]), fmaxf(y[r][1][e], y[r][1][2 + e]));
                     most = fmaxf(most, ym[r][e]);
                 }
-            float svm = fmaxf(fmaxf(sv[0][0], sv[0][1]), fmaxf(sv[1][0], sv[1][1]));
-            if (tb == tb0 || __any_sync(0xffffffffu, most > kP8Max || svm > sv_run)) {
-                // new references: the stage's maximum where it is the first or far above, the largest V scale
+            const float s0 = min_nan(min_nan(sv[0][0], sv[0][1]), min_nan(sv[1][0], sv[1][1])), s1 = fmaxf(fmaxf(sv[0][0], sv[0][1]), fmaxf(sv[1][0], sv[1][1]));
+            uint32_t pb[RW][2][2];
+            if (__all_sync(0xffffffffu, level && s0 * kNear8 >= sv_ref && s1 <= sv_ref * kNear8)) {
+                if (first || __any_sync(0xffffffffu, most > kP8Max)) {
+                    // new references: the stage's maximum where it is the first or far above (the weights' move along)
 #pragma unroll
-                for (int x = 4; x < 32; x <<= 1) svm = fmaxf(svm, __shfl_xor_sync(0xffffffffu, svm, x));
-                float vcorr = 1.f;
-                if (svm > sv_run) {
-                    sv_inv = __fdividef(1.0f, svm);
-                    vcorr = sv_run * sv_inv;
-                    sv_run = svm;
+                    for (int r = 0; r < RW; ++r) {
+                        float corr[2];
+#pragma unroll
+                        for (int e = 0; e < 2; ++e) {
+#pragma unroll
+                            for (int x = 4; x < 32; x <<= 1) ym[r][e] = fmaxf(ym[r][e], __shfl_xor_sync(0xffffffffu, ym[r][e], x));
+                            const float d = (first || ym[r][e] > kP8Max) && ym[r][e] > -INFINITY ? ym[r][e] - kP8Log2 : 0.f;
+                            mo[r][e] -= d;
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) { y[r][h][e] -= d; y[r][h][2 + e] -= d; }
+                            corr[e] = first ? 1.f : exp2_approx(-d);
+                            l_run[r][e] *= corr[e];
+                        }
+                        if (!first) {
+#pragma unroll
+                            for (int i = 0; i < ND; ++i) { o[r][i][0] *= corr[0]; o[r][i][1] *= corr[1]; o[r][i][2] *= corr[0]; o[r][i][3] *= corr[1]; }
+                        }
+                    }
                 }
+                __syncwarp();
+                // ---- probabilities and, as f16, weights
+                const bool scaled = !__all_sync(0xffffffffu, s0 == sv_ref && s1 == sv_ref);
+#pragma unroll
+                for (int r = 0; r < RW; ++r) {
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) y[r][h][i] = exp2_approx(y[r][h][i]);
+                    l_run[r][0] += (y[r][0][0] + y[r][0][2]) + (y[r][1][0] + y[r][1][2]);
+                    l_run[r][1] += (y[r][0][1] + y[r][0][3]) + (y[r][1][1] + y[r][1][3]);
+                    if (scaled) {
+#pragma unroll
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                const float f = sv[h][u] * sv_inv;
+                                y[r][h][2 * u] *= f;
+                                y[r][h][2 * u + 1] *= f;
+                            }
+                    }
+#pragma unroll
+                    for (int h = 0; h < 2; ++h)
+#pragma unroll
+                        for (int u = 0; u < 2; ++u) pb[r][h][u] = pack_f16x2(y[r][h][2 * u], y[r][h][2 * u + 1]);
+                }
+            } else {
+                // the same with weights that have references of their own
+                const float sv_log2 = __log2f(sv_ref);
+                float lf[2][2];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) {
+                        lf[h][u] = __log2f(sv[h][u]) - sv_log2;
+                        if (lf[h][u] < -300.f) lf[h][u] = -300.f;        // a scale of zero
+                    }
+                bool zero = true;
 #pragma unroll
                 for (int r = 0; r < RW; ++r) {
                     float corr[2];
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
+                        float z = fmaxf(fmaxf(y[r][0][e] + lf[0][0], y[r][0][2 + e] + lf[0][1]), fmaxf(y[r][1][e] + lf[1][0], y[r][1][2 + e] + lf[1][1]));
 #pragma unroll
-                        for (int x = 4; x < 32; x <<= 1) ym[r][e] = fmaxf(ym[r][e], __shfl_xor_sync(0xffffffffu, ym[r][e], x));
-                        const float d = (tb == tb0 || ym[r][e] > kP8Max) && ym[r][e] > -INFINITY ? ym[r][e] - kP8Log2 : 0.f;
-                        mo[r][e] -= d;
+                        for (int x = 4; x < 32; x <<= 1) {
+                            ym[r][e] = fmaxf(ym[r][e], __shfl_xor_sync(0xffffffffu, ym[r][e], x));
+                            z = fmaxf(z, __shfl_xor_sync(0xffffffffu, z, x));
+                        }
+                        const Moved8 mv = move8(ym[r][e], z + vo[r][e], first, kP8Max);
+                        mo[r][e] -= mv.p;
+                        vo[r][e] += mv.p - mv.w;
+                        zero = zero && vo[r][e] == 0.f;
+                        l_run[r][e] *= first ? 1.f : exp2_approx(-mv.p);
+                        corr[e] = first ? 1.f : exp2_approx(-mv.w);
+                        float sum[2];
 #pragma unroll
-                        for (int h = 0; h < 2; ++h) { y[r][h][e] -= d; y[r][h][2 + e] -= d; }
-                        corr[e] = tb == tb0 ? 1.f : exp2_approx(-d);
-                        l_run[r][e] *= corr[e];
-                        corr[e] *= vcorr;
+                        for (int h = 0; h < 2; ++h)
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                const float x = y[r][h][2 * u + e] - mv.p, f = sv[h][u] * sv_inv, p = exp2_approx(x);
+                                sum[h] = u ? sum[h] + p : p;
+                                // (what a pair gets does not depend on which of the two ways its stage takes)
+                                const float w = vo[r][e] == 0.f && f >= 1.0f / kNear8 && f <= kNear8 ? p * f : exp2_approx(x + (lf[h][u] + vo[r][e]));
+                                y[r][h][2 * u + e] = x == -INFINITY ? 0.f : w;
+                            }
+                        l_run[r][e] += sum[0] + sum[1];
                     }
-                    if (tb != tb0) {
+                    if (!first) {
 #pragma unroll
                         for (int i = 0; i < ND; ++i) { o[r][i][0] *= corr[0]; o[r][i][1] *= corr[1]; o[r][i][2] *= corr[0]; o[r][i][3] *= corr[1]; }
                     }
-                }
-            }
-            __syncwarp();
-            // ---- probabilities
-            const bool scaled = !__all_sync(0xffffffffu, sv[0][0] == sv_run && sv[0][1] == sv_run && sv[1][0] == sv_run && sv[1][1] == sv_run);
-            uint32_t pb[RW][2][2];
-#pragma unroll
-            for (int r = 0; r < RW; ++r) {
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) y[r][h][i] = exp2_approx(y[r][h][i]);
-                l_run[r][0] += (y[r][0][0] + y[r][0][2]) + (y[r][1][0] + y[r][1][2]);
-                l_run[r][1] += (y[r][0][1] + y[r][0][3]) + (y[r][1][1] + y[r][1][3]);
-                if (scaled) {
 #pragma unroll
                     for (int h = 0; h < 2; ++h)
 #pragma unroll
-                        for (int u = 0; u < 2; ++u) {
-                            const float f = sv[h][u] * sv_inv;
-                            y[r][h][2 * u] *= f;
-                            y[r][h][2 * u + 1] *= f;
-                        }
+                        for (int u = 0; u < 2; ++u) pb[r][h][u] = pack_f16x2(y[r][h][2 * u], y[r][h][2 * u + 1]);
                 }
-                __syncwarp();
+                level = __all_sync(0xffffffffu, zero);
+            }
+            __syncwarp();
+#pragma unroll
+            for (int r = 0; r < RW; ++r)
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
 #pragma unroll
-                    for (int u = 0; u < 2; ++u) pb[r][h][u] = movmatrix_trans(pack_f16x2(y[r][h][2 * u], y[r][h][2 * u + 1]));
-            }
+                    for (int u = 0; u < 2; ++u) pb[r][h][u] = movmatrix_trans(pb[r][h][u]);
             // ---- weighted values: dims 16 c + 2 g, 16 c + 2 g + 1 of pairs kq, kq + 1. In a stage that some row does not see whole, what
             // it does not see is a later row's value and need not be a number: there a value that is no number counts as 0 in the
             // products, and is put in afterwards where it is seen
@@ -832,9 +910,10 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
         const int groups = min(WT, (it.t1 - it.t0 + kA8Blk - 1) / kA8Blk);       // the others had none of the chunk's stages
 #pragma unroll
         for (int r = 0; r < RW; ++r) {
-            float m_ref[2];
+            float m_ref[2], back[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
+                back[e] = vo[r][e] == 0.f ? sv_ref : exp2f(__log2f(sv_ref) - vo[r][e]);
                 m_ref[e] = pn[r][e] > tb0 ? kP8Log2 - mo[r][e] : -INFINITY;
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) l_run[r][e] += __shfl_xor_sync(0xffffffffu, l_run[r][e], x);
@@ -846,7 +925,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                         if (prow[r][e] < nv && pn[r][e] > it.t0) {             // such a pair, and it sees something of the chunk
                             float *out = a.part + pout[r][e] + (size_t)it.chunk * part8_ld(DH);
 #pragma unroll
-                            for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(out + c * 16 + g * 2) = make_float2(o[r][c][e] * sv_run, o[r][c][2 + e] * sv_run);
+                            for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(out + c * 16 + g * 2) = make_float2(o[r][c][e] * back[e], o[r][c][2 + e] * back[e]);
                             if (g == 0) *reinterpret_cast<float2 *>(out + DH) = make_float2(m_ref[e], l_run[r][e]);
                         }
                 }
@@ -863,7 +942,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
 #pragma unroll
                     for (int e = 0; e < 2; ++e) {
 #pragma unroll
-                        for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(mine + (kq + e) * LD + c * 16 + g * 2) = make_float2(o[r][c][e] * sv_run, o[r][c][2 + e] * sv_run);
+                        for (int c = 0; c < ND; ++c) *reinterpret_cast<float2 *>(mine + (kq + e) * LD + c * 16 + g * 2) = make_float2(o[r][c][e] * back[e], o[r][c][2 + e] * back[e]);
                         if (g == 0) ml[warp * 8 + kq + e] = make_float2(m_ref[e], l_run[r][e]);
                     }
                     if (lane == 0 && wr == 0) last[wt] = last_slot;
@@ -909,9 +988,9 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
 
 // ---- attention of many pairs per KV head (dh = 128): a set is 128 pairs, the rows of a tcgen05 tile, and an item a chunk of a context
 // for one KV head and a set; blocks of 64 tokens. Scores: K's codes are an e4m3 operand as they lie in the cache, a query
-// is two (its nearest e4m3 and the rest's: 8 bits, a bf16's own, down to 2^-10 of the row's largest element; below that it is off by 2^-18 of the
-// largest), both against the same K tile. Values: f16 operands, the codes converted on the way into shared memory, the probabilities
-// rounded to 2^-12 of themselves; V's tile is token-major, which is the product's MN-major operand.
+// is two (its nearest e4m3 and the rest's: 8 bits, a bf16's own, down to 2^-9 of the row's largest element; below that it is off by up to 2^-17 of the
+// largest), both against the same K tile. Values: f16 operands, the codes converted on the way into shared memory, the weights (probability times V scale)
+// rounded as in kv8_attn_kernel, with a reference of each row's own; V's tile is token-major, which is the product's MN-major operand.
 // Warps 0-3 are the softmax, a thread a row (its scores are 64 columns of the thread's TMEM lane): the row's maximum and sum need no exchange.
 // Warps 4-7 bring K (cp.async) and V (through registers), both two blocks ahead; one thread of warp 8 issues the products:
 // block n + 1's scores before block n's values, which wait for its probabilities. Two CTAs per SM: one's softmax runs beside the other's
@@ -923,7 +1002,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
 constexpr int kT8Pairs = 128, kT8Blk = 64, kT8Threads = 288, kT8Copiers = 128, kT8KStages = 3;
 constexpr unsigned long long kT8WaitNs = 2000000000ull;
 struct Tile8Block {                                  // per V buffer, written beside its values
-    float sk[4], sv[4], sv_log2[4], sv_inv[4];       // of the block's 16-token tiles
+    float sk[4], sv_log2[4];                         // of the block's 16-token tiles
     uint32_t bad[4];                                 // values that are no number were left out (see kv8_attn_kernel); of each copy warp
 };
 struct Tile8Smem {
@@ -935,7 +1014,7 @@ struct Tile8Smem {
     static constexpr int O_LIST = O_WORDS + 8;
     static constexpr int TOTAL = O_LIST + kList8Words * 4;
 };
-static_assert(sizeof(Tile8Block) % 16 == 0 && offsetof(Tile8Block, sv) == 16 && 2 * (Tile8Smem::TOTAL + 1024) <= 228 * 1024, "two CTAs per SM");
+static_assert(sizeof(Tile8Block) % 16 == 0 && offsetof(Tile8Block, sv_log2) == 16 && 2 * (Tile8Smem::TOTAL + 1024) <= 228 * 1024, "two CTAs per SM");
 
 __device__ __forceinline__ bool tile8_wait(volatile uint32_t *abort_flag, uint64_t *bar, uint32_t parity) {
     if (mbar_try_wait(bar, parity)) return true;
@@ -1050,7 +1129,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 fence_proxy_async();
                 mbar_arrive(qready);
             }
-            float mo = kP8Log2, l_run = 0.f, sv_run = 0.f, sv_log2 = 0.f;
+            float mo = kP8Log2, l_run = 0.f, vo = 0.f;           // weights are held times 2^vo
             uint32_t bad = 0;
 #pragma unroll 1
             for (int tb = it.t0; tb < it.t1; tb += kT8Blk, ++n) {
@@ -1061,7 +1140,10 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 __syncwarp();
                 tc_fence_after_sync();
                 const Tile8Block *blk = reinterpret_cast<const Tile8Block *>(smem + Lay::O_BLK) + b;
-                const float4 sk4 = *reinterpret_cast<const float4 *>(blk->sk), sv4 = *reinterpret_cast<const float4 *>(blk->sv);
+                const float4 sk4 = *reinterpret_cast<const float4 *>(blk->sk);
+                float4 sl4 = *reinterpret_cast<const float4 *>(blk->sv_log2);
+                const bool first = tb == it.t0;
+                if (first) vo = -sl4.x;              // (the chunk's first tile, which every row sees that sees any of it)
                 const uint4 bd = *reinterpret_cast<const uint4 *>(blk->bad);
                 bad |= bd.x | bd.y | bd.z | bd.w;
                 // a code product times c is a score in log2 units (c > 0: nothing seen, -inf, stays that)
@@ -1081,12 +1163,12 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 }
                 __syncwarp();
                 // ---- the largest score (the scores are read from tensor memory twice: 64 of them would not fit the registers)
-                float ym = -INFINITY;
+                float ym = -INFINITY, zm = -INFINITY;
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     uint32_t x[32];
                     tmem_ld32_issue(tmem_s + (uint32_t)(h * 32), x);
-                    const float ch[2] = {h ? c[2] : c[0], h ? c[3] : c[1]};
+                    const float ch[2] = {h ? c[2] : c[0], h ? c[3] : c[1]}, lh[2] = {h ? sl4.z : sl4.x, h ? sl4.w : sl4.y};
                     tmem_ld_wait();
 #pragma unroll
                     for (int g = 0; g < 2; ++g) {
@@ -1094,20 +1176,16 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
 #pragma unroll
                         for (int j = 0; j < 4; ++j) m4[j] = fmaxf(fmaxf(__uint_as_float(x[g * 16 + j]), __uint_as_float(x[g * 16 + 4 + j])),
                                                                   fmaxf(__uint_as_float(x[g * 16 + 8 + j]), __uint_as_float(x[g * 16 + 12 + j])));
-                        ym = fmaxf(ym, fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), ch[g], mo));
+                        const float yg = fmaf(fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3])), ch[g], mo);
+                        ym = fmaxf(ym, yg);
+                        zm = fmaxf(zm, yg + (lh[g] + vo));
                     }
                 }
-                const bool first = tb == it.t0;
-                const float d = (first || ym > kP8Max) && ym > -INFINITY ? ym - kP8Log2 : 0.f;
-                mo -= d;
-                float corr = first ? 1.f : exp2_approx(-d);
-                l_run *= corr;
-                const float svm = fmaxf(fmaxf(sv4.x, sv4.y), fmaxf(sv4.z, sv4.w));
-                if (svm > sv_run) {
-                    corr *= __fdividef(sv_run, svm);
-                    sv_run = svm;
-                    sv_log2 = __log2f(svm);
-                }
+                const Moved8 mv = move8(ym, zm, first, kW8Max);
+                mo -= mv.p;
+                vo += mv.p - mv.w;
+                const float corr = first ? 1.f : exp2_approx(-mv.w);
+                l_run *= first ? 1.f : exp2_approx(-mv.p);
                 // ---- the block before has been added up: its probabilities may be overwritten, what it left can be scaled
                 if (n > 0) {
                     ok = tile8_wait(abort_flag, &vempty[b ^ 1], (uint32_t)((n - 1) >> 1) & 1u);
@@ -1128,11 +1206,11 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                     tmem_st_wait();
                 }
                 __syncwarp();
-                // ---- probabilities, as f16, times their V scales over the largest (2^-60 of it counts as much as nothing): in the exponent,
-                // and taken out of a tile's sum again
-                const float4 sl4 = *reinterpret_cast<const float4 *>(blk->sv_log2), si4 = *reinterpret_cast<const float4 *>(blk->sv_inv);
-                const float e[4] = {mo + fmaxf(sl4.x - sv_log2, -60.f), mo + fmaxf(sl4.y - sv_log2, -60.f), mo + fmaxf(sl4.z - sv_log2, -60.f), mo + fmaxf(sl4.w - sv_log2, -60.f)};
-                const float f[4] = {fminf(si4.x * sv_run, 0x1p60f), fminf(si4.y * sv_run, 0x1p60f), fminf(si4.z * sv_run, 0x1p60f), fminf(si4.w * sv_run, 0x1p60f)};
+                // ---- weights as f16: a tile's V scale is in the exponent, and taken out of its sum again (a weight 2^-60 of its probability
+                // counts as that: it is nothing beside the largest)
+                sl4 = *reinterpret_cast<const float4 *>(blk->sv_log2);
+                const float t[4] = {fmaxf(sl4.x + vo, -60.f), fmaxf(sl4.y + vo, -60.f), fmaxf(sl4.z + vo, -60.f), fmaxf(sl4.w + vo, -60.f)};
+                const float e[4] = {mo + t[0], mo + t[1], mo + t[2], mo + t[3]}, f[4] = {exp2_approx(-t[0]), exp2_approx(-t[1]), exp2_approx(-t[2]), exp2_approx(-t[3])};
 #pragma unroll 1
                 for (int h = 0; h < 2; ++h) {
                     uint32_t x[32];
@@ -1164,6 +1242,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             tc_fence_after_sync();
             const uint32_t out_row = prow != kFull && pn > it.t0 ? prow * (uint32_t)a.slots + (uint32_t)it.chunk : kFull;
             float *mine = a.part + (size_t)out_row * part8_ld(DH);
+            const float back = exp2f(-vo);
             if (out_row != kFull) *reinterpret_cast<float2 *>(mine + DH) = make_float2(kP8Log2 - mo, l_run);
             uint32_t to[8];                          // rows of the four that a warp writes at a time
 #pragma unroll
@@ -1175,7 +1254,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 tmem_ld32_issue(tmem_o + lane_addr + (uint32_t)c0, o);
                 tmem_ld_wait();
 #pragma unroll
-                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * sv_run);
+                for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(__uint_as_float(o[i]) * back);
 #pragma unroll
                 for (int c = 0; c < 8; ++c) sts128(p_row + (((uint32_t)c ^ sw) << 4), o[4 * c], o[4 * c + 1], o[4 * c + 2], o[4 * c + 3]);
                 __syncwarp();
@@ -1276,11 +1355,8 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 sts128(v1 + o, e4m3lo_f16x2(y.v[u].z), e4m3hi_f16x2(y.v[u].z), e4m3lo_f16x2(y.v[u].w), e4m3hi_f16x2(y.v[u].w));
             }
             if (warp == 4 && lane < 8) {
-                reinterpret_cast<float *>(blk)[lane] = y.scale;        // sk, sv
-                if (lane >= 4) {
-                    blk->sv_log2[lane - 4] = __log2f(y.scale);
-                    blk->sv_inv[lane - 4] = 1.0f / y.scale;
-                }
+                if (lane < 4) blk->sk[lane] = y.scale;
+                else blk->sv_log2[lane - 4] = fmaxf(__log2f(y.scale), -300.f);       // (a scale of zero)
             }
             if (lane == 0) blk->bad[warp - 4] = bad ? 1u : 0u;
             fence_proxy_async();

@@ -74,3 +74,120 @@ def test_append_beside_an_idle_holder_of_the_same_block():
         dev["seq_lens"] += torch.from_numpy(moved).cuda()
     for c in ctxs:
         c.close()
+
+
+def _attention(kv, q, n_new, page):
+    """q [B, M, Hq, dh] float64 -> (out, bound), NaN and 0 in rows that do not count. The bound, element by element, from what the
+    header says of the kernels:
+
+    * the output is bf16: 2^-8 of it;
+    * a weight, w_t = (probability of token t) * (its V scale), is rounded to f16: 2^-11 of itself, or 2^-27 of the row's and head's
+      largest weight (never more than the weight itself, which then counts as nothing), times the token's code;
+    * a score is off by 2^-20 of the sum of its products' magnitudes (products of codes and query elements are exact, fp32 adds
+      them, an MMA keeps 22 bits of the largest), and in tiles of 128 pairs by what a query element below 2^-9 of the row's largest loses
+      in two e4m3 parts, half of a smallest step (2^-10 where the largest lies in 224 .. 448): twice the largest such error
+      enters the output, once above and once below the fraction;
+    * 2^-14 for the powers of two, the scales' logarithms (2^-22 of up to 120) and fp32 sums and joins."""
+    B, M, Hq, dh = q.shape
+    hkv = kv["k_pages"].shape[1]
+    g = Hq // hkv
+    tiles = M * g > 32 and dh == 128 and page % 16 == 0
+    ones = {**kv, "v_scales": np.ones_like(kv["v_scales"])}
+    out, tol = np.full(q.shape, np.nan), np.zeros(q.shape)
+    for b in range(B):
+        if not n_new[b]:
+            continue
+        L = int(kv["seq_lens"][b])
+        T = min(L + int(n_new[b]), kv["block_table"].shape[1] * page)
+        K, V, code = R.tokens(kv, "k", b, T, page), R.tokens(kv, "v", b, T, page), np.abs(R.tokens(ones, "v", b, T, page))
+        pg = kv["block_table"][b, np.arange(T) // page]
+        S = kv["v_scales"][pg].astype(np.float64)
+        for m in range(int(n_new[b])):
+            n = min(L + m + 1, T)
+            for h in range(Hq):
+                k, v, qv = K[:n, h // g], V[:n, h // g], q[b, m, h]
+                s = k @ qv / np.sqrt(dh)
+                p = np.exp(s - s.max())
+                p /= p.sum()
+                o, mass = p @ v, p @ np.abs(v)
+                serr = 2.0 ** -20 * (np.abs(k) @ np.abs(qv)).max()
+                if tiles:
+                    big = np.abs(qv).max()
+                    serr += big * 2.0 ** -10 / 224 * (np.abs(k) @ (np.abs(qv) < 2.0 ** -9 * big)).max()
+                w = p * S[:n, h // g]
+                small = np.minimum(w, 2.0 ** -27 * w.max()) @ code[:n, h // g]
+                out[b, m, h] = o
+                tol[b, m, h] = 2.0 ** -8 * np.abs(o) + (2.0 ** -11 + 2.0 ** -14 + 2 * serr / np.sqrt(dh)) * mass + 1.01 * small
+    return out, tol
+
+
+def _attend(Bd, ctx, dev, q, n_new=None):
+    B, M = q.shape[:2]
+    out = torch.full(q.shape, 9.0, dtype=torch.bfloat16, device="cuda")
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ctx.fastmtp_kv8_attention(q, Bd.kv8(dev), B, M, out, n_new=None if n_new is None else _i32(n_new), dev_status=st)
+    assert int(st.item()) == 0
+    return out
+
+
+def _within(got, ref, tol, what=""):
+    err = np.abs(got.double().cpu().numpy() - ref)
+    assert np.all(err <= tol), (what, float((err / tol).max()), np.argwhere(~(err <= tol))[:3])
+
+
+# one and two tiles of eight pairs per set, two tiles per warp (64-wide heads; blocks of 5), tiles of 128 pairs
+FORMS = [(8, 1, 128, 16, 1), (28, 4, 128, 16, 4), (8, 2, 64, 16, 1), (8, 1, 64, 16, 3), (8, 1, 64, 16, 8), (8, 1, 128, 5, 6), (8, 1, 128, 16, 8),
+         (28, 4, 128, 16, 64)]
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,page,M", FORMS)
+@pytest.mark.parametrize("apart", [5, 18, 36, 100])
+def test_attention_where_scales_lie_far_apart(Hq, Hkv, dh, page, M, apart):
+    """A few blocks hold nearly all of the probability and have V scales 2^-apart of the others', whose products with their probabilities
+    are less still; for some heads it is the other way round. One block's scale is zero."""
+    Bd, rng = _bd(), np.random.default_rng(71 + apart)
+    lens = [700, 150, 40]
+    ctx = Bd.Context(_shape(Hq, Hkv, dh, page), max_rows=3 * M, max_K=1, max_ctx=1024)
+    kv = _cache(rng, Hkv, dh, page, [L + M for L in lens], M, garbage=False)
+    kv["seq_lens"] = np.asarray(lens, dtype=np.int32)
+    far = (apart * np.log(2.0) + 9) / np.sqrt(dh)         # a key of that size everywhere: a score 9 and more below what the scales lie apart
+    for b, L in enumerate(lens):
+        blocks = -(-(L + M) // page)
+        heavy = {0: (0,), 1: (blocks // 2,), 2: (blocks - 1,)}[b] + (blocks // 3,)
+        for i in range(blocks):
+            pg, low = kv["block_table"][b, i], i in heavy
+            kv["k_scales"][pg] = R.scale_for(far)
+            kv["k_pages"][pg] = R.encode(np.where(low, 0.0, -far / R.scale_for(far)) + 2.0 ** -9 * rng.integers(-2, 3, kv["k_pages"][pg].shape))
+            kv["v_scales"][pg] = 2.0 ** ((0 if low else apart) - 8 + int(rng.integers(0, 3)))
+        kv["v_scales"][kv["block_table"][b, blocks // 2 - 1]] = 0.0
+    qr = np.ones((3, M, Hq, dh))
+    qr[:, :, 1::4] = -0.25
+    q = torch.from_numpy(qr.astype(np.float32)).to(torch.bfloat16).cuda()
+    out = _attend(Bd, ctx, _to_gpu(kv), q)
+    _within(out, *_attention(kv, qr, [M] * 3, page))
+    ctx.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,page,M", [f for f in FORMS if f[4] > 1])
+def test_attention_rows_do_not_meet_later_rows_scales(Hq, Hkv, dh, page, M):
+    """A later row opens a block whose scales are enormous (its values are): the rows before it give the bits they give without it."""
+    Bd, rng = _bd(), np.random.default_rng(81)
+    back = min(M - 1, 2)                                  # rows before the new block
+    lens = [page - back, 20 * page - back, 5 * page - 1]
+    ctx = Bd.Context(_shape(Hq, Hkv, dh, page), max_rows=3 * M, max_K=1, max_ctx=1024)
+    kv = _cache(rng, Hkv, dh, page, [L + M for L in lens], M, garbage=False)
+    kv["seq_lens"] = np.asarray(lens, dtype=np.int32)
+    dev = _to_gpu(kv)
+    q, qr = _bf16(rng, (3, M, Hq, dh), 1.5)
+    good = _attend(Bd, ctx, dev, q)
+    _within(good, *_attention(kv, qr, [M] * 3, page))
+    for b, L in enumerate(lens):
+        for blk in range(-(-L // page), -(-(L + M) // page)):
+            for w in "kv":
+                kv[w + "_scales"][kv["block_table"][b, blk]] *= np.float32(2.0 ** (50 if w == "v" else 3))
+    out = _attend(Bd, ctx, _to_gpu(kv), q)
+    for b, L in enumerate(lens):
+        n = -(-L // page) * page - L
+        assert n > 0 and torch.equal(good[b, :n], out[b, :n]), b
+    _within(out, *_attention(kv, qr, [M] * 3, page))
+    ctx.close()
