@@ -55,9 +55,9 @@ struct fmtp_ctx {
     struct { int mode, B, M, G; } group_memo[16];                  // sequences per launch for (mode, B, M)
     int n_group_memo;
     TmapCache tmaps;                                               // tensor maps of the batched path's GEMM operands
-    // fmtp_selftest_inject_wait_timeout: the next draft call runs with this wait limit and one wait that cannot end
+    // fmtp_selftest_inject_wait_timeout: the next draft (4: 8-bit attention) call runs with this wait limit and one wait that cannot end
     unsigned long long inject_limit_ns;
-    int inject_which;                                              // 0 none, 1 grid barrier of the persistent kernel, 2 ring stage of a GEMM, 3 of the attention
+    int inject_which;                                              // 0 none, 1 grid barrier of the persistent kernel, 2 ring stage of a GEMM, 3 of the attention, 4 of the 8-bit attention
 };
 
 namespace {
@@ -399,7 +399,7 @@ int fmtp_create(const fmtp_shape *sh, fmtp_ctx **out) {
 }
 
 int fmtp_selftest_inject_wait_timeout(fmtp_ctx *c, int limit_ms, int which) {
-    if (!c || which < 1 || which > 3) return FMTP_EINVAL;
+    if (!c || which < 1 || which > 4) return FMTP_EINVAL;
     if (limit_ms < 1 || limit_ms > 1000) return FMTP_EINVAL;      // bounded on purpose
     c->inject_limit_ns = (unsigned long long)limit_ms * 1000000ull;
     c->inject_which = which;
@@ -544,7 +544,7 @@ int fastmtp_draft(fmtp_ctx *c, const fmtp_mtp_w *w, const fmtp_bf16 *h_last, con
             bc.rope_cos = c->s.rope_cos; bc.rope_sin = c->s.rope_sin;
             bc.n_sm = c->n_sm; bc.smem_optin = c->smem_optin; bc.ahead_budget = c->ahead_budget; bc.cache = &c->tmaps;
             bc.wait_limit_ns = kDefaultWaitNs;
-            if (c->inject_which >= 2) { bc.wait_limit_ns = c->inject_limit_ns; bc.inject = c->inject_which; c->inject_which = 0; }
+            if (c->inject_which == 2 || c->inject_which == 3) { bc.wait_limit_ns = c->inject_limit_ns; bc.inject = c->inject_which; c->inject_which = 0; }
             bc.B = (B - b0 < kBatchRows) ? B - b0 : kBatchRows;
             bc.K = K; bc.N = Neff; bc.ids = subset;
             bc.M0 = max_ext; bc.n_ext = n_ext ? n_ext + b0 : nullptr;
@@ -778,6 +778,8 @@ int fastmtp_kv8_attention(fmtp_ctx *c, const fmtp_bf16 *q, long long ldq, const 
     // as many sequences per launch as the partial results have room for, 64 at most
     const size_t fit = c->bws.part_rows / ((size_t)kv8_attention_slots(kv8_shape(c), M) * M);
     const int Gs = fit < (size_t)kBatchRows ? (int)fit : kBatchRows;
+    const bool inject = c->inject_which == 4;
+    if (inject) c->inject_which = 0;
     for (int b0 = 0; b0 < B; b0 += Gs) {
         Kv8AttnCall a;
         std::memset(&a, 0, sizeof(a));
@@ -791,6 +793,8 @@ int fastmtp_kv8_attention(fmtp_ctx *c, const fmtp_bf16 *q, long long ldq, const 
         a.status = dev_status ? dev_status : c->s.status;
         a.n_sm = c->n_sm;
         a.raised = c->tmaps.attn8_raised;
+        a.wait_limit_ns = inject ? c->inject_limit_ns : kDefaultWaitNs;
+        a.extra_arrivals = inject ? 1 : 0;
         int err = kv8_attention(a, static_cast<cudaStream_t>(stream), &c->launches);
         if (err) return cuda_fail(c, (cudaError_t)err);
     }

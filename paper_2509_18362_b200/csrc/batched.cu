@@ -1419,6 +1419,7 @@ int batched_target(const BatchedTargetCall &c, cudaStream_t st, long long *launc
             Kv8AttnCall a{};
             a.sh = s8; a.kv = c.kv8s[l]; a.q = ws.qkv; a.ldq = ld; a.B = c.B; a.M = c.M;
             a.part = ws.att_part; a.xop = ws.xop0; a.ld_xop = ws.ld0; a.status = ws.status; a.n_sm = c.n_sm; a.raised = c.cache->attn8_raised;
+            a.wait_limit_ns = c.wait_limit_ns;
             if ((rc = kv8_attention(a, st, launches))) return rc;
         } else if ((rc = attention(sh, ws, kv, geo, R, c.n_sm, c.wait_limit_ns, 0, c.cache, st, launches))) return rc;
         g = GemmArgs{};

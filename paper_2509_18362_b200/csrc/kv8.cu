@@ -283,6 +283,8 @@ struct Attn8Args {
     bf16_t *out, *xop;
     int ld_xop;
     uint32_t *status;
+    unsigned long long wait_limit_ns;                // kv8_tile_kernel: a wait gives up after this long
+    int extra_arrivals;                              // self-test: a K stage expects copies that are never made
 };
 
 constexpr int kA8Warps = 4, kA8Threads = kA8Warps * 32;
@@ -1000,7 +1002,6 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
 // (64 registers, spilt) 109 us, page look-ups one block ahead 84 us. Without the search for a maximum (block's exponentials first, again where one
 // does not fit f16) wide scores took 70 instead of 66 us.
 constexpr int kT8Pairs = 128, kT8Blk = 64, kT8Threads = 288, kT8Copiers = 128, kT8KStages = 3;
-constexpr unsigned long long kT8WaitNs = 2000000000ull;
 struct Tile8Block {                                  // per V buffer, written beside its values
     float sk[4], sv_log2[4];                         // of the block's 16-token tiles
     uint32_t bad[4];                                 // values that are no number were left out (see kv8_attn_kernel); of each copy warp
@@ -1016,14 +1017,15 @@ struct Tile8Smem {
 };
 static_assert(sizeof(Tile8Block) % 16 == 0 && offsetof(Tile8Block, sv_log2) == 16 && 2 * (Tile8Smem::TOTAL + 1024) <= 228 * 1024, "two CTAs per SM");
 
-__device__ __forceinline__ bool tile8_wait(volatile uint32_t *abort_flag, uint64_t *bar, uint32_t parity) {
+// Waits until the limit or, unless the wait is for what is under way for sure (`always`), until another wait of the CTA has given up.
+__device__ __forceinline__ bool tile8_wait(volatile uint32_t *abort_flag, uint64_t *bar, uint32_t parity, unsigned long long limit_ns, bool always = false) {
     if (mbar_try_wait(bar, parity)) return true;
     const unsigned long long t0 = global_timer_ns();
     uint32_t polls = 0;
     while (!mbar_try_wait(bar, parity)) {
         if ((++polls & 63u) == 0) {
-            if (*abort_flag) return false;
-            if (global_timer_ns() - t0 > kT8WaitNs) {
+            if (*abort_flag && !always) return false;
+            if (global_timer_ns() - t0 > limit_ns) {
                 *abort_flag = 1u;
                 return false;
             }
@@ -1045,7 +1047,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     List8<kT8Pairs, kT8Blk, 2, 3> list(a, smem + Lay::O_LIST);
     if (tid == 32) {
-        for (int i = 0; i < kT8KStages; ++i) { mbar_init(&kfull[i], kT8Copiers); mbar_init(&kempty[i], 1); }
+        for (int i = 0; i < kT8KStages; ++i) { mbar_init(&kfull[i], kT8Copiers + a.extra_arrivals); mbar_init(&kempty[i], 1); }
         for (int i = 0; i < 2; ++i) { mbar_init(&vfull[i], kT8Copiers); mbar_init(&vempty[i], 1); mbar_init(&sfull[i], 1); }
         mbar_init(pready, 128);
         mbar_init(qready, 128);
@@ -1135,7 +1137,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             for (int tb = it.t0; tb < it.t1; tb += kT8Blk, ++n) {
                 const int b = n & 1;
                 const uint32_t ph = (uint32_t)(n >> 1) & 1u, tmem_s = tmem + lane_addr + (uint32_t)(b * kT8Blk);
-                ok = tile8_wait(abort_flag, &vfull[b], ph) && tile8_wait(abort_flag, &sfull[b], ph);
+                ok = tile8_wait(abort_flag, &vfull[b], ph, a.wait_limit_ns) && tile8_wait(abort_flag, &sfull[b], ph, a.wait_limit_ns);
                 if (__any_sync(kFull, !ok)) { ok = false; break; }
                 __syncwarp();
                 tc_fence_after_sync();
@@ -1188,7 +1190,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 l_run *= first ? 1.f : exp2_approx(-mv.p);
                 // ---- the block before has been added up: its probabilities may be overwritten, what it left can be scaled
                 if (n > 0) {
-                    ok = tile8_wait(abort_flag, &vempty[b ^ 1], (uint32_t)((n - 1) >> 1) & 1u);
+                    ok = tile8_wait(abort_flag, &vempty[b ^ 1], (uint32_t)((n - 1) >> 1) & 1u, a.wait_limit_ns);
                     if (__any_sync(kFull, !ok)) { ok = false; break; }
                     tc_fence_after_sync();
                 }
@@ -1237,7 +1239,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             }
             if (!ok) break;
             // ---- the chunk's partial result, as kv8_attn_kernel leaves it; a warp writes four rows at a time
-            ok = tile8_wait(abort_flag, &vempty[(n - 1) & 1], (uint32_t)((n - 1) >> 1) & 1u);
+            ok = tile8_wait(abort_flag, &vempty[(n - 1) & 1], (uint32_t)((n - 1) >> 1) & 1u, a.wait_limit_ns);
             if (__any_sync(kFull, !ok)) break;
             tc_fence_after_sync();
             const uint32_t out_row = prow != kFull && pn > it.t0 ? prow * (uint32_t)a.slots + (uint32_t)it.chunk : kFull;
@@ -1308,7 +1310,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             y.there = x.tok >= 0;
             y.edge = x.edge;
             if (!y.there) return true;
-            if (__any_sync(kFull, !tile8_wait(abort_flag, &kempty[ks], kph ^ 1u))) return false;
+            if (__any_sync(kFull, !tile8_wait(abort_flag, &kempty[ks], kph ^ 1u, a.wait_limit_ns))) return false;
             int pg = x.pg;
             if ((unsigned)pg >= (unsigned)a.kv.num_pages) { atomicOr(a.status, kDevBadPage); pg = 0; }
             const uint32_t slot = (uint32_t)pg * (uint32_t)a.Hkv + (uint32_t)x.kvh, row = slot * (uint32_t)a.page + (uint32_t)x.off;
@@ -1331,7 +1333,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
         const uint32_t v0 = v_at + ((uint32_t)((2 * (piece & 3)) ^ (trow & 7)) << 4), v1 = v_at + ((uint32_t)((2 * (piece & 3) + 1) ^ (trow & 7)) << 4);
         auto convert = [&](Values &y) -> bool {
             const int b = n & 1;
-            if (__any_sync(kFull, !tile8_wait(abort_flag, &vempty[b], ((uint32_t)(n >> 1) & 1u) ^ 1u))) return false;
+            if (__any_sync(kFull, !tile8_wait(abort_flag, &vempty[b], ((uint32_t)(n >> 1) & 1u) ^ 1u, a.wait_limit_ns))) return false;
             Tile8Block *blk = reinterpret_cast<Tile8Block *>(smem + Lay::O_BLK) + b;
             bool bad = false;
             if (y.edge < kT8Blk) {
@@ -1392,10 +1394,10 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             uint32_t kph = 0, qph = 0;
             auto scores = [&](int n, bool fresh) -> bool {
                 if (fresh) {
-                    if (!tile8_wait(abort_flag, qready, qph)) return false;
+                    if (!tile8_wait(abort_flag, qready, qph, a.wait_limit_ns)) return false;
                     qph ^= 1u;
                 }
-                if (!tile8_wait(abort_flag, &kfull[ks], kph)) return false;
+                if (!tile8_wait(abort_flag, &kfull[ks], kph, a.wait_limit_ns)) return false;
                 fence_proxy_async();                 // the copies' shared-memory writes, before the tensor core reads them
                 tc_fence_after_sync();
                 const uint32_t d = tmem + (uint32_t)((n & 1) * kT8Blk), k = kd + (uint32_t)(ks * (Lay::K >> 4));
@@ -1423,7 +1425,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                     }
                 }
                 if (more && !fresh && !(ok = scores(n + 1, false))) break;
-                if (!(ok = tile8_wait(abort_flag, pready, (uint32_t)n & 1u) && tile8_wait(abort_flag, &vfull[n & 1], (uint32_t)(n >> 1) & 1u))) break;
+                if (!(ok = tile8_wait(abort_flag, pready, (uint32_t)n & 1u, a.wait_limit_ns) && tile8_wait(abort_flag, &vfull[n & 1], (uint32_t)(n >> 1) & 1u, a.wait_limit_ns))) break;
                 tc_fence_after_sync();
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
@@ -1434,9 +1436,10 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
                 first = first_next;
                 ++n;
             }
-            // every product issued above is done once this arrival lands
+            // every product issued above is done once this arrival lands: waited for whatever has given up, before tensor memory is
+            // freed and the tiles' shared memory left
             umma_commit(drain);
-            tile8_wait(abort_flag, drain, 0);
+            tile8_wait(abort_flag, drain, 0, a.wait_limit_ns, true);
         }
         __syncwarp();
     }
@@ -1616,6 +1619,7 @@ int kv8_attention(const Kv8AttnCall &c, cudaStream_t st, long long *launches) {
     a.Hq = c.sh.Hq; a.Hkv = c.sh.Hkv; a.gq = c.sh.Hq / c.sh.Hkv; a.page = c.sh.page; a.shift = shift_of(c.sh.page); a.max_ctx = c.sh.max_ctx;
     a.slots = kv8_attention_slots(c.sh, c.M); a.tiles16 = c.sh.page % 16 == 0; a.B = c.B; a.M = c.M; a.q = c.q; a.ldq = c.ldq; a.n_new = c.n_new; a.kv = c.kv; a.part = c.part;
     a.out = c.out; a.xop = c.xop; a.ld_xop = c.ld_xop; a.status = c.status;
+    a.wait_limit_ns = c.wait_limit_ns; a.extra_arrivals = c.extra_arrivals;
     *launches += 2;
     return c.sh.dh == 128 ? attn8_pick<128>(a, c.B * c.M, c.n_sm, c.raised, st) : attn8_pick<64>(a, c.B * c.M, c.n_sm, c.raised, st);
 }

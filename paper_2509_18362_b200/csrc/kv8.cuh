@@ -38,6 +38,8 @@ struct Kv8AttnCall {
     int ld_xop;
     uint32_t *status;
     int n_sm;
+    unsigned long long wait_limit_ns;     // every wait inside the kernels gives up after this long
+    int extra_arrivals;                   // self-test: see fmtp_selftest_inject_wait_timeout
     bool *raised;                         // [4] the context's: kernels whose shared-memory limit has been raised
 };
 int kv8_attention_slots(const Kv8Shape &sh, int M);

@@ -1,5 +1,7 @@
 """The 8-bit K/V cache where it is easily got wrong: sequences that sit a call out, blocks whose scales lie far apart, waits that run
 out, sizes at the ends of their ranges. References in kv8_ref; the bounds stand beside the tests."""
+import time
+
 import numpy as np
 import pytest
 import torch
@@ -190,4 +192,35 @@ def test_attention_rows_do_not_meet_later_rows_scales(Hq, Hkv, dh, page, M):
         n = -(-L // page) * page - L
         assert n > 0 and torch.equal(good[b, :n], out[b, :n]), b
     _within(out, *_attention(kv, qr, [M] * 3, page))
+    ctx.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,M,B", [(8, 1, 8, 3), (28, 4, 64, 2)])
+def test_a_wait_of_the_tiles_of_pairs_that_runs_out_leaves_the_context_usable(Hq, Hkv, M, B):
+    """The next call's stages of keys expect one copy more than is made and its waits are limited to 20 ms: it returns soon after with
+    the timeout flag, and the same call then gives the bits it gave before. An armed context's smaller calls do not wait."""
+    Bd, rng = _bd(), np.random.default_rng(91)
+    dh, page = 128, 16
+    ctx = Bd.Context(_shape(Hq, Hkv, dh, page), max_rows=B * M, max_K=1, max_ctx=2048)
+    lens = [900, 1500, 30][:B]
+    kv = _cache(rng, Hkv, dh, page, [L + M for L in lens], M, garbage=False)
+    kv["seq_lens"] = np.asarray(lens, dtype=np.int32)
+    dev = _to_gpu(kv)
+    q, qr = _bf16(rng, (B, M, Hq, dh))
+    want = _attend(Bd, ctx, dev, q)
+    _within(want, *_attention(kv, qr, [M] * B, page))
+    for _ in range(2):
+        out, st = torch.zeros_like(want), torch.zeros(1, dtype=torch.int32, device="cuda")
+        torch.cuda.synchronize()
+        ctx.fmtp_selftest_inject_wait_timeout(20, 4)
+        t0 = time.time()
+        ctx.fastmtp_kv8_attention(q, Bd.kv8(dev), B, M, out, dev_status=st)
+        torch.cuda.synchronize()
+        assert int(st.item()) == Bd.DEV_TIMEOUT and 0.015 < time.time() - t0 < 2.0
+        assert torch.equal(_attend(Bd, ctx, dev, q), want)
+    ctx.fmtp_selftest_inject_wait_timeout(20, 4)
+    _attend(Bd, ctx, dev, q[:, :1].contiguous())          # (eight pairs: no tiles, and the arming is used up)
+    assert torch.equal(_attend(Bd, ctx, dev, q), want)
+    with pytest.raises(Bd.FastMTPError):
+        ctx.fmtp_selftest_inject_wait_timeout(20, 5)
     ctx.close()
