@@ -211,7 +211,7 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv8_read_kernel(const Read8Ar
     const int s0 = a.start ? min(max(a.start[b], 0), kMaxLen) : 0;
     int n = a.count ? max(a.count[b], 0) : max(kv8_len(a.kv, b) - s0, 0);
     n = min(n, a.max_n);
-    if (n > max_tokens - s0) {
+    if (n > max(max_tokens - s0, 0)) {
         if (lane == 0 && tile == 0) atomicOr(a.status, kDevBadPos);
         n = max(max_tokens - s0, 0);
     }

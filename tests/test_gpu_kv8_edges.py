@@ -224,3 +224,20 @@ def test_a_wait_of_the_tiles_of_pairs_that_runs_out_leaves_the_context_usable(Hq
     with pytest.raises(Bd.FastMTPError):
         ctx.fmtp_selftest_inject_wait_timeout(20, 5)
     ctx.close()
+
+
+def test_read_of_nothing_from_beyond_every_slot():
+    """A start beyond every slot is no fault where nothing is asked for from there."""
+    Bd, rng = _bd(), np.random.default_rng(101)
+    Hkv, dh, page = 2, 64, 16
+    ctx = Bd.Context(_shape(4, Hkv, dh, page), max_rows=8, max_K=1, max_ctx=4096)
+    kv = _cache(rng, Hkv, dh, page, [20, 60, 33], 0)
+    dev = _to_gpu(kv)
+    out = [torch.full((3, 64, Hkv, dh), 7.0, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ctx.fastmtp_kv8_read(Bd.kv8(dev), 3, 64, *out, start=_i32([64, 5000, 2 ** 31 - 1]), count=_i32([0, -1, 0]), dev_status=st)
+    ctx.fastmtp_kv8_read(Bd.kv8(dev), 3, 64, *out, start=_i32([64, 5000, 2 ** 31 - 1]), dev_status=st)       # all that is committed from there on
+    assert int(st.item()) == 0 and all(bool((o == 7.0).all()) for o in out)
+    ctx.fastmtp_kv8_read(Bd.kv8(dev), 3, 64, *out, start=_i32([64, 0, 0]), count=_i32([1, 0, 0]), dev_status=st)
+    assert int(st.item()) == Bd.DEV_BAD_POS and all(bool((o == 7.0).all()) for o in out)
+    ctx.close()
