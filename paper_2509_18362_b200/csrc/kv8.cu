@@ -1598,7 +1598,8 @@ int kv8_read(const Kv8Shape &sh, const Kv8Ptrs &kv, int B, int max_n, const int3
              uint32_t *status, cudaStream_t st, long long *launches) {
     Read8Args a{};
     a.Hkv = sh.Hkv; a.page = sh.page; a.shift = shift_of(sh.page); a.max_ctx = sh.max_ctx; a.B = B; a.max_n = max_n;
-    a.tiles = (max_n + 15) / 16; a.start = start; a.count = count; a.kv = kv; a.out_k = out_k; a.out_v = out_v; a.status = status;
+    const long long slots = (long long)kv.max_pages * sh.page, most = slots < sh.max_ctx ? slots : sh.max_ctx;       // no sequence has more to read
+    a.tiles = (int)(((max_n < most ? max_n : most) + 15) / 16); a.start = start; a.count = count; a.kv = kv; a.out_k = out_k; a.out_v = out_v; a.status = status;
     const long long warps = (long long)B * a.tiles * sh.Hkv, blocks = (warps + kReadWarps - 1) / kReadWarps;
     if (blocks > 0x7fffffffll) return (int)cudaErrorInvalidConfiguration;
     ++*launches;

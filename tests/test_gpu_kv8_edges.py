@@ -241,3 +241,20 @@ def test_read_of_nothing_from_beyond_every_slot():
     ctx.fastmtp_kv8_read(Bd.kv8(dev), 3, 64, *out, start=_i32([64, 0, 0]), count=_i32([1, 0, 0]), dev_status=st)
     assert int(st.item()) == Bd.DEV_BAD_POS and all(bool((o == 7.0).all()) for o in out)
     ctx.close()
+
+
+def test_read_into_room_for_more_than_there_is():
+    """max_n is the caller's stride; only what there is to read takes part, whatever its size."""
+    Bd, rng = _bd(), np.random.default_rng(102)
+    Hkv, dh, page = 2, 64, 16
+    ctx = Bd.Context(_shape(4, Hkv, dh, page), max_rows=8, max_K=1, max_ctx=4096)
+    kv = _cache(rng, Hkv, dh, page, [60], 0)
+    dev = _to_gpu(kv)
+    for max_n in (1000, 2 ** 31 - 1):
+        out = [torch.full((64, Hkv, dh), 7.0, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+        st = torch.zeros(1, dtype=torch.int32, device="cuda")
+        ctx.fastmtp_kv8_read(Bd.kv8(dev), 1, max_n, *out, dev_status=st)
+        for w, o in zip("kv", out):
+            assert np.array_equal(o[:60].double().cpu().numpy(), R.tokens(kv, w, 0, 60, page)) and bool((o[60:] == 7.0).all())
+        assert int(st.item()) == 0
+    ctx.close()
