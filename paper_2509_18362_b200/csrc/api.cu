@@ -485,7 +485,9 @@ int check_target_args(const fmtp_ctx *c, const fmtp_target_w *w, const void *tok
 int target_batched(fmtp_ctx *c, const fmtp_target_w *w, const int32_t *tokens, const fmtp_kv *kvs, const fmtp_kv8 *kv8s, int B, int M,
                    fmtp_bf16 *out_h, fmtp_bf16 *out_logits, int32_t *out_argmax, uint32_t *dev_status, void *stream) {
     if (out_h && !aligned16(out_h)) return FMTP_EINVAL;
-    const int nl = c->shape.n_layers, V = c->shape.vocab, d = c->shape.d, Gs = kBatchRows / M;
+    const int nl = c->shape.n_layers, V = c->shape.vocab, d = c->shape.d, most = kv8s ? kv8_attention_sequences(kv8_shape(c), M) : kBatchRows;
+    const int Gs = kBatchRows / M < most ? kBatchRows / M : most;
+    if (Gs < 1) return FMTP_ESHAPE;
     LayerPtrs layers[kMaxLayers];
     KvPtrs lkv[kMaxLayers];
     Kv8Ptrs lkv8[kMaxLayers];
@@ -775,9 +777,10 @@ int fastmtp_kv8_attention(fmtp_ctx *c, const fmtp_bf16 *q, long long ldq, const 
     const int row = c->shape.n_q_heads * c->shape.head_dim;
     if (ldq < row || ldq % 8) return FMTP_EINVAL;
     if (!kv8_fits(c, *kv) || M > kBatchRows || (long long)B * M > c->shape.max_rows) return FMTP_ESHAPE;
-    // as many sequences per launch as the partial results have room for, 64 at most
+    // as many sequences per launch as the partial results have room for and the list of items can count, 64 at most
     const size_t fit = c->bws.part_rows / ((size_t)kv8_attention_slots(kv8_shape(c), M) * M);
-    const int Gs = fit < (size_t)kBatchRows ? (int)fit : kBatchRows;
+    const int most = kv8_attention_sequences(kv8_shape(c), M), Gs = fit < (size_t)most ? (int)fit : most;
+    if (Gs < 1) return FMTP_ESHAPE;
     const bool inject = c->inject_which == 4;
     if (inject) c->inject_which = 0;
     for (int b0 = 0; b0 < B; b0 += Gs) {

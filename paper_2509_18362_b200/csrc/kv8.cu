@@ -1615,6 +1615,14 @@ int kv8_attention_slots(const Kv8Shape &sh, int M) {
     return few > most ? few : most;
 }
 
+int kv8_attention_sequences(const Kv8Shape &sh, int M) {
+    // a list's costs (see List8) are added up in 31 bits: the sets and strides of attn8_pick's forms, at max_ctx
+    const int pairs = M * (sh.Hq / sh.Hkv), set = pairs <= 8 ? 8 : pairs <= 32 ? 16 : sh.dh == 128 && sh.page % 16 == 0 ? kT8Pairs : 32, stride = pairs <= 8 ? 4 * kA8Blk : 2 * kA8Blk;
+    const long long cost = (3 + 2ll * kv8_attention_slots(sh, M) + (sh.max_ctx + stride - 1) / stride) * sh.Hkv * ((pairs + set - 1) / set);
+    const long long fit = 0x7fffffffll / cost;
+    return fit < kBatchRows ? (int)fit : kBatchRows;
+}
+
 int kv8_attention(const Kv8AttnCall &c, cudaStream_t st, long long *launches) {
     Attn8Args a{};
     a.Hq = c.sh.Hq; a.Hkv = c.sh.Hkv; a.gq = c.sh.Hq / c.sh.Hkv; a.page = c.sh.page; a.shift = shift_of(c.sh.page); a.max_ctx = c.sh.max_ctx;

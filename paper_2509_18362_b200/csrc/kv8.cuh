@@ -43,6 +43,7 @@ struct Kv8AttnCall {
     bool *raised;                         // [4] the context's: kernels whose shared-memory limit has been raised
 };
 int kv8_attention_slots(const Kv8Shape &sh, int M);
+int kv8_attention_sequences(const Kv8Shape &sh, int M);       // that a launch takes, 0 to 64
 int kv8_attention(const Kv8AttnCall &c, cudaStream_t st, long long *launches);
 
 }  // namespace fmtp
