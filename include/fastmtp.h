@@ -343,7 +343,7 @@ int fastmtp_target_step(fmtp_ctx *ctx, const fmtp_target_w *w, const int32_t *to
  * nothing yet) neither counts nor changes. A block written by the call must belong to one sequence only; committed whole
  * blocks may be shared.
  * Positions without a slot (beyond max_pages_per_seq * page_size or max_ctx) and blocks whose page is out of range are skipped
- * and flagged. Any B, M >= 1; uses no workspace; calls on the same inputs give the same cache (also when repeated). */
+ * and flagged. Any B >= 1, 1 <= M <= max_ctx (else FMTP_ESHAPE); uses no workspace; calls on the same inputs give the same cache (also when repeated). */
 int fastmtp_kv8_append(fmtp_ctx *ctx, const fmtp_bf16 *k, const fmtp_bf16 *v, long long ld, const fmtp_kv8 *kv, int B, int M,
                        const int32_t *n_new, uint32_t *dev_status, void *stream);
 

@@ -258,3 +258,22 @@ def test_read_into_room_for_more_than_there_is():
             assert np.array_equal(o[:60].double().cpu().numpy(), R.tokens(kv, w, 0, 60, page)) and bool((o[60:] == 7.0).all())
         assert int(st.item()) == 0
     ctx.close()
+
+
+def test_append_takes_as_many_rows_as_a_sequence_may_have_positions():
+    Bd, rng = _bd(), np.random.default_rng(103)
+    Hkv, dh, page = 2, 64, 16
+    ctx = Bd.Context(_shape(4, Hkv, dh, page), max_rows=8, max_K=1, max_ctx=100)
+    kv = _cache(rng, Hkv, dh, page, [0], 112)
+    dev = _to_gpu(kv)
+    x, ref = _bf16(rng, (1, 101, Hkv, dh))
+    st = torch.zeros(1, dtype=torch.int32, device="cuda")
+    ctx.fastmtp_kv8_append(x, x, Bd.kv8(dev), 1, 100, dev_status=st)
+    for w in "kv":
+        R.append(kv, w, ref, [100], page)
+    _same_cache(dev, kv)
+    assert int(st.item()) == 0
+    with pytest.raises(Bd.FastMTPError) as e:
+        ctx.fastmtp_kv8_append(x, x, Bd.kv8(dev), 1, 101)
+    assert e.value.code == -2
+    ctx.close()
