@@ -277,3 +277,114 @@ def test_append_takes_as_many_rows_as_a_sequence_may_have_positions():
         ctx.fastmtp_kv8_append(x, x, Bd.kv8(dev), 1, 101)
     assert e.value.code == -2
     ctx.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,page,M", FORMS + [(4, 2, 64, 16, 64), (16, 16, 64, 32, 3), (5, 5, 64, 24, 33), (6, 3, 128, 1, 3), (64, 8, 128, 64, 1),
+                                                      (64, 8, 128, 48, 16), (28, 4, 128, 32, 19), (32, 8, 128, 64, 4)])
+def test_attention_is_as_near_as_the_header_says_and_repeats_itself(Hq, Hkv, dh, page, M):
+    """Random values in caches as they are filled, scores from even to peaked, lengths at the edges of stages, blocks and chunks, rows
+    that do not count, single-token contexts; four calls give the same bits."""
+    Bd, rng = _bd(), np.random.default_rng(Hq * 11 + M * 5 + page)
+    lens = [0, 1, 31, 32, 127, 129, 511, 40, 1100] if M <= 8 else [0, 31, 127, 40, 600]
+    B = len(lens)
+    n_new = [M] * (B - 2) + [max(1, M // 2), M]
+    ctx = Bd.Context(_shape(Hq, Hkv, dh, page), max_rows=B * M, max_K=1, max_ctx=2048)
+    kv = _cache(rng, Hkv, dh, page, [L + n for L, n in zip(lens, n_new)], M)
+    kv["seq_lens"] = np.asarray(lens, dtype=np.int32)
+    dev = _to_gpu(kv)
+    q, _ = _bf16(rng, (B, M, Hq, dh))
+    q *= (2.0 ** torch.from_numpy(rng.integers(-6, 3, (B, M, Hq, 1))).double()).to(torch.bfloat16).cuda()
+    out = _attend(Bd, ctx, dev, q, n_new)
+    ref, tol = _attention(kv, q.double().cpu().numpy(), n_new, page)
+    for b, n in enumerate(n_new):
+        _within(out[b, :n], ref[b, :n], tol[b, :n], b)
+    for _ in range(3):
+        assert torch.equal(_attend(Bd, ctx, dev, q, n_new), out)
+    ctx.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,page,M,B", [(28, 4, 128, 16, 1, 64), (28, 4, 128, 16, 4, 17), (28, 4, 128, 16, 64, 4), (32, 8, 128, 16, 1, 2),
+                                                (16, 2, 64, 16, 6, 40), (16, 2, 64, 5, 1, 64)])
+def test_attention_of_full_batches_repeats_itself(Hq, Hkv, dh, page, M, B):
+    """All SMs busy with ragged contexts, four calls in a row beside a copy on another stream, ten times over: the same bits each time."""
+    Bd, rng = _bd(), np.random.default_rng(B)
+    lens = [int(x) for x in rng.integers(0, 30000 if B == 2 else 5000, B)]
+    ctx = Bd.Context(_shape(Hq, Hkv, dh, page), max_rows=B * M, max_K=1, max_ctx=32768)
+    per = [-(-(L + M) // page) for L in lens]
+    g = torch.Generator(device="cuda").manual_seed(B)
+    num = sum(per) + 1
+    order = torch.randperm(num, generator=g, device="cuda").to(torch.int32)
+    table = torch.full((B, max(per)), -1, dtype=torch.int32, device="cuda")
+    at = 0
+    for b, p in enumerate(per):
+        table[b, :p] = order[at:at + p]
+        at += p
+    dev = {"block_table": table, "seq_lens": _i32(lens)}
+    for w in "kv":
+        x = torch.randn((num, Hkv, page, dh), generator=g, device="cuda")
+        dev[w + "_pages"] = (x * 100).clamp(-448, 448).to(torch.float8_e4m3fn).view(torch.uint8)
+        dev[w + "_scales"] = 2.0 ** torch.randint(-9, -4, (num, Hkv), generator=g, device="cuda").float()
+    q = torch.randn((B, M, Hq, dh), generator=g, device="cuda").to(torch.bfloat16)
+    want = _attend(Bd, ctx, dev, q)
+    assert bool(torch.isfinite(want.float()).all())
+    side, big = torch.cuda.Stream(), torch.zeros(1 << 27, device="cuda")
+    outs = [torch.zeros_like(want) for _ in range(4)]
+    for _ in range(10):
+        with torch.cuda.stream(side):
+            big.add_(1.0)
+        for o in outs:
+            o.zero_()
+            ctx.fastmtp_kv8_attention(q, Bd.kv8(dev), B, M, o)
+        assert all(torch.equal(o, want) for o in outs)
+    ctx.close()
+
+
+def test_speculative_decoding_over_8_bit_caches_stays_with_greedy():
+    """Rejected drafts may raise a block's scale, and rows scored together are cut into other chunks: the two are not the same bits. They
+    emit the same tokens up to a near tie (the bound of gpu_util and one bf16 spacing of the logit, as for the target step's own
+    greedy token), behind which they go separate ways."""
+    from paper_2509_18362_b200 import inputs as I
+    from paper_2509_18362_b200 import loop
+
+    from .gpu_util import GAP_TOL
+    Bd, shape, K, n_new, room = _bd(), I.TINY.with_layers(2), 3, 48, 128
+    for seed in (701, 702):
+        Wt = I.target_weights(shape, seed)
+        Wm = I.mtp_weights(shape, seed + 1, embed=Wt["embed"], lm_head=Wt["lm_head"])
+        prompt = [int(t) for t in I.token_ids(seed + 2, (21,), shape.vocab)]
+        ids = torch.from_numpy(I.subset_uniform(shape.vocab, 1024, seed + 3)).cuda()
+        ctx = Bd.Context(shape, max_rows=64, max_K=8, max_ctx=room)
+        dW = Bd.to_device(Wt)
+        blocks = room // shape.page_size
+        pool = (blocks + 1, shape.n_kv_heads, shape.page_size, shape.head_dim)
+
+        def target():
+            return loop.Target(ctx, shape, dW, [dict({w + "_pages": torch.zeros(pool, dtype=torch.uint8, device="cuda") for w in "kv"},
+                                                     **{w + "_scales": torch.ones(pool[:2], device="cuda") for w in "kv"},
+                                                     block_table=_i32([np.random.default_rng(seed + l).permutation(blocks + 1)[:blocks].tolist()]),
+                                                     seq_lens=_i32([0])) for l in range(shape.n_layers)])
+
+        plain = target()
+        _, tok = loop.prefill(plain, prompt)
+        ref, gaps = [tok], [0.0]
+        while len(ref) < n_new + K + 1:
+            _, logits, a = plain.step([[ref[-1]]], want_logits=True)
+            plain.advance(1)
+            top = torch.topk(logits[0, 0].double(), 2).values.tolist()
+            gaps.append((top[0] - top[1]) - 2.0 ** -7 * abs(top[0]))       # (a bf16 spacing is 2^-7 of the value at most)
+            ref.append(int(a.item()))
+
+        def inject(rnd, K, emitted):
+            good = ref[emitted:emitted + K]
+            n_ok = rnd % (K + 1)
+            return list(good[:n_ok]) + [(t + 1) % shape.vocab for t in good[n_ok:]]
+
+        dWm = dict(Bd.to_device({k: v for k, v in Wm.items() if k not in ("embed", "lm_head")}), embed=dW["embed"], lm_head=dW["lm_head"])
+        mkv = Bd.to_device(I.empty_paged_kv(shape, 1, room, seed + 20))
+        tgt = target()
+        out, stats = loop.speculative_decode(tgt, Bd.mtp_w(dWm), mkv, ids, prompt, n_new, K, inject)
+        apart = next((i for i in range(n_new) if out[i] != ref[i]), n_new)
+        assert apart > 0 and (apart == n_new or gaps[apart] < GAP_TOL), (apart, gaps[apart])
+        print(f"8-bit caches, seed {seed}: {apart} of {n_new} tokens alike, accepted {stats['accepted']}")
+        assert apart < n_new or {0, 1, 2, 3} <= set(stats["accepted"])
+        ctx.close()
