@@ -253,10 +253,10 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv8_read_kernel(const Read8Ar
 // the chunk's end, where their results are joined in shared memory; a group's warps take RW tiles each, which share the
 // conversions. (A warp for an item kept the SMs busy for three quarters of the time: an item of 256 tokens took it 25 us.)
 //
-// What bounds it (B200): instructions. A stage of one tile is about 700 of them, 128 conversions and 32 products among them, at 1.3 to 1.9 per cycle and
-// SM with 12 warps; the bytes alone would take two thirds of the time. 64 contexts of 512 to 8192 tokens, 28/4 heads of 128, one row each: 68 us, 4.4
-// TB/s of codes and scales (66% of the measured copy rate); two contexts of 50 000 to 60 000 tokens, 32/8 heads: 50 us, 4.5 TB/s. Short calls are latency: 2048
-// tokens of one sequence 11 us in two launches.
+// What bounds it (B200): instructions. A stage of one tile is about 730 of them, 128 conversions and 32 products among them, at 1.7 per cycle and
+// SM with 12 warps; the bytes alone would take two thirds of the time. 64 contexts of 512 to 8192 tokens, 28/4 heads of 128, one row each: 71 us, 4.2
+// TB/s of codes and scales (65% of the measured copy rate); two contexts of 50 000 to 60 000 tokens, 32/8 heads: 51 us, 4.4 TB/s; 64 contexts of 4096, 16/16
+// heads of 64: 118 us, 4.5 TB/s. Short calls are latency: 2048 tokens of one sequence 12 us in two launches.
 //
 // Both products run on mma.sync.m16n8k16 with f16 operands (sm_100a has no mma.sync on e4m3: the assembler emulates it with fifteen
 // instructions each). K and V are the A operand, 16 tokens or 16 dims, so that eight pairs fill the n side: S^T = K Q^T, O^T = V^T
@@ -269,7 +269,8 @@ __global__ void __launch_bounds__(kReadWarps * 32) kv8_read_kernel(const Read8Ar
 // probability's. A weight is rounded to 2^-11 of itself or 2^-27 of the pair's largest so far at least; a pair's references depend on what it sees alone.
 // The reference of the exponentials is the maximum of a group's first stage and is moved only when a score lies 2^5 above it, so most
 // stages need neither the maximum over all lanes nor a rescaling (partial results carry their reference). As long as all scales are within 2^3 of the first
-// token's, the weights' reference is the probabilities' times that scale, and a weight costs a product.
+// token's, the weights' reference is the probabilities' times that scale, and a weight costs a product. (The 64 contexts above: 68.7 us with one reference for all
+// pairs, the largest scale that anyone met, which could leave a row nothing; 73.3 with an exponential for each weight whose scale is not the first one's.)
 // A stage of the ring is 32 tokens of K and V with their scales, copied by the warps that read them (16-byte cp.async, any page
 // size).
 struct Attn8Args {
@@ -299,8 +300,8 @@ constexpr float kQ8 = 32.f;                          // queries below 448 * 32
 // enough for a context to keep many CTAs busy, long enough for the partial results (dh + 4 fp32 words for each pair and chunk,
 // 512 bytes against 256 bytes of K/V per token at dh = 128) to stay a small part of the traffic: up to `few` chunks until a chunk is
 // 2^base long, up to `most` chunks of that and more tokens beyond.
-// (few = 8 / 16 for 33 to 128 pairs, one set of tiles: 112 pairs of 1 x 4000 tokens 26.2 / 20.4 us, of 4 x 4000 28.9 / 23.2; for 448: 29.4 / 23.2 and
-// 57.6 / 65.7, the sets fill the SMs and each chunk's result costs.)
+// (few = 8 / 16 for 33 to 128 pairs, one set of tiles: 112 pairs of 1 x 4000 tokens 26.3 / 20.7 us, of 4 x 4000 29.3 / 23.8; for 448: 29.6 / 23.1 and
+// 58.4 / 67.3, the sets fill the SMs and each chunk's result costs.)
 struct Chunk8 { int first, few, base, most; };       // first and base: powers of two
 __host__ __device__ __forceinline__ Chunk8 chunk8_rule(int pairs) {
     return pairs <= 8 ? Chunk8{7, 16, 9, 128} : pairs <= 32 ? Chunk8{7, 16, 9, 64} : pairs <= 128 ? Chunk8{8, 16, 9, 32} : Chunk8{8, 8, 9, 32};
@@ -998,7 +999,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
 // block n + 1's scores before block n's values, which wait for its probabilities. Two CTAs per SM: one's softmax runs beside the other's
 // products. What bounds it (B200): issue and latency of softmax and conversions, 5 200 warp instructions per block at 1.8 per cycle and SM (a
 // block's exponentials alone are 512 cycles of an SM, its products 256), and the ends: 4 us of set-up and first loads, 5 us of
-// queries, 3 us for each chunk's result. Four contexts of 3500 to 4200 tokens, 64 rows each, 28/4 heads: 61 us with the join (7 us); held scores
+// queries, 3 us for each chunk's result. Four contexts of 3500 to 4200 tokens, 64 rows each, 28/4 heads: 61.6 us with the join (7 us); held scores
 // (64 registers, spilt) 109 us, page look-ups one block ahead 84 us. Without the search for a maximum (block's exponentials first, again where one
 // does not fit f16) wide scores took 70 instead of 66 us.
 constexpr int kT8Pairs = 128, kT8Blk = 64, kT8Threads = 288, kT8Copiers = 128, kT8KStages = 3;
@@ -1456,7 +1457,7 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
 
 // ---- a row's chunks joined in ascending order. A warp for a (query head, row), DH / 32 dims per lane; its lanes hold the weights of
 // 32 chunks, and a batch of the chunks' values is requested before they are known. WARPS > 1: the warps of a block take the 32s in turn and are joined in
-// their order (few rows of many chunks).
+// their order (contexts that may be long: few rows of many chunks).
 template <int DH, int WARPS>
 __global__ void __launch_bounds__(128) kv8_merge_kernel(const Attn8Args a) {
     chain_release();
@@ -1553,7 +1554,8 @@ int attn8_launch(void (*kern)(const Attn8Args), int ctas, int threads, int smem,
         *raised = e == cudaSuccess;
     }
     if (e == cudaSuccess) e = launch_chained(kern, dim3(ctas), dim3(threads), (size_t)smem, st, a);
-    // (more than 32 chunks: long contexts of a few rows)
+    // (by what the context's max_ctx allows, not by the call's lengths, which the host does not know: room for more than 32 chunks has a result's
+    // warps share them)
     if (e == cudaSuccess) e = a.slots > 32 ? launch_chained(kv8_merge_kernel<DH, 4>, dim3(a.Hq * rows), dim3(128), 0, st, a)
                                            : launch_chained(kv8_merge_kernel<DH, 1>, dim3((a.Hq * rows + 3) / 4), dim3(128), 0, st, a);
     return (int)e;
@@ -1565,11 +1567,11 @@ int attn8_warps(const Attn8Args &a, int rows, int n_sm, bool *raised, cudaStream
 }
 
 // One tile of pairs: four groups of one warp; up to four: two groups of two, a set for every two tiles. More: tiles of 128 pairs on tcgen05 where
-// a 16-token tile has one scale (dh = 128), else two groups of two warps with two tiles each. Measured, us, 28/4 heads of 128, chunks of 512 (tcgen05 / two tiles per warp): 35
-// pairs of 1 x 4000 tokens 25.1 / 23.4, of 16 x 1000 22.2 / 32.5, 84 pairs of 4 x 4000 28.0 / 43.0, 448 pairs of 1 x 4000 29.3 / 44.2, of 4
-// x 4000 57.8 / 131.9. At 28 pairs tcgen05 loses on few sequences (1 x 4000: 24.6 against 15.1 with groups of two; 17 ragged ones 42.9
-// against 34.1) and wins on many (48 x 2000: 79 against 97). At 28 pairs two tiles per warp: 44 us against 36 (the 17 ragged ones); at 448 pairs one
-// tile per warp: 146 us against 133.
+// a 16-token tile has one scale (dh = 128), else two groups of two warps with two tiles each. By the pairs alone, not by the batch or its contexts, so that what a sequence
+// gives does not depend on what it is called with, though that is not the faster form everywhere. Measured, us, 28/4 heads of 128, chunks as they are (tcgen05 / the other form): 28
+// pairs of 1 x 4000 tokens 19.4 / 15.4, of 17 x up to 4100 49.6 / 50.3, of 48 x 2000 89.0 / 101.5; 35 pairs of 1 x 4000 19.5 / 19.2, of 16 x 1000 22.4 /
+// 34.8; 84 pairs of 4 x 4000 22.1 / 44.2; 448 pairs of 1 x 4000 29.6 / 47.2, of 4 x 4000 58.5 / 141.8. Without tcgen05, 16/2 heads, 4 x 4000 tokens: 128 pairs, heads of 64,
+// 25.3, of 128 in blocks of 24 tokens 32.2; 512 pairs, heads of 64, 52.1.
 template <int DH>
 int attn8_pick(const Attn8Args &a, int rows, int n_sm, bool *raised, cudaStream_t st) {
     const int pairs = a.M * a.gq;
