@@ -741,7 +741,7 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
             const bool first = tb == tb0;
             if (first) {                             // the group's first token: whoever sees any of its tokens sees this one
                 sv_ref = __shfl_sync(0xffffffffu, sv[0][0], 0);
-                if (!(sv_ref > 0.f && sv_ref < INFINITY)) sv_ref = 1.f;
+                if (!(sv_ref >= 0x1p-120f && sv_ref <= 0x1p120f)) sv_ref = 1.f;          // (one whose inverse need not be right: weights go their own way)
                 sv_inv = __fdividef(1.0f, sv_ref);
             }
             float ym[RW][2], most = -INFINITY;

@@ -388,3 +388,26 @@ def test_speculative_decoding_over_8_bit_caches_stays_with_greedy():
         print(f"8-bit caches, seed {seed}: {apart} of {n_new} tokens alike, accepted {stats['accepted']}")
         assert apart < n_new or {0, 1, 2, 3} <= set(stats["accepted"])
         ctx.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,page,M", FORMS)
+@pytest.mark.parametrize("low,high,span", [(-132, -127, 0), (-134, -120, 5)])
+def test_attention_over_values_near_the_ends_of_the_numbers(Hq, Hkv, dh, page, M, low, high, span):
+    """Scales of blocks between 2^low and 2^high (and single ones 2^span beyond):
+    values below 2^-111 under scales that have lost bits themselves. (Beside the bound, half a step of the smallest bf16, 2^-134,
+    and of fp32's, 2^-150, of each of 32 sums.)"""
+    Bd, rng = _bd(), np.random.default_rng(111 + M)
+    lens = [700, 33, 5]
+    ctx = Bd.Context(_shape(Hq, Hkv, dh, page), max_rows=3 * M, max_K=1, max_ctx=1024)
+    kv = _cache(rng, Hkv, dh, page, [L + M for L in lens], M, garbage=False)
+    kv["seq_lens"] = np.asarray(lens, dtype=np.int32)
+    kv["v_scales"][:] = 2.0 ** rng.integers(low, high + 1, kv["v_scales"].shape)
+    if span:
+        kv["v_scales"][rng.random(kv["v_scales"].shape) < 0.2] = 2.0 ** (high + span if high > 0 else low - span)
+    if high > 0:                                          # codes below 16: values below 2^126
+        kv["v_pages"] = R.encode(R.TABLE[kv["v_pages"]] / 32)
+    q, qr = _bf16(rng, (3, M, Hq, dh))
+    out = _attend(Bd, ctx, _to_gpu(kv), q)
+    ref, tol = _attention(kv, qr, [M] * 3, page)
+    _within(out, ref, tol + 2.0 ** -134 + 32 * 2.0 ** -150)
+    ctx.close()
