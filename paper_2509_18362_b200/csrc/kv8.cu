@@ -294,6 +294,8 @@ constexpr float kP8Log2 = 6.f;                       // probabilities relative t
 constexpr float kW8Max = 15.f, kW8Min = 2.f;          // the largest weight so far is kept between 2^2 and 2^15
 constexpr float kNear8 = 8.f;                        // V scales within this factor of the reference leave weights and probabilities one reference,
 constexpr float kP8Max = 11.f;                       // which is moved when a probability comes out above 2^11 (times eight: below 2^15)
+constexpr float kBig8 = 0x1p-26f, kBig8Log2 = 26.f;   // partial results of scales above 1 are kept times 2^-26, with a reference 2^26 higher: their sums
+                                                     // (up to 2^15 for each token) of large values stay numbers
 constexpr float kQ8 = 32.f;                          // queries below 448 * 32
 
 // Tokens of a chunk: a function of the sequence's committed length and of the call's rows per sequence, never of the batch. Short
@@ -916,8 +918,11 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
             float m_ref[2], back[2];
 #pragma unroll
             for (int e = 0; e < 2; ++e) {
-                back[e] = vo[r][e] == 0.f ? sv_ref : exp2f(__log2f(sv_ref) - vo[r][e]);
-                m_ref[e] = pn[r][e] > tb0 ? kP8Log2 - mo[r][e] : -INFINITY;
+                const float lb = (vo[r][e] == 0.f ? 0.f : __log2f(sv_ref)) - vo[r][e];
+                const bool large = vo[r][e] == 0.f ? sv_ref > 1.f : lb > 0.f;
+                back[e] = vo[r][e] == 0.f ? (large ? sv_ref * kBig8 : sv_ref) : exp2f(large ? lb - kBig8Log2 : lb);
+                m_ref[e] = pn[r][e] > tb0 ? kP8Log2 - mo[r][e] + (large ? kBig8Log2 : 0.f) : -INFINITY;
+                if (large) l_run[r][e] *= kBig8;
 #pragma unroll
                 for (int x = 4; x < 32; x <<= 1) l_run[r][e] += __shfl_xor_sync(0xffffffffu, l_run[r][e], x);
             }
@@ -1245,8 +1250,10 @@ __global__ void __launch_bounds__(kT8Threads, 2) kv8_tile_kernel(const __grid_co
             tc_fence_after_sync();
             const uint32_t out_row = prow != kFull && pn > it.t0 ? prow * (uint32_t)a.slots + (uint32_t)it.chunk : kFull;
             float *mine = a.part + (size_t)out_row * part8_ld(DH);
-            const float back = exp2f(-vo);
-            if (out_row != kFull) *reinterpret_cast<float2 *>(mine + DH) = make_float2(kP8Log2 - mo, l_run);
+            const bool large = vo < 0.f;
+            const float back = exp2f(large ? -vo - kBig8Log2 : -vo);
+            if (out_row != kFull)
+                *reinterpret_cast<float2 *>(mine + DH) = make_float2(kP8Log2 - mo + (large ? kBig8Log2 : 0.f), large ? l_run * kBig8 : l_run);
             uint32_t to[8];                          // rows of the four that a warp writes at a time
 #pragma unroll
             for (int i = 0; i < 8; ++i) to[i] = __shfl_sync(kFull, out_row, 4 * i + (lane >> 3));

@@ -391,9 +391,9 @@ def test_speculative_decoding_over_8_bit_caches_stays_with_greedy():
 
 
 @pytest.mark.parametrize("Hq,Hkv,dh,page,M", FORMS)
-@pytest.mark.parametrize("low,high,span", [(-132, -127, 0), (-134, -120, 5)])
+@pytest.mark.parametrize("low,high,span", [(112, 115, 0), (110, 117, 5), (-132, -127, 0), (-134, -120, 5)])
 def test_attention_over_values_near_the_ends_of_the_numbers(Hq, Hkv, dh, page, M, low, high, span):
-    """Scales of blocks between 2^low and 2^high (and single ones 2^span beyond):
+    """Scales of blocks between 2^low and 2^high (and single ones 2^span beyond): values up to 2^126 whose mean is a finite number, and
     values below 2^-111 under scales that have lost bits themselves. (Beside the bound, half a step of the smallest bf16, 2^-134,
     and of fp32's, 2^-150, of each of 32 sums.)"""
     Bd, rng = _bd(), np.random.default_rng(111 + M)
