@@ -377,9 +377,9 @@ int fastmtp_kv8_attention(fmtp_ctx *ctx, const fmtp_bf16 *q, long long ldq, cons
  * fastmtp_kv8_append and fastmtp_kv8_attention (rotated queries, keys and values rounded to bf16 first). Runs on the batched
  * path whatever B is (groups of up to 64 rows); M <= 64. Because a block's scale may have grown for a draft that was
  * rejected since, speculative and plain greedy decoding agree within rounding, not bit for bit. What it saves is memory; time only where
- * contexts are long or many: at the 7B shape four layers take 740 us against 835 for 64 ragged sequences of up to 8192 tokens and 489
+ * contexts are long or many: at the 7B shape four layers take 752 us against 834 for 64 ragged sequences of up to 8192 tokens and 489
  * against 494 for four rows of one sequence at 8192, but 442 against 344 for one row at 2048 (which fastmtp_target_step gives its
- * persistent kernel) and 4 to 12% more for four rows of each of 3 to 17 sequences. */
+ * persistent kernel) and 5 to 12% more for four rows of each of 3 to 17 sequences. */
 int fastmtp_target_step_kv8(fmtp_ctx *ctx, const fmtp_target_w *w, const int32_t *tokens, const fmtp_kv8 *layer_kvs, int B, int M,
                             fmtp_bf16 *out_h, fmtp_bf16 *out_logits, int32_t *out_argmax, uint32_t *dev_status, void *stream);
 
