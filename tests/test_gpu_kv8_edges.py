@@ -411,3 +411,20 @@ def test_attention_over_values_near_the_ends_of_the_numbers(Hq, Hkv, dh, page, M
     ref, tol = _attention(kv, qr, [M] * 3, page)
     _within(out, ref, tol + 2.0 ** -134 + 32 * 2.0 ** -150)
     ctx.close()
+
+
+@pytest.mark.parametrize("Hq,Hkv,dh,page,M", FORMS)
+@pytest.mark.parametrize("keys", [105, 60, -60, -105])
+def test_attention_of_large_keys_and_small_queries(Hq, Hkv, dh, page, M, keys):
+    """Keys times 2^keys under queries times 2^-keys: the scores are those of neither."""
+    Bd, rng = _bd(), np.random.default_rng(121 + M)
+    lens = [300, 33, 5]
+    ctx = Bd.Context(_shape(Hq, Hkv, dh, page), max_rows=3 * M, max_K=1, max_ctx=1024)
+    kv = _cache(rng, Hkv, dh, page, [L + M for L in lens], M, garbage=False)
+    kv["seq_lens"] = np.asarray(lens, dtype=np.int32)
+    kv["k_scales"] = (kv["k_scales"].astype(np.float64) * 2.0 ** keys).astype(np.float32)
+    q, _ = _bf16(rng, (3, M, Hq, dh))
+    q = (q.double() * 2.0 ** -keys).to(torch.bfloat16)
+    out = _attend(Bd, ctx, _to_gpu(kv), q)
+    _within(out, *_attention(kv, q.double().cpu().numpy(), [M] * 3, page))
+    ctx.close()
