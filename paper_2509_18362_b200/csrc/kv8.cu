@@ -380,8 +380,8 @@ __device__ __forceinline__ float min_nan(float a, float b) {         // NaN if o
     asm("min.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
     return r;
 }
-__device__ __forceinline__ void cp_async4(uint32_t dst, const void *src, uint32_t bytes) {
-    asm volatile("cp.async.ca.shared.global [%0], [%1], 4, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
+__device__ __forceinline__ void cp_async4(uint32_t dst, const void *src) {
+    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(dst), "l"(src) : "memory");
 }
 // How far (log2) the references of a pair's probabilities and weights move in a stage whose largest exponents are ym and zm: a reference above which
 // something lies too far, or which is not there yet, to 2^6 below the largest. The weights' moves along with the probabilities' (so that
@@ -592,10 +592,9 @@ __global__ void __launch_bounds__(kA8Threads, Attn8Smem<DH, RW, WR>::CTAS) kv8_a
                     cp_async16_off_hint<0>(d + Lay::KV, a.kv.v_pages + off, n, policy);
                 }
             }
-            if (wr == 0) {
-                const uint32_t n = cur.tok + lane < cur.t1 ? 4u : 0u;
-                cp_async4(sb + 2 * Lay::KV + lane * 4, a.kv.k_scales + slot, n);
-                cp_async4(sb + 2 * Lay::KV + kA8Blk * 4 + lane * 4, a.kv.v_scales + slot, n);
+            if (wr == 0) {                           // (beyond what is seen: the last token's scales, so that the stage's need not differ)
+                cp_async4(sb + 2 * Lay::KV + lane * 4, a.kv.k_scales + slot);
+                cp_async4(sb + 2 * Lay::KV + kA8Blk * 4 + lane * 4, a.kv.v_scales + slot);
             }
             if (++cslot == S) cslot = 0;
             cur.tok += STRIDE;
